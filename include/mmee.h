@@ -7,6 +7,10 @@
  * the mappings that do not fit the on-chip buffer and returns the k best under one objective.
  * All model arithmetic runs in CUDA kernels (sm_100a); there is no CPU fallback.
  *
+ * Beside the search, the library runs the chains that it searches mappings for, on tensors in device memory:
+ * attention over states of another length (mmee_attention) and the gated feed-forward block (mmee_gated_ffn),
+ * each with its gradients.
+ *
  * Plain C ABI: structs of fixed-width integers and doubles, raw pointers.  Every pointer
  * argument says below whether it is HOST or DEVICE memory.  All functions return an int status
  * (MMEE_OK = 0); nothing throws, aborts or traps.
@@ -414,6 +418,65 @@ int mmee_kernel_timing(mmee_handle_t* handle, int enable);
  * Synchronous; a few milliseconds; allocates and frees 4 KB of device memory.
  */
 int mmee_alu_peak(double out[4]);
+
+/* ------------------------------------------------------------------------------------------------
+ * The chains themselves, run on this GPU.  Their sizes come as the workload that a mapping is searched
+ * for; tensors are DEVICE memory of 16-bit values (word_bytes = 2), 16-byte aligned, the last dimension
+ * contiguous, every other stride a multiple of eight elements (a dimension of one entry may have any).
+ * Calls are asynchronous on cuda_stream, allocate nothing, keep nothing from call to call and may be
+ * captured into a graph; sums are kept in 32 bits and no result depends on the order in which blocks
+ * finish.  A call that returns another status than MMEE_OK has launched nothing or (MMEE_ERR_CUDA) left
+ * its outputs undefined.
+ * ---------------------------------------------------------------------------------------------- */
+#define MMEE_F16   0u
+#define MMEE_BF16  1u
+
+#define MMEE_ACT_SILU     0u   /* g / (1 + exp(-g))                                            */
+#define MMEE_ACT_GELU     1u   /* g * Phi(g), by the error function                            */
+#define MMEE_ACT_RELU     2u   /* max(g, 0); its derivative at 0 is 0                          */
+#define MMEE_ACT_SIGMOID  3u   /* 1 / (1 + exp(-g))                                            */
+
+/*
+ * mmee_gated_ffn -- hidden = act(x w_gate^T) * (x w_up^T),  y = hidden w_down^T.
+ * Workload: a two-GEMM chain as one instance (batch = q_heads = kv_heads = 1): seq_q = tokens (I), d_qk = width of
+ * x (K), seq_kv = width of the hidden values (L), d_v = width of y (J).  Widths are multiples of eight.
+ * Gate and up are 32-bit sums; hidden is rounded once to the tensors' type, y once.
+ */
+typedef struct {
+    uint32_t dtype;                          /* MMEE_F16 or MMEE_BF16                             */
+    uint32_t activation;                     /* MMEE_ACT_*                                        */
+    const void *x;                           /* tokens x K                                        */
+    const void *w_gate, *w_up;               /* L x K each                                        */
+    const void *w_down;                      /* J x L                                             */
+    int64_t  x_stride, w_gate_stride, w_up_stride, w_down_stride;   /* elements from row to row   */
+    void    *hidden;                         /* out: tokens x L, contiguous (backward: in)        */
+    float   *kept;                           /* out, may be NULL: gate, then up, tokens x L each, for the backward
+                                                pass (there: in)                                  */
+    void    *y;                              /* out: tokens x J, contiguous (backward: not used)  */
+} mmee_gated_ffn_t;
+int mmee_gated_ffn(const mmee_workload_t* workload, const mmee_gated_ffn_t* f, void* cuda_stream);
+
+/*
+ * mmee_gated_ffn_backward -- the gradients of x and the three weights for a gradient d_y of y, from the
+ * `hidden` and `kept` that the forward call wrote for the same x and weights.  The gradients of gate and up
+ * are rounded once to the tensors' type, each result once.
+ */
+typedef struct {
+    const void *d_y;                         /* tokens x J                                        */
+    int64_t  d_y_stride;
+    void    *d_x, *d_w_gate, *d_w_up, *d_w_down;   /* out: shaped as x and the weights, contiguous */
+    void    *workspace;                      /* DEVICE, mmee_gated_ffn_workspace bytes, for this call alone until it ends */
+    uint64_t workspace_bytes;
+} mmee_gated_ffn_grad_t;
+int mmee_gated_ffn_backward(const mmee_workload_t* workload, const mmee_gated_ffn_t* f, const mmee_gated_ffn_grad_t* g,
+                            void* cuda_stream);
+int mmee_gated_ffn_workspace(const mmee_workload_t* workload, uint64_t* bytes);
+
+/*
+ * mmee_chain_status -- MMEE_OK, or MMEE_ERR_TIMEOUT once after a wait inside one of the chains' kernels ran out
+ * (a few seconds; its outputs are not a result).  Waits for the device's work.
+ */
+int mmee_chain_status(void);
 
 #ifdef __cplusplus
 }

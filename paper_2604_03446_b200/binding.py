@@ -15,6 +15,8 @@ OBJ_ENERGY, OBJ_LATENCY, OBJ_EDP, OBJ_ENERGY_LCAP, OBJ_LATENCY_ECAP = 0, 1, 2, 3
 TILE_POW2, TILE_ALL_DIVISORS = 0, 1
 ORD_NORECOMP2, ORD_ALL6 = 0, 1
 FUSE_FUSED, FUSE_SOFTMAX_IN_OP1, FUSE_SEPARATE = 1, 2, 4
+F16, BF16 = 0, 1
+ACT_SILU, ACT_GELU, ACT_RELU, ACT_SIGMOID = range(4)
 MAX_TOPK = 16
 NO_INDEX = 2 ** 64 - 1
 OK, ERR_ARG, ERR_OVERFLOW, ERR_QUANTUM, ERR_NO_FEASIBLE, ERR_CUDA, ERR_TIMEOUT, ERR_RANGE, ERR_CHECK = range(9)
@@ -22,7 +24,7 @@ OK, ERR_ARG, ERR_OVERFLOW, ERR_QUANTUM, ERR_NO_FEASIBLE, ERR_CUDA, ERR_TIMEOUT, 
 EXPORTS = ("mmee_create", "mmee_search", "mmee_search_host", "mmee_destroy", "mmee_trim", "mmee_search_static", "mmee_num_candidates", "mmee_num_tilings",
            "mmee_num_rows", "mmee_strerror", "mmee_last_cuda_error", "mmee_eval", "mmee_decode", "mmee_dump_keys", "mmee_filter_flags", "mmee_solve_host", "mmee_pareto_front", "mmee_pareto_front_bs_da", "mmee_search_shapes",
            "mmee_query_vector", "mmee_recompute_flag", "mmee_row_pruning_keep", "mmee_last_search_stats", "mmee_kernel_timing",
-           "mmee_alu_peak")
+           "mmee_alu_peak", "mmee_gated_ffn", "mmee_gated_ffn_backward", "mmee_gated_ffn_workspace", "mmee_chain_status")
 
 
 class Workload(C.Structure):
@@ -68,6 +70,18 @@ class LaunchStats(C.Structure):
                 ("rows_per_tiling", C.c_uint32), ("rows_evaluated_per_tiling", C.c_uint32),
                 ("exact_path_visits", C.c_uint64), ("create_ms", C.c_float), ("reserved", C.c_uint32),
                 ("rows_tested", C.c_uint64)]
+
+
+class GatedFfn(C.Structure):
+    _fields_ = [("dtype", C.c_uint32), ("activation", C.c_uint32),
+                ("x", C.c_void_p), ("w_gate", C.c_void_p), ("w_up", C.c_void_p), ("w_down", C.c_void_p),
+                ("x_stride", C.c_int64), ("w_gate_stride", C.c_int64), ("w_up_stride", C.c_int64),
+                ("w_down_stride", C.c_int64), ("hidden", C.c_void_p), ("kept", C.c_void_p), ("y", C.c_void_p)]
+
+
+class GatedFfnGrad(C.Structure):
+    _fields_ = [("d_y", C.c_void_p), ("d_y_stride", C.c_int64), ("d_x", C.c_void_p), ("d_w_gate", C.c_void_p),
+                ("d_w_up", C.c_void_p), ("d_w_down", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
 
 
 RESULT_BYTES = C.sizeof(Result)
@@ -132,6 +146,10 @@ def library():
     L.mmee_last_search_stats.argtypes = [H, C.POINTER(LaunchStats)]
     L.mmee_kernel_timing.argtypes = [H, C.c_int]
     L.mmee_alu_peak.argtypes = [C.POINTER(C.c_double)]
+    L.mmee_gated_ffn.argtypes = [C.POINTER(Workload), C.POINTER(GatedFfn), C.c_void_p]
+    L.mmee_gated_ffn_backward.argtypes = [C.POINTER(Workload), C.POINTER(GatedFfn), C.POINTER(GatedFfnGrad), C.c_void_p]
+    L.mmee_gated_ffn_workspace.argtypes = [C.POINTER(Workload), C.POINTER(C.c_uint64)]
+    L.mmee_chain_status.argtypes = []
     _lib = L
     return L
 
@@ -335,6 +353,97 @@ def mmee_alu_peak():
     out = (C.c_double * 4)()
     _check(library().mmee_alu_peak(out), "mmee_alu_peak")
     return list(out)
+
+
+def _refuse(where: str, why: str):
+    raise MmeeError(ERR_ARG, "%s: %s" % (where, why))
+
+
+def _chain_tensors(where: str, rank: int, **tensors):
+    """(type code, device) that the tensors of one call share: CUDA tensors of one 16-bit type on one device."""
+    import torch
+    first = next(iter(tensors.values()))
+    for name, t in tensors.items():
+        if not isinstance(t, torch.Tensor) or t.dim() != rank:
+            _refuse(where, "%s is not a tensor of %d dimensions" % (name, rank))
+        if t.dtype != first.dtype or t.device != first.device:
+            _refuse(where, "%s is of another type or on another device" % name)
+        if t.stride(-1) != 1 and t.shape[-1] > 1:
+            _refuse(where, "the last dimension of %s is not contiguous" % name)
+    if first.dtype not in (torch.bfloat16, torch.float16) or first.device.type != "cuda":
+        _refuse(where, "bfloat16 or float16 tensors on a CUDA device are wanted")
+    return (BF16 if first.dtype == torch.bfloat16 else F16), first.device
+
+
+def _on(device, stream):
+    """What a call on tensors of `device` runs under, so that its launches and the memory it takes are the device's and the
+    stream's; nothing where both are current already."""
+    import contextlib
+    import torch
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _ffn_call(where, x, w_gate, w_up, w_down, activation):
+    code, device = _chain_tensors(where, 2, x=x, w_gate=w_gate, w_up=w_up, w_down=w_down)
+    tokens, d_in = x.shape
+    d_ff, d_out = w_gate.shape[0], w_down.shape[0]
+    if w_gate.shape != (d_ff, d_in) or w_up.shape != (d_ff, d_in) or w_down.shape != (d_out, d_ff):
+        _refuse(where, "w_gate and w_up are (inner, in), w_down is (out, inner), x is (tokens, in)")
+    w = Workload(batch=1, q_heads=1, kv_heads=1, seq_q=tokens, seq_kv=d_ff, d_qk=d_in, d_v=d_out, word_bytes=2)
+    f = GatedFfn(dtype=code, activation=activation, x=x.data_ptr(), w_gate=w_gate.data_ptr(), w_up=w_up.data_ptr(),
+                 w_down=w_down.data_ptr(), x_stride=x.stride(0), w_gate_stride=w_gate.stride(0), w_up_stride=w_up.stride(0),
+                 w_down_stride=w_down.stride(0))
+    return w, f, device
+
+
+def mmee_gated_ffn(x, w_gate, w_up, w_down, activation: int = ACT_SILU, save: bool = False, stream=None):
+    """y = (act(x w_gate^T) * (x w_up^T)) w_down^T: (y, saved).  x: (tokens, in), w_gate and w_up: (inner, in), w_down: (out, inner),
+    bfloat16 or float16.  saved: what mmee_gated_ffn_backward needs where `save`, otherwise None.  Asynchronous."""
+    import torch
+    w, f, device = _ffn_call("mmee_gated_ffn", x, w_gate, w_up, w_down, activation)
+    with _on(device, stream):
+        hidden = torch.empty((w.seq_q, w.seq_kv), dtype=x.dtype, device=device)
+        kept = torch.empty((2, w.seq_q, w.seq_kv), dtype=torch.float32, device=device) if save else None
+        y = torch.empty((w.seq_q, w.d_v), dtype=x.dtype, device=device)
+        f.hidden, f.y, f.kept = hidden.data_ptr(), y.data_ptr(), kept.data_ptr() if save else None
+        code = (_lib or library()).mmee_gated_ffn(w, f, _current_stream())
+    if code:
+        _check(code, "mmee_gated_ffn")
+    return y, ((hidden, kept) if save else None)
+
+
+def mmee_gated_ffn_backward(d_y, x, w_gate, w_up, w_down, saved, activation: int = ACT_SILU, stream=None):
+    """The gradients (d_x, d_w_gate, d_w_up, d_w_down) of mmee_gated_ffn for a gradient d_y of y; `saved` is what the forward call
+    with the same x, weights and activation returned.  Asynchronous."""
+    import torch
+    where = "mmee_gated_ffn_backward"
+    w, f, device = _ffn_call(where, x, w_gate, w_up, w_down, activation)
+    _chain_tensors(where, 2, x=x, d_y=d_y)
+    hidden, kept = saved
+    if d_y.shape != (w.seq_q, w.d_v):
+        _refuse(where, "d_y is (tokens, out)")
+    if (hidden.shape != (w.seq_q, w.seq_kv) or hidden.dtype != x.dtype or kept.shape != (2, w.seq_q, w.seq_kv) or
+            kept.dtype != torch.float32 or not hidden.is_contiguous() or not kept.is_contiguous() or
+            hidden.device != device or kept.device != device):
+        _refuse(where, "saved is not what the forward call for these tensors returned")
+    need = C.c_uint64()
+    _check(library().mmee_gated_ffn_workspace(w, need), where)
+    with _on(device, stream):
+        space = torch.empty(need.value, dtype=torch.uint8, device=device)
+        grads = [torch.empty(t.shape, dtype=x.dtype, device=device) for t in (x, w_gate, w_up, w_down)]
+        f.hidden, f.kept = hidden.data_ptr(), kept.data_ptr()
+        g = GatedFfnGrad(d_y.data_ptr(), d_y.stride(0), *[t.data_ptr() for t in grads], space.data_ptr(), need.value)
+        code = library().mmee_gated_ffn_backward(w, f, g, _current_stream())
+    if code:
+        _check(code, where)
+    return tuple(grads)
+
+
+def mmee_chain_status() -> None:
+    """Raises once after a wait inside a chain's kernel ran out (its outputs are not a result).  Waits for the device."""
+    _check(library().mmee_chain_status(), "mmee_chain_status")
 
 
 def read_results(buf, n: int):

@@ -1,0 +1,64 @@
+// Host side shared by the calls that run a chain: tensor maps, device limits, the status of past launches.
+#include "mmee_chain.h"
+
+namespace mmee {
+
+namespace {
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+    static const EncodeTiled f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return f;
+}
+
+}  // namespace
+
+int tile_map(CUtensorMap* map, bool bf16, const void* base, uint32_t rank, const uint64_t* extent, const int64_t* stride, uint32_t rows) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return cuda_status(cudaErrorNotSupported);
+    cuuint64_t dims[5], bytes[5];
+    cuuint32_t box[5], step[5];
+    for (uint32_t i = 0; i < rank; ++i) {
+        dims[i] = extent[i];
+        box[i] = i == 0 ? 64 : i == 1 ? rows : 1;
+        step[i] = 1;
+    }
+    // (a dimension of one entry may carry any stride: a legal one stands in)
+    for (uint32_t i = 0; i + 1 < rank; ++i) bytes[i] = extent[i + 1] == 1 ? 16 : (cuuint64_t)stride[i] * 2;
+    const CUresult r = encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank,
+                              const_cast<void*>(base), dims, bytes, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? MMEE_OK : MMEE_ERR_ARG;
+}
+
+int sm_count(uint32_t* out) {
+    int device = 0, n = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device);
+    if (e != cudaSuccess) return cuda_status(e);
+    *out = (uint32_t)n;
+    return MMEE_OK;
+}
+
+int allow_smem(const void* kernel, uint32_t bytes) {
+    return cuda_status(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+}
+
+}  // namespace mmee
+
+extern "C" int mmee_chain_status(void) {
+    uint32_t f = 0;
+    const int rc = mmee::ffn_gave_up(&f);
+    return rc ? rc : f ? MMEE_ERR_TIMEOUT : MMEE_OK;
+}

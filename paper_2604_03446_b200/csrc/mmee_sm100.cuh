@@ -1,0 +1,203 @@
+// The sm_100a instructions that the chain kernels are built from: mbarriers with limited waits, TMA loads, tensor memory
+// and the fifth-generation matrix instructions, with the descriptors of 128-byte-swizzled tiles.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace mmee {
+
+constexpr uint32_t kRowBytes = 128;            // one row of a swizzled tile: 64 values of 16 bits
+constexpr uint32_t kGroupBytes = 8 * kRowBytes;    // eight rows: the unit of the swizzle pattern
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ bool elect_one() {
+    uint32_t is;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}" : "=r"(is));
+    return is != 0;
+}
+
+// --- mbarriers ------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void mbar_init_visible() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}"
+                 : "=r"(done)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    return done != 0;
+}
+
+__device__ __forceinline__ uint64_t global_ns() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+
+constexpr uint64_t kWaitNs = 4000000000ull;    // no wait of a sound launch comes near this
+
+static __device__ __noinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up) {
+    const uint64_t begin = global_ns();
+    while (!mbar_try(bar, parity)) {
+        if (gave_up && *gave_up) return false;
+        if (global_ns() - begin > kWaitNs) {
+            if (gave_up) *gave_up = 1;
+            return false;
+        }
+    }
+    return true;
+}
+
+// Waits until the barrier's phase of this parity is over.  False: the wait ran out, here or in another role of the CTA
+// (`gave_up`, one word of shared memory); the role then leaves its loop.  With gave_up = nullptr: a wait of its own.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up) {
+    for (int i = 0; i < 64; ++i)
+        if (mbar_try(bar, parity)) return true;
+    return mbar_wait_long(bar, parity, gave_up);
+}
+
+// --- TMA ------------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void tma_prefetch(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+__device__ __forceinline__ void tma_load_2d(uint32_t to, const CUtensorMap* map, uint32_t bar, int32_t x, int32_t y) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(to),
+                 "l"(map), "r"(bar), "r"(x), "r"(y)
+                 : "memory");
+}
+
+__device__ __forceinline__ void tma_load_4d(uint32_t to, const CUtensorMap* map, uint32_t bar, int32_t x, int32_t y, int32_t z, int32_t w) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(to),
+                 "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
+                 : "memory");
+}
+
+// What threads wrote to shared memory, seen by the tensor cores.
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// --- tensor memory --------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void tmem_alloc(uint32_t* to_smem, uint32_t columns) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(to_smem)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void tmem_free(uint32_t base, uint32_t columns) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns) : "memory");
+}
+
+__device__ __forceinline__ void tcgen05_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tcgen05_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+#define MMEE_R8(r, i) "=r"((r)[(i)]), "=r"((r)[(i) + 1]), "=r"((r)[(i) + 2]), "=r"((r)[(i) + 3]), "=r"((r)[(i) + 4]), "=r"((r)[(i) + 5]), "=r"((r)[(i) + 6]), "=r"((r)[(i) + 7])
+#define MMEE_RW8(r, i) "+r"((r)[(i)]), "+r"((r)[(i) + 1]), "+r"((r)[(i) + 2]), "+r"((r)[(i) + 3]), "+r"((r)[(i) + 4]), "+r"((r)[(i) + 5]), "+r"((r)[(i) + 6]), "+r"((r)[(i) + 7])
+#define MMEE_IN8(r, i) "r"((r)[(i)]), "r"((r)[(i) + 1]), "r"((r)[(i) + 2]), "r"((r)[(i) + 3]), "r"((r)[(i) + 4]), "r"((r)[(i) + 5]), "r"((r)[(i) + 6]), "r"((r)[(i) + 7])
+
+// 32 columns of the warp's 32 lanes; the values are there after tmem_loaded of the same registers.
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+        "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : MMEE_R8(r, 0), MMEE_R8(r, 8), MMEE_R8(r, 16), MMEE_R8(r, 24)
+        : "r"(addr));
+}
+
+// The registers are operands, so that no use of them moves before the wait.
+__device__ __forceinline__ void tmem_loaded32(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : MMEE_RW8(r, 0), MMEE_RW8(r, 8), MMEE_RW8(r, 16), MMEE_RW8(r, 24)::"memory");
+}
+
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, "
+        "%20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr),
+        MMEE_IN8(r, 0), MMEE_IN8(r, 8), MMEE_IN8(r, 16), MMEE_IN8(r, 24)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
+                 MMEE_IN8(r, 0), MMEE_IN8(r, 8)
+                 : "memory");
+}
+
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// --- matrix instructions --------------------------------------------------------------------------------------------
+
+// Shared-memory descriptor of a tile with 128-byte swizzle.  Reduction along the row (K-major): rows in groups of eight,
+// `lbo` unused.  Reduction along the rows (MN-major): `lbo` is the distance between blocks of 64 columns.  A step of 16
+// along the reduction adds 32 bytes (K-major, within a block of 64) or two groups of rows (MN-major).
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr, uint32_t lbo) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(kGroupBytes >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+constexpr uint64_t kStepK = 32 >> 4, kStepMN = (2 * kGroupBytes) >> 4;
+
+// Instruction descriptor: 16-bit operands of one type, 32-bit sums.
+__host__ __device__ constexpr uint32_t mma_desc(bool bf16, uint32_t m, uint32_t n, bool a_mn, bool b_mn) {
+    return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | ((n >> 3) << 17) | ((m >> 4) << 24);
+}
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b),
+                 "r"(desc), "r"((uint32_t)add)
+                 : "memory");
+}
+
+// A from tensor memory (two values of 16 bits to a column).
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b),
+                 "r"(desc), "r"((uint32_t)add)
+                 : "memory");
+}
+
+// The barrier gets an arrival when all matrix instructions that this thread has issued are done.
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// --- values ---------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t r;
+    if (BF16)
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+template <bool BF16>
+__device__ __forceinline__ float2 unpack2(uint32_t v) {
+    if (BF16) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+    return __half22float2(*reinterpret_cast<const __half2*>(&v));
+}
+
+}  // namespace mmee
