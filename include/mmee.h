@@ -437,6 +437,29 @@ int mmee_alu_peak(double out[4]);
 #define MMEE_ACT_SIGMOID  3u   /* 1 / (1 + exp(-g))                                            */
 
 /*
+ * mmee_attention -- for every query head h of sequence b, with the key head h / (q_heads / kv_heads):
+ * o = softmax(scale q k^T) v over the first kv_len[b] keys, lse = log sum exp(scale q k^T).
+ * Workload: all fields; d_qk and d_v are multiples of eight up to MMEE_ATTENTION_MAX_D, q_heads a multiple of kv_heads.
+ * A row without valid keys (or whose scores are all -infinity) gives o = 0 and lse = -infinity; what lies behind a
+ * sequence's valid keys, infinities and NaN too, changes nothing.  Scores and sums are kept in 32 bits, probabilities are
+ * rounded once to the tensors' type (the tensor cores need that), o once.
+ */
+#define MMEE_ATTENTION_MAX_D  128u
+typedef struct {
+    uint32_t dtype;                          /* MMEE_F16 or MMEE_BF16                             */
+    float    scale;                          /* positive and finite                               */
+    const void *q, *k, *v;                   /* [batch][token][head][d], any order of strides     */
+    void    *o;                              /* out (backward: in)                                */
+    int64_t  q_stride[3], k_stride[3], v_stride[3], o_stride[3];   /* elements: batch, token, head */
+    float   *lse;                            /* out, may be NULL (backward: in): [batch][q_heads][seq_q], contiguous */
+    const int32_t *kv_len;                   /* DEVICE, one per sequence, clamped to 0..seq_kv; NULL: all keys */
+    void    *workspace;                      /* DEVICE, mmee_attention_workspace bytes (0: may be NULL), for this call alone until it ends */
+    uint64_t workspace_bytes;
+} mmee_attention_t;
+int mmee_attention(const mmee_workload_t* workload, const mmee_attention_t* a, void* cuda_stream);
+int mmee_attention_workspace(const mmee_workload_t* workload, uint64_t* bytes);
+
+/*
  * mmee_gated_ffn -- hidden = act(x w_gate^T) * (x w_up^T),  y = hidden w_down^T.
  * Workload: a two-GEMM chain as one instance (batch = q_heads = kv_heads = 1): seq_q = tokens (I), d_qk = width of
  * x (K), seq_kv = width of the hidden values (L), d_v = width of y (J).  Widths are multiples of eight.

@@ -24,7 +24,8 @@ OK, ERR_ARG, ERR_OVERFLOW, ERR_QUANTUM, ERR_NO_FEASIBLE, ERR_CUDA, ERR_TIMEOUT, 
 EXPORTS = ("mmee_create", "mmee_search", "mmee_search_host", "mmee_destroy", "mmee_trim", "mmee_search_static", "mmee_num_candidates", "mmee_num_tilings",
            "mmee_num_rows", "mmee_strerror", "mmee_last_cuda_error", "mmee_eval", "mmee_decode", "mmee_dump_keys", "mmee_filter_flags", "mmee_solve_host", "mmee_pareto_front", "mmee_pareto_front_bs_da", "mmee_search_shapes",
            "mmee_query_vector", "mmee_recompute_flag", "mmee_row_pruning_keep", "mmee_last_search_stats", "mmee_kernel_timing",
-           "mmee_alu_peak", "mmee_gated_ffn", "mmee_gated_ffn_backward", "mmee_gated_ffn_workspace", "mmee_chain_status")
+           "mmee_alu_peak", "mmee_gated_ffn", "mmee_gated_ffn_backward", "mmee_gated_ffn_workspace",
+           "mmee_attention", "mmee_attention_workspace", "mmee_chain_status")
 
 
 class Workload(C.Structure):
@@ -70,6 +71,13 @@ class LaunchStats(C.Structure):
                 ("rows_per_tiling", C.c_uint32), ("rows_evaluated_per_tiling", C.c_uint32),
                 ("exact_path_visits", C.c_uint64), ("create_ms", C.c_float), ("reserved", C.c_uint32),
                 ("rows_tested", C.c_uint64)]
+
+
+class Attention(C.Structure):
+    _fields_ = [("dtype", C.c_uint32), ("scale", C.c_float), ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("o", C.c_void_p), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
+                ("o_stride", C.c_int64 * 3), ("lse", C.c_void_p), ("kv_len", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_uint64)]
 
 
 class GatedFfn(C.Structure):
@@ -149,6 +157,8 @@ def library():
     L.mmee_gated_ffn.argtypes = [C.POINTER(Workload), C.POINTER(GatedFfn), C.c_void_p]
     L.mmee_gated_ffn_backward.argtypes = [C.POINTER(Workload), C.POINTER(GatedFfn), C.POINTER(GatedFfnGrad), C.c_void_p]
     L.mmee_gated_ffn_workspace.argtypes = [C.POINTER(Workload), C.POINTER(C.c_uint64)]
+    L.mmee_attention.argtypes = [C.POINTER(Workload), C.POINTER(Attention), C.c_void_p]
+    L.mmee_attention_workspace.argtypes = [C.POINTER(Workload), C.POINTER(C.c_uint64)]
     L.mmee_chain_status.argtypes = []
     _lib = L
     return L
@@ -439,6 +449,46 @@ def mmee_gated_ffn_backward(d_y, x, w_gate, w_up, w_down, saved, activation: int
     if code:
         _check(code, where)
     return tuple(grads)
+
+
+def _attention_call(where, q, k, v, kv_len, scale):
+    import torch
+    code, device = _chain_tensors(where, 4, q=q, k=k, v=v)
+    batch, seq_q, q_heads, d_qk = q.shape
+    seq_kv, kv_heads = k.shape[1], k.shape[2]
+    if k.shape != (batch, seq_kv, kv_heads, d_qk) or v.shape[:3] != k.shape[:3]:
+        _refuse(where, "q is (batch, tokens, heads, d), k and v have one batch, length and number of heads, q and k one width")
+    if kv_len is not None and (not isinstance(kv_len, torch.Tensor) or kv_len.dtype != torch.int32 or kv_len.shape != (batch,) or
+                               kv_len.device != device or not kv_len.is_contiguous()):
+        _refuse(where, "kv_len is a contiguous int32 tensor, one entry per sequence, on the tensors' device")
+    w = Workload(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, v.shape[3], 2)
+    a = Attention(dtype=code, scale=d_qk ** -0.5 if scale is None and d_qk else scale or 0.0, q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(),
+                  q_stride=q.stride()[:3], k_stride=k.stride()[:3], v_stride=v.stride()[:3],
+                  kv_len=None if kv_len is None else kv_len.data_ptr())
+    return w, a, device
+
+
+def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
+    """softmax(scale q k^T) v over each sequence's first kv_len keys: (o, lse).  q: (batch, tokens, q_heads, d_qk), k: (batch, keys,
+    kv_heads, d_qk), v: (batch, keys, kv_heads, d_v), bfloat16 or float16; kv_len: int32 tensor with an entry per sequence, None: all keys;
+    scale: d_qk ** -0.5 unless given.  lse: float32 (batch, q_heads, tokens).  Asynchronous."""
+    import torch
+    w, a, device = _attention_call("mmee_attention", q, k, v, kv_len, scale)
+    lib, need = _lib or library(), C.c_uint64()
+    with _on(device, stream):
+        code = lib.mmee_attention_workspace(w, need)
+        if code:
+            _check(code, "mmee_attention")
+        o = torch.empty((w.batch, w.seq_q, w.q_heads, w.d_v), dtype=q.dtype, device=device)
+        lse = torch.empty((w.batch, w.q_heads, w.seq_q), dtype=torch.float32, device=device)
+        if need.value:
+            space = torch.empty(need.value, dtype=torch.uint8, device=device)
+            a.workspace, a.workspace_bytes = space.data_ptr(), need.value
+        a.o, a.lse, a.o_stride[:] = o.data_ptr(), lse.data_ptr(), o.stride()[:3]
+        code = lib.mmee_attention(w, a, _current_stream())
+    if code:
+        _check(code, "mmee_attention")
+    return o, lse
 
 
 def mmee_chain_status() -> None:

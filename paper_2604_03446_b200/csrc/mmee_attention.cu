@@ -1,0 +1,563 @@
+// Attention over states of another length, run: S = Q K^T scale, P = softmax over a sequence's valid keys, O = P V, and the
+// gradients of Q, K and V.
+//
+// The forward kernel keeps scores in tensor memory: a CTA holds up to two tiles of 128 query rows, keys and values stream
+// through shared memory by TMA in tiles of 128, S = Q K^T lands in tensor memory, a warpgroup per query tile (a thread per
+// row, so that no reduction crosses threads) turns it into P in place, which the next matrix instruction takes from there.
+// While one tile's scores are turned, the tensor cores work for the other.
+#include "mmee_chain.h"
+#include "mmee_sm100.cuh"
+
+namespace mmee {
+
+namespace {
+
+__device__ uint32_t g_gave_up;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr uint32_t kTile = 128;                        // query rows and keys of a tile
+
+// A row's sums refer to a maximum that is moved only when the scores pass it by more than this (in powers of two): the
+// results are the same up to rounding, and moving it means going through the row's sums in tensor memory.
+constexpr float kSlack = 8.f;
+// fp16 has its smallest normal value at 2^-14: probabilities are kept 2^7 larger (at most 2^15 with the slack), which the
+// division by their sum takes out again.
+template <bool BF16>
+__device__ constexpr float kBias = BF16 ? 0.f : 7.f;
+
+struct Strides {
+    int64_t batch, token, head;        // elements
+};
+
+struct AttentionParams {
+    uint32_t batch, q_heads, group, seq_q, seq_kv, d_qk, d_v;
+    uint32_t splits, tiles_per_split;  // parts that the keys are cut into, tiles of each
+    float scale;
+    const int32_t* kv_len;
+    void* o;
+    Strides os;
+    float* lse;                        // [batch][q_heads][seq_q]
+    float *part_o, *part_lse;          // splits > 1: [split][batch][q_heads][seq_q] rows of d_v; log2 of the sums
+};
+
+__device__ __forceinline__ uint32_t valid_keys(const int32_t* kv_len, uint32_t b, uint32_t seq_kv) {
+    if (!kv_len) return seq_kv;
+    const int32_t n = __ldg(kv_len + b);
+    return n < 0 ? 0u : min((uint32_t)n, seq_kv);
+}
+
+// Zeroes rows [from, to) of a tile of `blocks` blocks of 64 columns, by a whole warp: keys behind a sequence's end may hold
+// anything, and nothing times infinity would count.  (The swizzle moves sixteen-byte pieces within a row only.)
+__device__ __forceinline__ void zero_rows(uint32_t tile, uint32_t blocks, uint32_t from, uint32_t to) {
+    const uint32_t pieces = (to - from) * (kRowBytes / 16);
+    for (uint32_t b = 0; b < blocks; ++b)
+        for (uint32_t i = threadIdx.x & 31u; i < pieces; i += 32)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + b * kTile * kRowBytes + from * kRowBytes + i * 16), "r"(0) : "memory");
+    fence_async_shared();
+    __syncwarp();
+}
+
+// Writes 8 * n values of a row.
+template <bool BF16>
+__device__ __forceinline__ void write_row(void* to, int64_t at, const float* v, uint32_t from, uint32_t cols) {
+    uint4* const p = reinterpret_cast<uint4*>(static_cast<uint16_t*>(to) + at + from);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (from + 8 * j < cols)
+            p[j] = make_uint4(pack2<BF16>(v[8 * j], v[8 * j + 1]), pack2<BF16>(v[8 * j + 2], v[8 * j + 3]),
+                              pack2<BF16>(v[8 * j + 4], v[8 * j + 5]), pack2<BF16>(v[8 * j + 6], v[8 * j + 7]));
+}
+
+// --- forward --------------------------------------------------------------------------------------------------------
+
+template <int DK, int DV>
+struct ForwardShape {
+    static constexpr uint32_t kQ = (DK / 64) * kTile * kRowBytes, kV = (DV / 64) * kTile * kRowBytes;
+    static constexpr uint32_t kRing = 2;
+    static constexpr uint32_t smem(uint32_t tiles) { return tiles * kQ + kRing * (kQ + kV) + 1024; }
+};
+
+template <int DK, int DV, int TILES, bool BF16>
+__global__ void __launch_bounds__(TILES * 128 + 64, 1)
+attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
+                 const AttentionParams p) {
+    using Shape = ForwardShape<DK, DV>;
+    constexpr uint32_t kRing = Shape::kRing, kLoad = TILES * 4, kMma = kLoad + 1;
+    constexpr uint32_t kColumns = TILES * (128 + DV) <= 256 ? 256 : 512;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t bars[TILES * 4 + 4 * kRing + 1];
+    __shared__ uint32_t tmem_base, gave_up;
+
+    const uint32_t b = blockIdx.z / p.splits, split = blockIdx.z % p.splits, head = blockIdx.y;
+    const uint32_t q0 = blockIdx.x * TILES * kTile;
+    const uint32_t tiles = (p.seq_q - q0 <= kTile) ? 1 : TILES;
+    const uint32_t keys = valid_keys(p.kv_len, b, p.seq_kv);
+    const uint32_t t0 = split * p.tiles_per_split, t_all = (keys + kTile - 1) / kTile;
+    const uint32_t n = t0 < t_all ? min(p.tiles_per_split, t_all - t0) : 0;      // key tiles of this CTA
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+
+    const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
+    const uint32_t bar0 = smem_addr(bars);
+    auto q_full = [&](uint32_t t) { return bar0 + 8 * t; };
+    auto s_full = [&](uint32_t t) { return bar0 + 8 * (TILES + t); };
+    auto p_full = [&](uint32_t t) { return bar0 + 8 * (2 * TILES + t); };
+    auto o_full = [&](uint32_t t) { return bar0 + 8 * (3 * TILES + t); };
+    auto k_full = [&](uint32_t s) { return bar0 + 8 * (4 * TILES + s); };
+    auto k_empty = [&](uint32_t s) { return bar0 + 8 * (4 * TILES + kRing + s); };
+    auto v_full = [&](uint32_t s) { return bar0 + 8 * (4 * TILES + 2 * kRing + s); };
+    auto v_empty = [&](uint32_t s) { return bar0 + 8 * (4 * TILES + 3 * kRing + s); };
+    const uint32_t drained = bar0 + 8 * (4 * TILES + 4 * kRing);
+    auto q_tile = [&](uint32_t t) { return base + t * Shape::kQ; };
+    auto k_tile = [&](uint32_t s) { return base + TILES * Shape::kQ + s * Shape::kQ; };
+    auto v_tile = [&](uint32_t s) { return base + (TILES + kRing) * Shape::kQ + s * Shape::kV; };
+
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (uint32_t t = 0; t < TILES; ++t) {
+            mbar_init(q_full(t), 1);
+            mbar_init(s_full(t), 1);
+            mbar_init(p_full(t), 128);
+            mbar_init(o_full(t), 1);
+        }
+        for (uint32_t s = 0; s < kRing; ++s) {
+            mbar_init(k_full(s), 1);
+            mbar_init(k_empty(s), 1);
+            mbar_init(v_full(s), 1);
+            mbar_init(v_empty(s), 1);
+        }
+        mbar_init(drained, 1);
+        mbar_init_visible();
+    }
+    if (warp == kMma) tmem_alloc(&tmem_base, kColumns);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = tmem_base;
+    volatile uint32_t* const lost = &gave_up;
+    auto s_col = [&](uint32_t t) { return tmem + t * 128; };
+    auto o_col = [&](uint32_t t) { return tmem + TILES * 128 + t * DV; };
+
+    if (warp == kLoad) {
+        if (elect_one() && n) {
+            const int32_t h = (int32_t)head, hk = (int32_t)(head / p.group), bb = (int32_t)b;
+            uint32_t k_sent = 0, v_sent = 0;
+            bool sound = true;
+            auto load_q = [&](uint32_t t) {
+                mbar_expect(q_full(t), Shape::kQ);
+                for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(q_tile(t) + j * kTile * kRowBytes, &mq, q_full(t), 64 * j, (int32_t)(q0 + t * kTile), h, bb);
+            };
+            load_q(0);
+            for (uint32_t i = 0; i < n; ++i) {
+                const uint32_t s = i % kRing, turn = ((i / kRing) & 1) ^ 1;
+                const int32_t row = (int32_t)((t0 + i) * kTile);
+                if (!(sound = mbar_wait(k_empty(s), turn, lost))) break;
+                mbar_expect(k_full(s), Shape::kQ);
+                for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(k_tile(s) + j * kTile * kRowBytes, &mk, k_full(s), 64 * j, row, hk, bb);
+                ++k_sent;
+                if (i == 0)
+                    for (uint32_t t = 1; t < tiles; ++t) load_q(t);
+                if (!(sound = mbar_wait(v_empty(s), turn, lost))) break;
+                mbar_expect(v_full(s), Shape::kV);
+                for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(v_tile(s) + j * kTile * kRowBytes, &mv, v_full(s), 64 * j, row, hk, bb);
+                ++v_sent;
+            }
+            if (!sound) {                              // what is in flight lands before the CTA ends
+                for (uint32_t t = 0; t < (k_sent ? tiles : 1); ++t) mbar_wait(q_full(t), 0, nullptr);
+                for (uint32_t s = 0; s < kRing; ++s) {
+                    if (k_sent > s) mbar_wait(k_full(s), ((k_sent - 1 - s) / kRing) & 1, nullptr);
+                    if (v_sent > s) mbar_wait(v_full(s), ((v_sent - 1 - s) / kRing) & 1, nullptr);
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == kMma) {
+        constexpr uint32_t desc_s = mma_desc(BF16, kTile, kTile, false, false);
+        const uint32_t desc_o = mma_desc(BF16, kTile, (p.d_v + 15) / 16 * 16, false, true);
+        const uint32_t steps_s = (p.d_qk + 15) / 16;
+        auto scores = [&](uint32_t t, uint32_t s) {    // S_t = Q_t K^T
+            const uint64_t dq = tile_desc(q_tile(t), 16), dk = tile_desc(k_tile(s), 16);
+            for (uint32_t k = 0; k < steps_s; ++k) {
+                const uint64_t at = (uint64_t)(k / 4) * (kTile * kRowBytes >> 4) + (k % 4) * kStepK;
+                mma_ss(s_col(t), dq + at, dk + at, desc_s, k);
+            }
+            mma_commit(s_full(t));
+        };
+        bool sound = n > 0;
+        if (sound) {
+            sound = mbar_wait(k_full(0), 0, lost);
+            for (uint32_t t = 0; t < tiles && sound; ++t) {
+                if (!(sound = mbar_wait(q_full(t), 0, lost))) break;
+                tcgen05_fence_after();
+                if (elect_one()) {
+                    scores(t, 0);
+                    if (t + 1 == tiles) mma_commit(k_empty(0));
+                }
+                __syncwarp();
+            }
+        }
+        for (uint32_t i = 0; i < n && sound; ++i) {
+            const uint32_t s = i % kRing, s1 = (i + 1) % kRing;
+            const uint32_t valid = min(kTile, keys - (t0 + i) * kTile), steps_o = (valid + 15) / 16;
+            if (!(sound = mbar_wait(v_full(s), (i / kRing) & 1, lost))) break;
+            if (valid % 16) zero_rows(v_tile(s), DV / 64, valid, steps_o * 16);
+            if (i + 1 < n && !(sound = mbar_wait(k_full(s1), ((i + 1) / kRing) & 1, lost))) break;
+            for (uint32_t t = 0; t < tiles; ++t) {
+                if (!(sound = mbar_wait(p_full(t), i & 1, lost))) break;
+                tcgen05_fence_after();
+                if (elect_one()) {
+                    const uint64_t dv = tile_desc(v_tile(s), kTile * kRowBytes);
+                    for (uint32_t k = 0; k < steps_o; ++k) mma_ts(o_col(t), s_col(t) + 8 * k, dv + k * kStepMN, desc_o, i | k);
+                    if (t + 1 == tiles) mma_commit(v_empty(s));
+                    if (i + 1 < n) {
+                        scores(t, s1);
+                        if (t + 1 == tiles) mma_commit(k_empty(s1));
+                    } else {
+                        mma_commit(o_full(t));
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    } else if (warp / 4 < tiles) {
+        const uint32_t t = warp / 4, row = (warp % 4) * 32 + lane, lanes = ((warp % 4) * 32) << 16;
+        const float sl2 = p.scale * kLog2e;
+        float m = -INFINITY, l = 0.f;                  // reference and sum, in powers of two
+        bool sound = true;
+        for (uint32_t i = 0; i < n; ++i) {
+            if (!(sound = mbar_wait(s_full(t), i & 1, lost))) break;
+            tcgen05_fence_after();
+            // The first 64 scores stay in registers; the others are read for the maximum and once more for their
+            // probabilities, while the tensor memory is idle (128 at once would spill).
+            const int valid = (int)min(kTile, keys - (t0 + i) * kTile);
+            uint32_t x[64], y[32];
+            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            auto take_most = [&](const uint32_t* v) {
+#pragma unroll
+                for (int c = 0; c < 32; ++c) top[c & 3] = fmaxf(top[c & 3], __uint_as_float(v[c]));
+            };
+            auto cut = [&](uint32_t* v, int from) {    // scores of keys behind the end
+                if (valid < from + 32) {
+#pragma unroll
+                    for (int c = 0; c < 32; ++c)
+                        if (from + c >= valid) v[c] = 0xff800000u;
+                }
+            };
+            tmem_load32(s_col(t) + lanes + 96, y);
+            tmem_load32(s_col(t) + lanes + 64, x);
+            tmem_loaded32(y);
+            tmem_loaded32(x);
+            cut(y, 96);
+            take_most(y);
+            tmem_load32(s_col(t) + lanes, y);
+            cut(x, 64);
+            take_most(x);
+            tmem_load32(s_col(t) + lanes + 32, x + 32);
+            tmem_loaded32(y);
+            tmem_loaded32(x + 32);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) x[c] = y[c];
+            cut(x, 0);
+            take_most(x);
+            cut(x + 32, 32);
+            take_most(x + 32);
+            const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sl2;
+            if (i == 0) {
+                m = most;
+            } else if (__any_sync(0xffffffffu, most > m + kSlack)) {
+                // The sums so far: all matrix instructions issued before these scores are done, P V of the last tile too.
+                const float to = most > m + kSlack ? most : m, by = to == m ? 1.f : exp2_fast(m - to);
+                m = to;
+                l *= by;
+#pragma unroll 1
+                for (int c = 0; c < DV; c += 16) {     // (few registers: the scores are live)
+                    uint32_t o[16];
+                    tmem_load16(o_col(t) + lanes + c, o);
+                    tmem_loaded16(o);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * by);
+                    tmem_store16(o_col(t) + lanes + c, o);
+                }
+            }
+            const float from = (m == -INFINITY ? 0.f : m) - kBias<BF16>;
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            auto turn = [&](const uint32_t* v, int at) {       // 32 scores into probabilities
+                uint32_t pk[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float a = exp2_fast(fmaf(__uint_as_float(v[2 * j]), sl2, -from));
+                    const float e = exp2_fast(fmaf(__uint_as_float(v[2 * j + 1]), sl2, -from));
+                    sum[j & 3] += a + e;
+                    pk[j] = pack2<BF16>(a, e);
+                }
+                tmem_store16(s_col(t) + lanes + at / 2, pk);
+            };
+            // (the probabilities of columns 0 to 63 lie over the scores of 0 to 31: those are read by now)
+            turn(x, 0);
+            tmem_load32(s_col(t) + lanes + 64, y);
+            turn(x + 32, 32);
+            tmem_loaded32(y);
+            cut(y, 64);
+            tmem_load32(s_col(t) + lanes + 96, x);
+            turn(y, 64);
+            tmem_loaded32(x);
+            cut(x, 96);
+            turn(x, 96);
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tmem_stored();
+            tcgen05_fence_before();
+            mbar_arrive(p_full(t));
+        }
+        const uint32_t token = q0 + t * kTile + row;
+        if (n && sound) sound = mbar_wait(o_full(t), 0, lost);
+        tcgen05_fence_after();
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const uint64_t at = ((uint64_t)b * p.q_heads + head) * p.seq_q + token;
+        const uint64_t rows = (uint64_t)p.batch * p.q_heads * p.seq_q;
+        if (sound && token < p.seq_q) {
+            const float l2 = l == 0.f ? -INFINITY : m - kBias<BF16> + log2f(l);
+            if (p.splits > 1)
+                p.part_lse[split * rows + at] = l2;
+            else if (p.lse)
+                p.lse[at] = l2 * kLn2;
+        }
+        if (sound) {
+            const int64_t to = (int64_t)b * p.os.batch + (int64_t)token * p.os.token + (int64_t)head * p.os.head;
+#pragma unroll
+            for (uint32_t c = 0; c < DV; c += 32) {
+                uint32_t o[32];
+                if (n) {
+                    tmem_load32(o_col(t) + lanes + c, o);
+                    tmem_loaded32(o);
+                }
+                if (token < p.seq_q && c < p.d_v) {
+                    float v[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = l == 0.f ? 0.f : __uint_as_float(o[j]) * inv;
+                    if (p.splits > 1) {
+                        if (l != 0.f) {
+                            float4* const q = reinterpret_cast<float4*>(p.part_o + (split * rows + at) * p.d_v + c);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (c + 4 * j < p.d_v) q[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                        }
+                    } else {
+                        write_row<BF16>(p.o, to, v, c, p.d_v);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    if (warp == kMma) {
+        if (gave_up) {                                 // matrix instructions in flight end before their memory is freed
+            if (elect_one()) {
+                g_gave_up = 1;
+                mma_commit(drained);
+                mbar_wait(drained, 0, nullptr);
+            }
+            __syncwarp();
+        }
+        tcgen05_fence_after();
+        tmem_free(tmem, kColumns);
+    }
+}
+
+// Joins the parts of the keys: a warp per query row.  Every row's parts are added in the same order.
+template <bool BF16>
+__global__ void __launch_bounds__(128) attention_join_kernel(const AttentionParams p) {
+    const uint64_t rows = (uint64_t)p.batch * p.q_heads * p.seq_q;
+    const uint64_t at = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const uint32_t lane = threadIdx.x & 31u;
+    if (at >= rows) return;
+    float top = -INFINITY;
+    for (uint32_t s = lane; s < p.splits; s += 32) top = fmaxf(top, p.part_lse[s * rows + at]);
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    const float from = top == -INFINITY ? 0.f : top;
+    float v[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+    for (uint32_t s = 0; s < p.splits; ++s) {
+        const float part = p.part_lse[s * rows + at];
+        if (part == -INFINITY) continue;               // no valid key: its values were not written
+        const float w = exp2f(part - from);
+        sum += w;
+        if (4 * lane < p.d_v) {
+            const float4 o = *reinterpret_cast<const float4*>(p.part_o + (s * rows + at) * p.d_v + 4 * lane);
+            v[0] += w * o.x, v[1] += w * o.y, v[2] += w * o.z, v[3] += w * o.w;
+        }
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const uint32_t token = (uint32_t)(at % p.seq_q), head = (uint32_t)(at / p.seq_q % p.q_heads);
+    const uint64_t b = at / ((uint64_t)p.seq_q * p.q_heads);
+    if (p.lse && lane == 0) p.lse[at] = sum == 0.f ? -INFINITY : (from + log2f(sum)) * kLn2;
+    if (4 * lane < p.d_v) {
+        uint16_t* const to = static_cast<uint16_t*>(p.o) + (int64_t)b * p.os.batch + (int64_t)token * p.os.token + (int64_t)head * p.os.head;
+        *reinterpret_cast<uint2*>(to + 4 * lane) = make_uint2(pack2<BF16>(v[0] * inv, v[1] * inv), pack2<BF16>(v[2] * inv, v[3] * inv));
+    }
+}
+
+// --- host -----------------------------------------------------------------------------------------------------------
+
+struct View {
+    const void* base;
+    uint32_t seq, heads, d;
+    Strides s;
+};
+
+int view_map(CUtensorMap* map, bool bf16, uint32_t batch, const View& v) {
+    const uint64_t extent[4] = {v.d, v.seq, v.heads, batch};
+    const int64_t stride[3] = {v.s.token, v.s.head, v.s.batch};
+    return tile_map(map, bf16, v.base, 4, extent, stride, kTile);
+}
+
+Strides strides(const int64_t s[3]) { return {s[0], s[1], s[2]}; }
+
+int check_view(const View& v, uint32_t batch) {
+    if (!v.base || !aligned16(v.base)) return MMEE_ERR_ARG;
+    const int64_t s[3] = {v.s.batch, v.s.token, v.s.head};
+    const uint32_t n[3] = {batch, v.seq, v.heads};
+    for (int i = 0; i < 3; ++i)
+        if (n[i] > 1 && (s[i] <= 0 || s[i] % 8 || s[i] >> 38)) return MMEE_ERR_ARG;
+    return MMEE_OK;
+}
+
+struct Problem {
+    AttentionParams p;
+    View q, k, v, o;
+    bool bf16;
+};
+
+int check(const mmee_workload_t* w, const mmee_attention_t* a, Problem* out) {
+    if (!w || !a) return MMEE_ERR_ARG;
+    if (!w->batch || !w->q_heads || !w->kv_heads || !w->seq_q || !w->seq_kv || !w->d_qk || !w->d_v) return MMEE_ERR_ARG;
+    if (w->q_heads % w->kv_heads || w->word_bytes != 2 || (w->d_qk | w->d_v) % 8) return MMEE_ERR_ARG;
+    if (w->d_qk > MMEE_ATTENTION_MAX_D || w->d_v > MMEE_ATTENTION_MAX_D) return MMEE_ERR_RANGE;
+    if (w->batch > 4095 || w->q_heads > 65535 || (w->seq_q | w->seq_kv) >> 30) return MMEE_ERR_RANGE;
+    if (a->dtype != MMEE_F16 && a->dtype != MMEE_BF16) return MMEE_ERR_ARG;
+    if (!(a->scale > 0.f) || !(a->scale < INFINITY)) return MMEE_ERR_ARG;
+    out->q = {a->q, w->seq_q, w->q_heads, w->d_qk, strides(a->q_stride)};
+    out->k = {a->k, w->seq_kv, w->kv_heads, w->d_qk, strides(a->k_stride)};
+    out->v = {a->v, w->seq_kv, w->kv_heads, w->d_v, strides(a->v_stride)};
+    out->o = {a->o, w->seq_q, w->q_heads, w->d_v, strides(a->o_stride)};
+    for (const View* v : {&out->q, &out->k, &out->v, &out->o}) {
+        const int rc = check_view(*v, w->batch);
+        if (rc) return rc;
+    }
+    AttentionParams& p = out->p;
+    p = AttentionParams{};
+    p.batch = w->batch;
+    p.q_heads = w->q_heads;
+    p.group = w->q_heads / w->kv_heads;
+    p.seq_q = w->seq_q;
+    p.seq_kv = w->seq_kv;
+    p.d_qk = w->d_qk;
+    p.d_v = w->d_v;
+    p.splits = 1;
+    p.tiles_per_split = (uint32_t)ceil_div(w->seq_kv, kTile);
+    p.scale = a->scale;
+    p.kv_len = a->kv_len;
+    p.o = a->o;
+    p.os = out->o.s;
+    p.lse = a->lse;
+    out->bf16 = a->dtype == MMEE_BF16;
+    return MMEE_OK;
+}
+
+template <int DK, int DV, int TILES, bool BF16>
+int launch_forward(const Problem& x, cudaStream_t stream) {
+    CUtensorMap mq, mk, mv;
+    int rc = view_map(&mq, BF16, x.p.batch, x.q);
+    if (!rc) rc = view_map(&mk, BF16, x.p.batch, x.k);
+    if (!rc) rc = view_map(&mv, BF16, x.p.batch, x.v);
+    constexpr uint32_t smem = ForwardShape<DK, DV>::smem(TILES);
+    if (!rc) rc = allow_smem((const void*)attention_kernel<DK, DV, TILES, BF16>, smem);
+    if (rc) return rc;
+    const dim3 grid((uint32_t)ceil_div(x.p.seq_q, TILES * kTile), x.p.q_heads, x.p.batch * x.p.splits);
+    attention_kernel<DK, DV, TILES, BF16><<<grid, TILES * 128 + 64, smem, stream>>>(mq, mk, mv, x.p);
+    return cuda_status(cudaGetLastError());
+}
+
+template <int DK, int DV>
+int forward_typed(const Problem& x, cudaStream_t stream) {
+    if (x.p.seq_q <= kTile) return x.bf16 ? launch_forward<DK, DV, 1, true>(x, stream) : launch_forward<DK, DV, 1, false>(x, stream);
+    return x.bf16 ? launch_forward<DK, DV, 2, true>(x, stream) : launch_forward<DK, DV, 2, false>(x, stream);
+}
+
+int forward(const Problem& x, cudaStream_t stream) {
+    const bool k = x.p.d_qk > 64, v = x.p.d_v > 64;
+    return k ? v ? forward_typed<128, 128>(x, stream) : forward_typed<128, 64>(x, stream)
+             : v ? forward_typed<64, 128>(x, stream) : forward_typed<64, 64>(x, stream);
+}
+
+// Parts that the keys are cut into where the query tiles alone leave most of the multiprocessors without work: as many as fill
+// them once, of at least two tiles each.
+int choose_splits(AttentionParams* p) {
+    uint32_t sms;
+    const int rc = sm_count(&sms);
+    if (rc) return rc;
+    const uint64_t ctas = ceil_div(p->seq_q, p->seq_q <= kTile ? kTile : 2 * kTile) * p->q_heads * p->batch;
+    const uint32_t tiles = (uint32_t)ceil_div(p->seq_kv, kTile);
+    uint64_t splits = 2 * ctas > sms ? 1 : sms / ctas;
+    if (splits > tiles / 2) splits = tiles / 2;
+    if (splits > 16) splits = 16;                      // (batch * splits has to stay within the grid, and parts cost memory)
+    if (splits < 1) splits = 1;
+    p->tiles_per_split = (uint32_t)ceil_div(tiles, splits);
+    p->splits = (uint32_t)ceil_div(tiles, p->tiles_per_split);
+    return MMEE_OK;
+}
+
+uint64_t parts_bytes(const AttentionParams& p) {
+    return p.splits > 1 ? round_up((uint64_t)p.splits * p.batch * p.q_heads * p.seq_q * 4, 16) * (p.d_v + 1) : 0;
+}
+
+}  // namespace
+
+int attention_gave_up(uint32_t* word) {
+    const uint32_t zero = 0;
+    int rc = cuda_status(cudaMemcpyFromSymbol(word, g_gave_up, sizeof *word));
+    if (!rc && *word) rc = cuda_status(cudaMemcpyToSymbol(g_gave_up, &zero, sizeof zero));
+    return rc;
+}
+
+}  // namespace mmee
+
+using namespace mmee;
+
+extern "C" int mmee_attention_workspace(const mmee_workload_t* w, uint64_t* bytes) {
+    if (!w || !bytes || !w->kv_heads) return MMEE_ERR_ARG;
+    AttentionParams p{};
+    p.batch = w->batch;
+    p.q_heads = w->q_heads;
+    p.seq_q = w->seq_q;
+    p.seq_kv = w->seq_kv;
+    p.d_v = w->d_v;
+    if (!p.batch || !p.q_heads || !p.seq_q || !p.seq_kv) return MMEE_ERR_ARG;
+    const int rc = choose_splits(&p);
+    if (!rc) *bytes = parts_bytes(p);
+    return rc;
+}
+
+extern "C" int mmee_attention(const mmee_workload_t* workload, const mmee_attention_t* a, void* cuda_stream) {
+    Problem x;
+    int rc = check(workload, a, &x);
+    if (!rc) rc = choose_splits(&x.p);
+    if (rc) return rc;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (x.p.splits > 1) {
+        if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < parts_bytes(x.p)) return MMEE_ERR_ARG;
+        const uint64_t rows = (uint64_t)x.p.splits * x.p.batch * x.p.q_heads * x.p.seq_q;
+        x.p.part_o = static_cast<float*>(a->workspace);
+        x.p.part_lse = x.p.part_o + rows * x.p.d_v;
+    }
+    if ((rc = forward(x, stream))) return rc;
+    if (x.p.splits > 1) {
+        const uint64_t rows = (uint64_t)x.p.batch * x.p.q_heads * x.p.seq_q;
+        const uint32_t grid = (uint32_t)ceil_div(rows, 4);
+        if (x.bf16)
+            attention_join_kernel<true><<<grid, 128, 0, stream>>>(x.p);
+        else
+            attention_join_kernel<false><<<grid, 128, 0, stream>>>(x.p);
+        rc = cuda_status(cudaGetLastError());
+    }
+    return rc;
+}

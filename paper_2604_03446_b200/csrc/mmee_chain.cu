@@ -58,7 +58,8 @@ int allow_smem(const void* kernel, uint32_t bytes) {
 }  // namespace mmee
 
 extern "C" int mmee_chain_status(void) {
-    uint32_t f = 0;
-    const int rc = mmee::ffn_gave_up(&f);
-    return rc ? rc : f ? MMEE_ERR_TIMEOUT : MMEE_OK;
+    uint32_t a = 0, f = 0;
+    int rc = mmee::attention_gave_up(&a);
+    if (!rc) rc = mmee::ffn_gave_up(&f);
+    return rc ? rc : a | f ? MMEE_ERR_TIMEOUT : MMEE_OK;
 }

@@ -122,9 +122,19 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* r) {
         : "r"(addr));
 }
 
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : MMEE_R8(r, 0), MMEE_R8(r, 8)
+                 : "r"(addr));
+}
+
 // The registers are operands, so that no use of them moves before the wait.
 __device__ __forceinline__ void tmem_loaded32(uint32_t* r) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" : MMEE_RW8(r, 0), MMEE_RW8(r, 8), MMEE_RW8(r, 16), MMEE_RW8(r, 24)::"memory");
+}
+
+__device__ __forceinline__ void tmem_loaded16(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : MMEE_RW8(r, 0), MMEE_RW8(r, 8)::"memory");
 }
 
 __device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t* r) {
