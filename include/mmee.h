@@ -460,6 +460,22 @@ int mmee_attention(const mmee_workload_t* workload, const mmee_attention_t* a, v
 int mmee_attention_workspace(const mmee_workload_t* workload, uint64_t* bytes);
 
 /*
+ * mmee_attention_backward -- the gradients of q, k and v for a gradient d_o of o, from the o and lse that the forward call
+ * wrote for the same tensors.  A key head's gradients are the sums over the query heads that share it; keys behind a
+ * sequence's end get zeros.  P and dS are rounded once to the tensors' type, each result once.
+ */
+typedef struct {
+    const void *d_o;                         /* as o                                              */
+    void    *d_q, *d_k, *d_v;                /* out: as q, k, v                                   */
+    int64_t  d_o_stride[3], d_q_stride[3], d_k_stride[3], d_v_stride[3];
+    void    *workspace;                      /* DEVICE, mmee_attention_backward_workspace bytes, for this call alone until it ends */
+    uint64_t workspace_bytes;
+} mmee_attention_grad_t;
+int mmee_attention_backward(const mmee_workload_t* workload, const mmee_attention_t* a, const mmee_attention_grad_t* g,
+                            void* cuda_stream);
+int mmee_attention_backward_workspace(const mmee_workload_t* workload, uint64_t* bytes);
+
+/*
  * mmee_gated_ffn -- hidden = act(x w_gate^T) * (x w_up^T),  y = hidden w_down^T.
  * Workload: a two-GEMM chain as one instance (batch = q_heads = kv_heads = 1): seq_q = tokens (I), d_qk = width of
  * x (K), seq_kv = width of the hidden values (L), d_v = width of y (J).  Widths are multiples of eight.

@@ -25,7 +25,8 @@ EXPORTS = ("mmee_create", "mmee_search", "mmee_search_host", "mmee_destroy", "mm
            "mmee_num_rows", "mmee_strerror", "mmee_last_cuda_error", "mmee_eval", "mmee_decode", "mmee_dump_keys", "mmee_filter_flags", "mmee_solve_host", "mmee_pareto_front", "mmee_pareto_front_bs_da", "mmee_search_shapes",
            "mmee_query_vector", "mmee_recompute_flag", "mmee_row_pruning_keep", "mmee_last_search_stats", "mmee_kernel_timing",
            "mmee_alu_peak", "mmee_gated_ffn", "mmee_gated_ffn_backward", "mmee_gated_ffn_workspace",
-           "mmee_attention", "mmee_attention_workspace", "mmee_chain_status")
+           "mmee_attention", "mmee_attention_workspace", "mmee_attention_backward", "mmee_attention_backward_workspace",
+           "mmee_chain_status")
 
 
 class Workload(C.Structure):
@@ -78,6 +79,12 @@ class Attention(C.Structure):
                 ("o", C.c_void_p), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
                 ("o_stride", C.c_int64 * 3), ("lse", C.c_void_p), ("kv_len", C.c_void_p), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_uint64)]
+
+
+class AttentionGrad(C.Structure):
+    _fields_ = [("d_o", C.c_void_p), ("d_q", C.c_void_p), ("d_k", C.c_void_p), ("d_v", C.c_void_p),
+                ("d_o_stride", C.c_int64 * 3), ("d_q_stride", C.c_int64 * 3), ("d_k_stride", C.c_int64 * 3),
+                ("d_v_stride", C.c_int64 * 3), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
 
 
 class GatedFfn(C.Structure):
@@ -159,6 +166,8 @@ def library():
     L.mmee_gated_ffn_workspace.argtypes = [C.POINTER(Workload), C.POINTER(C.c_uint64)]
     L.mmee_attention.argtypes = [C.POINTER(Workload), C.POINTER(Attention), C.c_void_p]
     L.mmee_attention_workspace.argtypes = [C.POINTER(Workload), C.POINTER(C.c_uint64)]
+    L.mmee_attention_backward.argtypes = [C.POINTER(Workload), C.POINTER(Attention), C.POINTER(AttentionGrad), C.c_void_p]
+    L.mmee_attention_backward_workspace.argtypes = [C.POINTER(Workload), C.POINTER(C.c_uint64)]
     L.mmee_chain_status.argtypes = []
     _lib = L
     return L
@@ -489,6 +498,32 @@ def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
     if code:
         _check(code, "mmee_attention")
     return o, lse
+
+
+def mmee_attention_backward(d_o, q, k, v, o, lse, kv_len=None, scale=None, stream=None):
+    """The gradients (d_q, d_k, d_v) of mmee_attention for a gradient d_o of o; o and lse are what the forward call with the same
+    tensors returned.  Keys behind a sequence's end get zeros.  Asynchronous."""
+    import torch
+    where = "mmee_attention_backward"
+    w, a, device = _attention_call(where, q, k, v, kv_len, scale)
+    _chain_tensors(where, 4, q=q, o=o, d_o=d_o)
+    shape = (w.batch, w.seq_q, w.q_heads, w.d_v)
+    if o.shape != shape or d_o.shape != shape:
+        _refuse(where, "o and d_o are (batch, tokens, q_heads, d_v)")
+    if (lse.shape != (w.batch, w.q_heads, w.seq_q) or lse.dtype != torch.float32 or lse.device != device or not lse.is_contiguous()):
+        _refuse(where, "lse is what the forward call for these tensors returned")
+    lib, need = _lib or library(), C.c_uint64()
+    _check(lib.mmee_attention_backward_workspace(w, need), where)
+    with _on(device, stream):
+        space = torch.empty(need.value, dtype=torch.uint8, device=device)
+        grads = [torch.empty(t.shape, dtype=q.dtype, device=device) for t in (q, k, v)]
+        a.o, a.lse, a.o_stride[:] = o.data_ptr(), lse.data_ptr(), o.stride()[:3]
+        g = AttentionGrad(d_o.data_ptr(), *[t.data_ptr() for t in grads], d_o.stride()[:3], *[t.stride()[:3] for t in grads],
+                          space.data_ptr(), need.value)
+        code = lib.mmee_attention_backward(w, a, g, _current_stream())
+    if code:
+        _check(code, where)
+    return tuple(grads)
 
 
 def mmee_chain_status() -> None:

@@ -5,17 +5,13 @@
 // through shared memory by TMA in tiles of 128, S = Q K^T lands in tensor memory, a warpgroup per query tile (a thread per
 // row, so that no reduction crosses threads) turns it into P in place, which the next matrix instruction takes from there.
 // While one tile's scores are turned, the tensor cores work for the other.
-#include "mmee_chain.h"
-#include "mmee_sm100.cuh"
+#include "mmee_attention.cuh"
 
 namespace mmee {
 
 namespace {
 
 __device__ uint32_t g_gave_up;
-
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr uint32_t kTile = 128;                        // query rows and keys of a tile
 
 // A row's sums refer to a maximum that is moved only when the scores pass it by more than this (in powers of two): the
 // results are the same up to rounding, and moving it means going through the row's sums in tensor memory.
@@ -24,49 +20,6 @@ constexpr float kSlack = 8.f;
 // division by their sum takes out again.
 template <bool BF16>
 __device__ constexpr float kBias = BF16 ? 0.f : 7.f;
-
-struct Strides {
-    int64_t batch, token, head;        // elements
-};
-
-struct AttentionParams {
-    uint32_t batch, q_heads, group, seq_q, seq_kv, d_qk, d_v;
-    uint32_t splits, tiles_per_split;  // parts that the keys are cut into, tiles of each
-    float scale;
-    const int32_t* kv_len;
-    void* o;
-    Strides os;
-    float* lse;                        // [batch][q_heads][seq_q]
-    float *part_o, *part_lse;          // splits > 1: [split][batch][q_heads][seq_q] rows of d_v; log2 of the sums
-};
-
-__device__ __forceinline__ uint32_t valid_keys(const int32_t* kv_len, uint32_t b, uint32_t seq_kv) {
-    if (!kv_len) return seq_kv;
-    const int32_t n = __ldg(kv_len + b);
-    return n < 0 ? 0u : min((uint32_t)n, seq_kv);
-}
-
-// Zeroes rows [from, to) of a tile of `blocks` blocks of 64 columns, by a whole warp: keys behind a sequence's end may hold
-// anything, and nothing times infinity would count.  (The swizzle moves sixteen-byte pieces within a row only.)
-__device__ __forceinline__ void zero_rows(uint32_t tile, uint32_t blocks, uint32_t from, uint32_t to) {
-    const uint32_t pieces = (to - from) * (kRowBytes / 16);
-    for (uint32_t b = 0; b < blocks; ++b)
-        for (uint32_t i = threadIdx.x & 31u; i < pieces; i += 32)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + b * kTile * kRowBytes + from * kRowBytes + i * 16), "r"(0) : "memory");
-    fence_async_shared();
-    __syncwarp();
-}
-
-// Writes 8 * n values of a row.
-template <bool BF16>
-__device__ __forceinline__ void write_row(void* to, int64_t at, const float* v, uint32_t from, uint32_t cols) {
-    uint4* const p = reinterpret_cast<uint4*>(static_cast<uint16_t*>(to) + at + from);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (from + 8 * j < cols)
-            p[j] = make_uint4(pack2<BF16>(v[8 * j], v[8 * j + 1]), pack2<BF16>(v[8 * j + 2], v[8 * j + 3]),
-                              pack2<BF16>(v[8 * j + 4], v[8 * j + 5]), pack2<BF16>(v[8 * j + 6], v[8 * j + 7]));
-}
 
 // --- forward --------------------------------------------------------------------------------------------------------
 
@@ -397,71 +350,6 @@ __global__ void __launch_bounds__(128) attention_join_kernel(const AttentionPara
 }
 
 // --- host -----------------------------------------------------------------------------------------------------------
-
-struct View {
-    const void* base;
-    uint32_t seq, heads, d;
-    Strides s;
-};
-
-int view_map(CUtensorMap* map, bool bf16, uint32_t batch, const View& v) {
-    const uint64_t extent[4] = {v.d, v.seq, v.heads, batch};
-    const int64_t stride[3] = {v.s.token, v.s.head, v.s.batch};
-    return tile_map(map, bf16, v.base, 4, extent, stride, kTile);
-}
-
-Strides strides(const int64_t s[3]) { return {s[0], s[1], s[2]}; }
-
-int check_view(const View& v, uint32_t batch) {
-    if (!v.base || !aligned16(v.base)) return MMEE_ERR_ARG;
-    const int64_t s[3] = {v.s.batch, v.s.token, v.s.head};
-    const uint32_t n[3] = {batch, v.seq, v.heads};
-    for (int i = 0; i < 3; ++i)
-        if (n[i] > 1 && (s[i] <= 0 || s[i] % 8 || s[i] >> 38)) return MMEE_ERR_ARG;
-    return MMEE_OK;
-}
-
-struct Problem {
-    AttentionParams p;
-    View q, k, v, o;
-    bool bf16;
-};
-
-int check(const mmee_workload_t* w, const mmee_attention_t* a, Problem* out) {
-    if (!w || !a) return MMEE_ERR_ARG;
-    if (!w->batch || !w->q_heads || !w->kv_heads || !w->seq_q || !w->seq_kv || !w->d_qk || !w->d_v) return MMEE_ERR_ARG;
-    if (w->q_heads % w->kv_heads || w->word_bytes != 2 || (w->d_qk | w->d_v) % 8) return MMEE_ERR_ARG;
-    if (w->d_qk > MMEE_ATTENTION_MAX_D || w->d_v > MMEE_ATTENTION_MAX_D) return MMEE_ERR_RANGE;
-    if (w->batch > 4095 || w->q_heads > 65535 || (w->seq_q | w->seq_kv) >> 30) return MMEE_ERR_RANGE;
-    if (a->dtype != MMEE_F16 && a->dtype != MMEE_BF16) return MMEE_ERR_ARG;
-    if (!(a->scale > 0.f) || !(a->scale < INFINITY)) return MMEE_ERR_ARG;
-    out->q = {a->q, w->seq_q, w->q_heads, w->d_qk, strides(a->q_stride)};
-    out->k = {a->k, w->seq_kv, w->kv_heads, w->d_qk, strides(a->k_stride)};
-    out->v = {a->v, w->seq_kv, w->kv_heads, w->d_v, strides(a->v_stride)};
-    out->o = {a->o, w->seq_q, w->q_heads, w->d_v, strides(a->o_stride)};
-    for (const View* v : {&out->q, &out->k, &out->v, &out->o}) {
-        const int rc = check_view(*v, w->batch);
-        if (rc) return rc;
-    }
-    AttentionParams& p = out->p;
-    p = AttentionParams{};
-    p.batch = w->batch;
-    p.q_heads = w->q_heads;
-    p.group = w->q_heads / w->kv_heads;
-    p.seq_q = w->seq_q;
-    p.seq_kv = w->seq_kv;
-    p.d_qk = w->d_qk;
-    p.d_v = w->d_v;
-    p.splits = 1;
-    p.tiles_per_split = (uint32_t)ceil_div(w->seq_kv, kTile);
-    p.scale = a->scale;
-    p.kv_len = a->kv_len;
-    p.o = a->o;
-    p.os = out->o.s;
-    p.lse = a->lse;
-    out->bf16 = a->dtype == MMEE_BF16;
-    return MMEE_OK;
-}
 
 template <int DK, int DV, int TILES, bool BF16>
 int launch_forward(const Problem& x, cudaStream_t stream) {

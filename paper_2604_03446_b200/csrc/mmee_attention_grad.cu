@@ -1,0 +1,643 @@
+// The gradients of attention.  With P = exp(S - lse) and delta = rowsum(dO * O):
+//   dV = P^T dO,  dS = P * (dO V^T - delta),  dK = scale dS^T Q,  dQ = scale dS K.
+//
+// Two kernels, so that every sum has one owner and one order: one holds a tile of keys and goes through the query tiles of all
+// heads that share them (dK, dV), the other holds a tile of queries and goes through the keys (dQ).  Each makes P and dS anew;
+// that is seven products instead of five, and no atomics.  P and dS go from tensor memory through registers and back, in place,
+// and are operands of the next matrix instruction there.
+//
+// In fp16 P is kept 2^12 larger, and dS by a power of two for which the largest value that these tensors allow,
+// 2 d_v max|dO| max|V|, still fits: gradients much smaller than one keep their bits.  Both leave the results exactly.
+#include "mmee_attention.cuh"
+
+namespace mmee {
+
+namespace {
+
+__device__ uint32_t g_gave_up;
+
+struct GradParams {
+    AttentionParams a;                 // (lse: in)
+    const void* d_o;
+    Strides dos;
+    const void* v;
+    Strides vs;
+    uint32_t kv_heads;
+    float* delta;                      // [batch][q_heads][seq_q]
+    uint32_t* most;                    // fp16: bits of max|dO| and of max|V|
+    void *dq, *dk, *dv;
+    Strides dqs, dks, dvs;
+};
+
+template <bool BF16>
+__device__ constexpr float kPShift = BF16 ? 0.f : 12.f;
+
+// Power of two that dS is kept larger by.
+template <bool BF16>
+__device__ __forceinline__ int ds_shift(const GradParams& p) {
+    if (BF16) return 0;
+    const float bound = 2.f * (float)p.a.d_v * __uint_as_float(p.most[0]) * __uint_as_float(p.most[1]);
+    if (!(bound > 0.f) || !(bound < INFINITY)) return 0;
+    return max(-100, min(100, 14 - ilogbf(bound)));
+}
+
+// delta of every query row, half a warp to a row; in fp16 also the largest sizes in dO and in V's valid rows (their order
+// does not matter).
+template <bool BF16>
+__global__ void __launch_bounds__(256) grad_rows_kernel(const GradParams p) {
+    const AttentionParams& a = p.a;
+    const uint64_t rows = (uint64_t)a.batch * a.q_heads * a.seq_q, keys = BF16 ? 0 : (uint64_t)a.batch * p.kv_heads * a.seq_kv;
+    const uint32_t lane = threadIdx.x & 15u;
+    float most[2] = {0.f, 0.f};
+    for (uint64_t r = ((uint64_t)blockIdx.x * 256 + threadIdx.x) >> 4; r < rows + keys; r += (uint64_t)gridDim.x * 16) {
+        if (r < rows) {
+            const uint32_t token = (uint32_t)(r % a.seq_q), head = (uint32_t)(r / a.seq_q % a.q_heads);
+            const int64_t b = (int64_t)(r / ((uint64_t)a.seq_q * a.q_heads));
+            float sum = 0.f;
+            if (8 * lane < a.d_v) {
+                const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.d_o) + b * p.dos.batch + (int64_t)token * p.dos.token + (int64_t)head * p.dos.head + 8 * lane);
+                const uint4 y = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.o) + b * a.os.batch + (int64_t)token * a.os.token + (int64_t)head * a.os.head + 8 * lane);
+                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 f = unpack2<BF16>(xs[j]), g = unpack2<BF16>(ys[j]);
+                    sum += f.x * g.x + f.y * g.y;
+                    if (!BF16) most[0] = fmaxf(most[0], fmaxf(fabsf(f.x), fabsf(f.y)));
+                }
+            }
+            for (int d = 8; d; d >>= 1) sum += __shfl_xor_sync(0xffffu << (threadIdx.x & 16u), sum, d);
+            if (lane == 0) p.delta[r] = sum;
+        } else {
+            const uint64_t k = r - rows;
+            const uint32_t token = (uint32_t)(k % a.seq_kv), head = (uint32_t)(k / a.seq_kv % p.kv_heads);
+            const uint32_t b = (uint32_t)(k / ((uint64_t)a.seq_kv * p.kv_heads));
+            if (token < valid_keys(a.kv_len, b, a.seq_kv) && 8 * lane < a.d_v) {
+                const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.v) + (int64_t)b * p.vs.batch + (int64_t)token * p.vs.token + (int64_t)head * p.vs.head + 8 * lane);
+                const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 f = unpack2<BF16>(xs[j]);
+                    most[1] = fmaxf(most[1], fmaxf(fabsf(f.x), fabsf(f.y)));
+                }
+            }
+        }
+    }
+    if (!BF16) {
+        for (int i = 0; i < 2; ++i) {
+            float m = most[i];
+            for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+            if ((threadIdx.x & 31u) == 0) atomicMax(p.most + i, __float_as_uint(m));
+        }
+    }
+}
+
+// A row's lse in powers of two, from which P follows; rows that count nothing get P = 0.
+__device__ __forceinline__ float row_log(const GradParams& p, uint64_t at, bool in) {
+    if (!in) return INFINITY;
+    const float l = p.a.lse[at];
+    return l == -INFINITY ? INFINITY : l * kLog2e;
+}
+
+template <int DK, int DV>
+struct GradShape {
+    static constexpr uint32_t kQ = (DK / 64) * kTile * kRowBytes, kV = (DV / 64) * kTile * kRowBytes, kRing = 2;
+    static constexpr uint32_t smem = (1 + kRing) * (kQ + kV) + 1024;
+};
+
+// Products of two tiles in shared memory, both with the reduction along their rows.
+__device__ __forceinline__ void tile_product(uint32_t to, uint32_t a, uint32_t b, uint32_t desc, uint32_t steps) {
+    const uint64_t da = tile_desc(a, 16), db = tile_desc(b, 16);
+    for (uint32_t k = 0; k < steps; ++k) {
+        const uint64_t at = (uint64_t)(k / 4) * (kTile * kRowBytes >> 4) + (k % 4) * kStepK;
+        mma_ss(to, da + at, db + at, desc, k);
+    }
+}
+
+// Adds the product of a 128 x 128 operand in tensor memory (two halves of 64 columns, each packed into its first 32) and a tile
+// whose rows are the reduction.
+__device__ __forceinline__ void turned_product(uint32_t to, uint32_t a, uint32_t b, uint32_t desc, uint32_t steps, bool add) {
+    const uint64_t db = tile_desc(b, kTile * kRowBytes);
+    for (uint32_t k = 0; k < steps; ++k) mma_ts(to, a + (k / 4) * 64 + (k % 4) * 8, db + k * kStepMN, desc, add || k);
+}
+
+// --- dK and dV ------------------------------------------------------------------------------------------------------
+
+template <int DK, int DV, bool BF16>
+__global__ void __launch_bounds__(320, 1)
+grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
+                 const __grid_constant__ CUtensorMap mo, const GradParams p) {
+    using Shape = GradShape<DK, DV>;
+    constexpr uint32_t kRing = Shape::kRing;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(16) float row_stats[2][2][kTile];         // [turn][lse, delta]
+    __shared__ __align__(8) uint64_t bars[2 * kRing + 7];
+    __shared__ uint32_t tmem_base, gave_up;
+
+    const AttentionParams& a = p.a;
+    const uint32_t b = blockIdx.z, head = blockIdx.y, k0 = blockIdx.x * kTile;
+    const uint32_t keys = valid_keys(a.kv_len, b, a.seq_kv);
+    const uint32_t tiles_q = (a.seq_q + kTile - 1) / kTile, n = k0 < keys ? a.group * tiles_q : 0;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+
+    const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
+    const uint32_t k_tile = base, v_tile = base + Shape::kQ;
+    auto q_tile = [&](uint32_t s) { return base + (1 + s) * (Shape::kQ + Shape::kV); };
+    auto o_tile = [&](uint32_t s) { return q_tile(s) + Shape::kQ; };
+    const uint32_t bar0 = smem_addr(bars);
+    auto full = [&](uint32_t s) { return bar0 + 8 * s; };
+    auto empty = [&](uint32_t s) { return bar0 + 8 * (kRing + s); };
+    const uint32_t kv_full = bar0 + 8 * 2 * kRing, s_full = kv_full + 8, dp_full = kv_full + 16, p_full = kv_full + 24, ds_full = kv_full + 32,
+                   sums_full = kv_full + 40, drained = kv_full + 48;
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (uint32_t s = 0; s < kRing; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        mbar_init(kv_full, 1);
+        mbar_init(s_full, 1);
+        mbar_init(dp_full, 1);
+        mbar_init(p_full, 256);
+        mbar_init(ds_full, 256);
+        mbar_init(sums_full, 1);
+        mbar_init(drained, 1);
+        mbar_init_visible();
+    }
+    if (warp == 9) tmem_alloc(&tmem_base, 512);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = tmem_base, s_col = tmem, dp_col = tmem + 128, dv_col = tmem + 256, dk_col = dv_col + DV;
+    volatile uint32_t* const lost = &gave_up;
+
+    if (warp == 8) {
+        if (elect_one() && n) {
+            const int32_t bb = (int32_t)b, hk = (int32_t)head;
+            mbar_expect(kv_full, Shape::kQ + Shape::kV);
+            for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(k_tile + j * kTile * kRowBytes, &mk, kv_full, 64 * j, (int32_t)k0, hk, bb);
+            for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(v_tile + j * kTile * kRowBytes, &mv, kv_full, 64 * j, (int32_t)k0, hk, bb);
+            uint32_t sent = 0;
+            bool sound = true;
+            for (uint32_t i = 0; i < n; ++i) {
+                const uint32_t s = i % kRing;
+                if (!(sound = mbar_wait(empty(s), ((i / kRing) & 1) ^ 1, lost))) break;
+                const int32_t h = (int32_t)(head * a.group + i / tiles_q), row = (int32_t)(i % tiles_q * kTile);
+                mbar_expect(full(s), Shape::kQ + Shape::kV);
+                for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(q_tile(s) + j * kTile * kRowBytes, &mq, full(s), 64 * j, row, h, bb);
+                for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(o_tile(s) + j * kTile * kRowBytes, &mo, full(s), 64 * j, row, h, bb);
+                ++sent;
+            }
+            if (!sound) {                              // what is in flight lands before the CTA ends
+                mbar_wait(kv_full, 0, nullptr);
+                for (uint32_t s = 0; s < kRing; ++s)
+                    if (sent > s) mbar_wait(full(s), ((sent - 1 - s) / kRing) & 1, nullptr);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 9) {
+        constexpr uint32_t desc = mma_desc(BF16, kTile, kTile, false, false);
+        const uint32_t steps_k = (a.d_qk + 15) / 16, steps_v = (a.d_v + 15) / 16;
+        const uint32_t desc_dv = mma_desc(BF16, kTile, 16 * steps_v, false, true), desc_dk = mma_desc(BF16, kTile, 16 * steps_k, false, true);
+        bool sound = n > 0 && mbar_wait(kv_full, 0, lost) && mbar_wait(full(0), 0, lost);
+        if (sound) {
+            tcgen05_fence_after();
+            if (elect_one()) {
+                tile_product(s_col, k_tile, q_tile(0), desc, steps_k);
+                mma_commit(s_full);
+                tile_product(dp_col, v_tile, o_tile(0), desc, steps_v);
+                mma_commit(dp_full);
+            }
+            __syncwarp();
+        }
+        for (uint32_t i = 0; i < n && sound; ++i) {
+            const uint32_t s = i % kRing, s1 = (i + 1) % kRing;
+            if (!(sound = mbar_wait(p_full, i & 1, lost))) break;
+            tcgen05_fence_after();
+            if (elect_one()) turned_product(dv_col, s_col, o_tile(s), desc_dv, 8, i);
+            __syncwarp();
+            if (i + 1 < n) {
+                if (!(sound = mbar_wait(full(s1), ((i + 1) / kRing) & 1, lost))) break;
+                tcgen05_fence_after();
+                if (elect_one()) {
+                    tile_product(s_col, k_tile, q_tile(s1), desc, steps_k);
+                    mma_commit(s_full);
+                }
+                __syncwarp();
+            }
+            if (!(sound = mbar_wait(ds_full, i & 1, lost))) break;
+            tcgen05_fence_after();
+            if (elect_one()) {
+                turned_product(dk_col, dp_col, q_tile(s), desc_dk, 8, i);
+                mma_commit(empty(s));
+                if (i + 1 < n) {
+                    tile_product(dp_col, v_tile, o_tile(s1), desc, steps_v);
+                    mma_commit(dp_full);
+                } else {
+                    mma_commit(sums_full);
+                }
+            }
+            __syncwarp();
+        }
+    } else {
+        const uint32_t half = warp / 4, row = (warp % 4) * 32 + lane, lanes = ((warp % 4) * 32) << 16;
+        const float sl2 = a.scale * kLog2e;
+        const int shift = n ? ds_shift<BF16>(p) : 0;
+        const float ds_scale = exp2f((float)shift - kPShift<BF16>);
+        const bool valid = k0 + row < keys;
+        auto stats_of = [&](uint32_t i, float* l, float* d) {
+            const uint32_t h = head * a.group + i / tiles_q, token = i % tiles_q * kTile + threadIdx.x;
+            const uint64_t at = ((uint64_t)b * a.q_heads + h) * a.seq_q + token;
+            const bool in = token < a.seq_q;
+            *l = row_log(p, at, in) - kPShift<BF16>;
+            *d = in ? p.delta[at] : 0.f;
+        };
+        float next_l = 0.f, next_d = 0.f;
+        if (n && threadIdx.x < kTile) {
+            stats_of(0, &next_l, &next_d);
+            row_stats[0][0][threadIdx.x] = next_l;
+            row_stats[0][1][threadIdx.x] = next_d;
+        }
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        bool sound = true;
+        for (uint32_t i = 0; i < n; ++i) {
+            if (i + 1 < n && threadIdx.x < kTile) stats_of(i + 1, &next_l, &next_d);
+            const float* const logs = &row_stats[i & 1][0][64 * half];
+            const float* const deltas = &row_stats[i & 1][1][64 * half];
+            float pr[64];
+            if (!(sound = mbar_wait(s_full, i & 1, lost))) break;
+            tcgen05_fence_after();
+#pragma unroll
+            for (int c = 0; c < 64; c += 32) {
+                uint32_t x[32], pk[16];
+                tmem_load32(s_col + lanes + 64 * half + c, x);
+                tmem_loaded32(x);
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                    const float4 l = *reinterpret_cast<const float4*>(logs + c + j);
+                    const float ls[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float v = exp2_fast(fmaf(__uint_as_float(x[j + e]), sl2, -ls[e]));
+                        pr[c + j + e] = valid && ls[e] != INFINITY ? v : 0.f;
+                    }
+                    pk[j / 2] = pack2<BF16>(pr[c + j], pr[c + j + 1]);
+                    pk[j / 2 + 1] = pack2<BF16>(pr[c + j + 2], pr[c + j + 3]);
+                }
+                // (32 columns of P over the first 32 of this half's 64 of S: what each store covers has been read)
+                tmem_store16(s_col + lanes + 64 * half + c / 2, pk);
+            }
+            tmem_stored();
+            tcgen05_fence_before();
+            mbar_arrive(p_full);
+            if (!(sound = mbar_wait(dp_full, i & 1, lost))) break;
+            tcgen05_fence_after();
+#pragma unroll
+            for (int c = 0; c < 64; c += 32) {
+                uint32_t x[32], pk[16];
+                tmem_load32(dp_col + lanes + 64 * half + c, x);
+                tmem_loaded32(x);
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                    const float4 d = *reinterpret_cast<const float4*>(deltas + c + j);
+                    const float ds[4] = {d.x, d.y, d.z, d.w};
+                    float v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[e] = pr[c + j + e] * (__uint_as_float(x[j + e]) - ds[e]) * ds_scale;
+                        if (!valid) v[e] = 0.f;
+                    }
+                    pk[j / 2] = pack2<BF16>(v[0], v[1]);
+                    pk[j / 2 + 1] = pack2<BF16>(v[2], v[3]);
+                }
+                tmem_store16(dp_col + lanes + 64 * half + c / 2, pk);
+            }
+            tmem_stored();
+            tcgen05_fence_before();
+            mbar_arrive(ds_full);
+            if (i + 1 < n && threadIdx.x < kTile) {
+                row_stats[(i + 1) & 1][0][threadIdx.x] = next_l;
+                row_stats[(i + 1) & 1][1][threadIdx.x] = next_d;
+            }
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+        }
+        if (n && sound) sound = mbar_wait(sums_full, 0, lost);
+        tcgen05_fence_after();
+        if (sound) {
+            const uint32_t token = k0 + row;
+            const float by_v = exp2f(-kPShift<BF16>), by_k = a.scale * exp2f((float)-shift);
+            auto write = [&](uint32_t col, uint32_t d, uint32_t width, void* to, const Strides& st, float by) {
+                for (uint32_t c = half * d / 2; c < (half + 1) * d / 2; c += 32) {
+                    uint32_t x[32];
+                    if (n) {
+                        tmem_load32(col + lanes + c, x);
+                        tmem_loaded32(x);
+                    }
+                    if (token < a.seq_kv && c < width) {
+                        float v[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = valid ? __uint_as_float(x[j]) * by : 0.f;
+                        write_row<BF16>(to, (int64_t)b * st.batch + (int64_t)token * st.token + (int64_t)head * st.head, v, c, width);
+                    }
+                    __syncwarp();
+                }
+            };
+            write(dv_col, DV, a.d_v, p.dv, p.dvs, by_v);
+            write(dk_col, DK, a.d_qk, p.dk, p.dks, by_k);
+        }
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        if (gave_up) {                                 // matrix instructions in flight end before their memory is freed
+            if (elect_one()) {
+                g_gave_up = 1;
+                mma_commit(drained);
+                mbar_wait(drained, 0, nullptr);
+            }
+            __syncwarp();
+        }
+        tcgen05_fence_after();
+        tmem_free(tmem, 512);
+    }
+}
+
+// --- dQ -------------------------------------------------------------------------------------------------------------
+
+template <int DK, int DV, bool BF16>
+__global__ void __launch_bounds__(320, 1)
+grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
+                    const __grid_constant__ CUtensorMap mo, const GradParams p) {
+    using Shape = GradShape<DK, DV>;
+    constexpr uint32_t kRing = Shape::kRing;
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t bars[2 * kRing + 7];
+    __shared__ uint32_t tmem_base, gave_up;
+
+    const AttentionParams& a = p.a;
+    const uint32_t b = blockIdx.z, head = blockIdx.y, q0 = blockIdx.x * kTile;
+    const uint32_t keys = valid_keys(a.kv_len, b, a.seq_kv), n = (keys + kTile - 1) / kTile;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+
+    const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
+    const uint32_t q_tile = base, o_tile = base + Shape::kQ;
+    auto k_tile = [&](uint32_t s) { return base + (1 + s) * (Shape::kQ + Shape::kV); };
+    auto v_tile = [&](uint32_t s) { return k_tile(s) + Shape::kQ; };
+    const uint32_t bar0 = smem_addr(bars);
+    auto full = [&](uint32_t s) { return bar0 + 8 * s; };
+    auto empty = [&](uint32_t s) { return bar0 + 8 * (kRing + s); };
+    const uint32_t q_full = bar0 + 8 * 2 * kRing, dp_full = q_full + 24, ds_full = q_full + 32, sums_full = q_full + 40, drained = q_full + 48;
+    auto s_full = [&](uint32_t t) { return q_full + 8 + 8 * t; };
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (uint32_t s = 0; s < kRing; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        mbar_init(q_full, 1);
+        mbar_init(s_full(0), 1);
+        mbar_init(s_full(1), 1);
+        mbar_init(dp_full, 1);
+        mbar_init(ds_full, 256);
+        mbar_init(sums_full, 1);
+        mbar_init(drained, 1);
+        mbar_init_visible();
+    }
+    if (warp == 9) tmem_alloc(&tmem_base, 512);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = tmem_base, dp_col = tmem + 256, dq_col = tmem + 384;
+    auto s_col = [&](uint32_t t) { return tmem + 128 * t; };
+    volatile uint32_t* const lost = &gave_up;
+
+    if (warp == 8) {
+        if (elect_one() && n) {
+            const int32_t bb = (int32_t)b, h = (int32_t)head, hk = (int32_t)(head / a.group);
+            mbar_expect(q_full, Shape::kQ + Shape::kV);
+            for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(q_tile + j * kTile * kRowBytes, &mq, q_full, 64 * j, (int32_t)q0, h, bb);
+            for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(o_tile + j * kTile * kRowBytes, &mo, q_full, 64 * j, (int32_t)q0, h, bb);
+            uint32_t sent = 0;
+            bool sound = true;
+            for (uint32_t i = 0; i < n; ++i) {
+                const uint32_t s = i % kRing;
+                if (!(sound = mbar_wait(empty(s), ((i / kRing) & 1) ^ 1, lost))) break;
+                mbar_expect(full(s), Shape::kQ + Shape::kV);
+                for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(k_tile(s) + j * kTile * kRowBytes, &mk, full(s), 64 * j, (int32_t)(i * kTile), hk, bb);
+                for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(v_tile(s) + j * kTile * kRowBytes, &mv, full(s), 64 * j, (int32_t)(i * kTile), hk, bb);
+                ++sent;
+            }
+            if (!sound) {                              // what is in flight lands before the CTA ends
+                mbar_wait(q_full, 0, nullptr);
+                for (uint32_t s = 0; s < kRing; ++s)
+                    if (sent > s) mbar_wait(full(s), ((sent - 1 - s) / kRing) & 1, nullptr);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 9) {
+        constexpr uint32_t desc = mma_desc(BF16, kTile, kTile, false, false);
+        const uint32_t steps_k = (a.d_qk + 15) / 16, steps_v = (a.d_v + 15) / 16;
+        const uint32_t desc_dq = mma_desc(BF16, kTile, 16 * steps_k, false, true);
+        // Tile i has landed; keys behind the end become zeros (in dS K they meet zeros).
+        auto landed = [&](uint32_t i) {
+            if (!mbar_wait(full(i % kRing), (i / kRing) & 1, lost)) return false;
+            const uint32_t left = keys - i * kTile;
+            if (left < kTile && left % 16) zero_rows(k_tile(i % kRing), DK / 64, left, (left + 15) / 16 * 16);
+            tcgen05_fence_after();
+            return true;
+        };
+        bool sound = n > 0 && mbar_wait(q_full, 0, lost) && landed(0);
+        if (sound) {
+            if (elect_one()) {
+                tile_product(s_col(0), q_tile, k_tile(0), desc, steps_k);
+                mma_commit(s_full(0));
+                tile_product(dp_col, o_tile, v_tile(0), desc, steps_v);
+                mma_commit(dp_full);
+            }
+            __syncwarp();
+        }
+        for (uint32_t i = 0; i < n && sound; ++i) {
+            const uint32_t s = i % kRing, s1 = (i + 1) % kRing;
+            if (i + 1 < n) {
+                if (!(sound = landed(i + 1))) break;
+                if (elect_one()) {
+                    tile_product(s_col((i + 1) & 1), q_tile, k_tile(s1), desc, steps_k);
+                    mma_commit(s_full((i + 1) & 1));
+                }
+                __syncwarp();
+            }
+            if (!(sound = mbar_wait(ds_full, i & 1, lost))) break;
+            tcgen05_fence_after();
+            if (elect_one()) {
+                if (i + 1 < n) {
+                    tile_product(dp_col, o_tile, v_tile(s1), desc, steps_v);
+                    mma_commit(dp_full);
+                }
+                turned_product(dq_col, s_col(i & 1), k_tile(s), desc_dq, (min(kTile, keys - i * kTile) + 15) / 16, i);
+                mma_commit(empty(s));
+                if (i + 1 == n) mma_commit(sums_full);
+            }
+            __syncwarp();
+        }
+    } else {
+        const uint32_t half = warp / 4, row = (warp % 4) * 32 + lane, lanes = ((warp % 4) * 32) << 16, token = q0 + row;
+        const float sl2 = a.scale * kLog2e;
+        const int shift = n ? ds_shift<BF16>(p) : 0;
+        const uint64_t at = ((uint64_t)b * a.q_heads + head) * a.seq_q + token;
+        const bool in = token < a.seq_q;
+        // dS = 2^shift exp2(S sl2 - log) (dP - delta): the power goes into the exponent.
+        const float log = row_log(p, at, in), from = log - (float)shift, delta = in ? p.delta[at] : 0.f;
+        const bool counts = log != INFINITY;
+        bool sound = true;
+        for (uint32_t i = 0; i < n; ++i) {
+            const int valid = counts ? (int)min(kTile, keys - i * kTile) - 64 * (int)half : 0;      // columns of this half that count
+            float pr[64];
+            if (!(sound = mbar_wait(s_full(i & 1), (i >> 1) & 1, lost))) break;
+            tcgen05_fence_after();
+            const uint32_t s = s_col(i & 1) + lanes + 64 * half;
+            uint32_t x[32];
+#pragma unroll
+            for (int c = 0; c < 64; c += 32) {
+                tmem_load32(s + c, x);
+                tmem_loaded32(x);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) pr[c + j] = exp2_fast(fmaf(__uint_as_float(x[j]), sl2, -from));
+            }
+            if (!(sound = mbar_wait(dp_full, i & 1, lost))) break;
+            tcgen05_fence_after();
+#pragma unroll
+            for (int c = 0; c < 64; c += 32) {
+                uint32_t pk[16];
+                tmem_load32(dp_col + lanes + 64 * half + c, x);
+                tmem_loaded32(x);
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) {
+                    float v0 = pr[c + j] * (__uint_as_float(x[j]) - delta), v1 = pr[c + j + 1] * (__uint_as_float(x[j + 1]) - delta);
+                    if (c + j >= valid) v0 = 0.f;
+                    if (c + j + 1 >= valid) v1 = 0.f;
+                    pk[j / 2] = pack2<BF16>(v0, v1);
+                }
+                tmem_store16(s + c / 2, pk);
+            }
+            tmem_stored();
+            tcgen05_fence_before();
+            mbar_arrive(ds_full);
+        }
+        if (n && sound) sound = mbar_wait(sums_full, 0, lost);
+        tcgen05_fence_after();
+        if (sound) {
+            const float by = a.scale * exp2f((float)-shift);
+            for (uint32_t c = half * DK / 2; c < (half + 1) * DK / 2; c += 32) {
+                uint32_t x[32];
+                if (n) {
+                    tmem_load32(dq_col + lanes + c, x);
+                    tmem_loaded32(x);
+                }
+                if (in && c < a.d_qk) {
+                    float v[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = n ? __uint_as_float(x[j]) * by : 0.f;
+                    write_row<BF16>(p.dq, (int64_t)b * p.dqs.batch + (int64_t)token * p.dqs.token + (int64_t)head * p.dqs.head, v, c, a.d_qk);
+                }
+                __syncwarp();
+            }
+        }
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        if (gave_up) {                                 // matrix instructions in flight end before their memory is freed
+            if (elect_one()) {
+                g_gave_up = 1;
+                mma_commit(drained);
+                mbar_wait(drained, 0, nullptr);
+            }
+            __syncwarp();
+        }
+        tcgen05_fence_after();
+        tmem_free(tmem, 512);
+    }
+}
+
+// --- host -----------------------------------------------------------------------------------------------------------
+
+template <int DK, int DV, bool BF16>
+int launch_grads(const Problem& x, const View& d_o, const GradParams& p, cudaStream_t stream) {
+    const AttentionParams& a = p.a;
+    CUtensorMap mq, mk, mv, mo;
+    int rc = view_map(&mq, BF16, a.batch, x.q);
+    if (!rc) rc = view_map(&mk, BF16, a.batch, x.k);
+    if (!rc) rc = view_map(&mv, BF16, a.batch, x.v);
+    if (!rc) rc = view_map(&mo, BF16, a.batch, d_o);
+    constexpr uint32_t smem = GradShape<DK, DV>::smem;
+    if (!rc) rc = allow_smem((const void*)grad_keys_kernel<DK, DV, BF16>, smem);
+    if (!rc) rc = allow_smem((const void*)grad_queries_kernel<DK, DV, BF16>, smem);
+    if (rc) return rc;
+    if (!BF16 && (rc = cuda_status(cudaMemsetAsync(p.most, 0, 8, stream)))) return rc;
+    const uint64_t rows = (uint64_t)a.batch * a.q_heads * a.seq_q + (BF16 ? 0 : (uint64_t)a.batch * p.kv_heads * a.seq_kv);
+    uint32_t sms;
+    if ((rc = sm_count(&sms))) return rc;
+    grad_rows_kernel<BF16><<<(uint32_t)min(ceil_div(rows, 16), (uint64_t)sms * 8), 256, 0, stream>>>(p);
+    grad_keys_kernel<DK, DV, BF16><<<dim3((uint32_t)ceil_div(a.seq_kv, kTile), p.kv_heads, a.batch), 320, smem, stream>>>(mq, mk, mv, mo, p);
+    grad_queries_kernel<DK, DV, BF16><<<dim3((uint32_t)ceil_div(a.seq_q, kTile), a.q_heads, a.batch), 320, smem, stream>>>(mq, mk, mv, mo, p);
+    return cuda_status(cudaGetLastError());
+}
+
+template <int DK, int DV>
+int grads_typed(const Problem& x, const View& d_o, const GradParams& p, cudaStream_t stream) {
+    return x.bf16 ? launch_grads<DK, DV, true>(x, d_o, p, stream) : launch_grads<DK, DV, false>(x, d_o, p, stream);
+}
+
+uint64_t rows_bytes(const mmee_workload_t& w) { return round_up((uint64_t)w.batch * w.q_heads * w.seq_q * 4, 16); }
+
+}  // namespace
+
+int attention_grad_gave_up(uint32_t* word) {
+    const uint32_t zero = 0;
+    int rc = cuda_status(cudaMemcpyFromSymbol(word, g_gave_up, sizeof *word));
+    if (!rc && *word) rc = cuda_status(cudaMemcpyToSymbol(g_gave_up, &zero, sizeof zero));
+    return rc;
+}
+
+}  // namespace mmee
+
+using namespace mmee;
+
+extern "C" int mmee_attention_backward_workspace(const mmee_workload_t* w, uint64_t* bytes) {
+    if (!w || !bytes) return MMEE_ERR_ARG;
+    *bytes = rows_bytes(*w) + 16;
+    return MMEE_OK;
+}
+
+extern "C" int mmee_attention_backward(const mmee_workload_t* workload, const mmee_attention_t* attention, const mmee_attention_grad_t* g,
+                                       void* cuda_stream) {
+    Problem x;
+    const int rc = check(workload, attention, &x);
+    if (rc) return rc;
+    if (!g || !attention->lse) return MMEE_ERR_ARG;
+    const mmee_workload_t& w = *workload;
+    const View d_o{g->d_o, w.seq_q, w.q_heads, w.d_v, strides(g->d_o_stride)};
+    const View dq{g->d_q, w.seq_q, w.q_heads, w.d_qk, strides(g->d_q_stride)}, dk{g->d_k, w.seq_kv, w.kv_heads, w.d_qk, strides(g->d_k_stride)};
+    const View dv{g->d_v, w.seq_kv, w.kv_heads, w.d_v, strides(g->d_v_stride)};
+    for (const View* v : {&d_o, &dq, &dk, &dv})
+        if (check_view(*v, w.batch)) return MMEE_ERR_ARG;
+    if (!g->workspace || !aligned16(g->workspace) || g->workspace_bytes < rows_bytes(w) + 16) return MMEE_ERR_ARG;
+    GradParams p{};
+    p.a = x.p;
+    p.d_o = g->d_o;
+    p.dos = d_o.s;
+    p.v = attention->v;
+    p.vs = x.v.s;
+    p.kv_heads = w.kv_heads;
+    p.delta = static_cast<float*>(g->workspace);
+    p.most = reinterpret_cast<uint32_t*>(static_cast<char*>(g->workspace) + rows_bytes(w));
+    p.dq = g->d_q;
+    p.dk = g->d_k;
+    p.dv = g->d_v;
+    p.dqs = dq.s;
+    p.dks = dk.s;
+    p.dvs = dv.s;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const bool bk = w.d_qk > 64, bv = w.d_v > 64;
+    return bk ? bv ? grads_typed<128, 128>(x, d_o, p, stream) : grads_typed<128, 64>(x, d_o, p, stream)
+              : bv ? grads_typed<64, 128>(x, d_o, p, stream) : grads_typed<64, 64>(x, d_o, p, stream);
+}

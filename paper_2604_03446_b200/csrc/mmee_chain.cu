@@ -58,8 +58,9 @@ int allow_smem(const void* kernel, uint32_t bytes) {
 }  // namespace mmee
 
 extern "C" int mmee_chain_status(void) {
-    uint32_t a = 0, f = 0;
+    uint32_t a = 0, g = 0, f = 0;
     int rc = mmee::attention_gave_up(&a);
+    if (!rc) rc = mmee::attention_grad_gave_up(&g);
     if (!rc) rc = mmee::ffn_gave_up(&f);
-    return rc ? rc : a | f ? MMEE_ERR_TIMEOUT : MMEE_OK;
+    return rc ? rc : a | g | f ? MMEE_ERR_TIMEOUT : MMEE_OK;
 }

@@ -27,6 +27,7 @@ inline uint64_t round_up(uint64_t a, uint64_t b) { return ceil_div(a, b) * b; }
 
 // The words that kernels set when a wait ran out, read and cleared (one for each file with such kernels).
 int attention_gave_up(uint32_t* word);
+int attention_grad_gave_up(uint32_t* word);
 int ffn_gave_up(uint32_t* word);
 
 }  // namespace mmee

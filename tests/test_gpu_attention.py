@@ -228,6 +228,109 @@ def test_same_bits_every_time_on_any_stream_and_replayed(size):
         assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
 
 
+# --- gradients ------------------------------------------------------------------------------------------------------
+
+def check_backward(q, k, v, do, kv_len=None, scale=None):
+    o, lse = mm.mmee_attention(q, k, v, kv_len=kv_len, scale=scale)
+    grads = mm.mmee_attention_backward(do, q, k, v, o, lse, kv_len=kv_len, scale=scale)
+    want = formulas(q, k, v, kv_len, torch.finfo(q.dtype).eps / 2, scale, do)
+    for name, got in zip(("dq", "dk", "dv"), grads):
+        inside(name, got, want[name])
+    return o, lse, grads
+
+
+@gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("size", [s for s in SIZES if s[4] <= 5000], ids=lambda s: "x".join(map(str, s)))
+def test_gradients_against_64_bits(size, dtype):
+    q, k, v, do = make(size, TYPES[dtype], seed=11)
+    check_backward(q, k, v, do)
+    mm.mmee_chain_status()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("size", [(13, 4, 2, 1, 300, 64, 64), (13, 2, 2, 40, 260, 72, 128), (13, 4, 2, 140, 300, 128, 40)])
+def test_gradients_with_lengths_and_what_lies_behind_them(size, dtype):
+    q, k, v, do = make(size, TYPES[dtype], seed=12)
+    n = lengths(size[0], size[4], 0)
+    o, lse, grads = check_backward(q, k, v, do, n)
+    behind = torch.arange(size[4], device="cuda") >= n[:, None]
+    assert (grads[1][behind] == 0).all() and (grads[2][behind] == 0).all() and (grads[0][n <= 0] == 0).all()
+    for junk in (float("nan"), float("inf"), 6e4):
+        k2, v2 = k.clone(), v.clone()
+        k2[behind], v2[behind] = junk, junk
+        for a, b in zip(grads, mm.mmee_attention_backward(do, q, k2, v2, o, lse, kv_len=n)):
+            assert torch.equal(a, b)
+
+
+@gpu
+@pytest.mark.parametrize("size_of_do", [2.0 ** -20, 2.0 ** -8, 1.0, 2.0 ** 9])
+@pytest.mark.parametrize("size_of_v", [2.0 ** -6, 1.0, 2.0 ** 5])
+def test_small_and_large_gradients_in_fp16(size_of_do, size_of_v):
+    """Gradients far from one: what fits the type does not overflow on the way, and small ones keep their bits."""
+    q, k, v, do = make((1, 2, 1, 150, 400, 64, 64), torch.float16, seed=13)
+    o, lse = mm.mmee_attention(q, k, (v * size_of_v).half())
+    check_backward(q, k, (v * size_of_v).half(), (do * size_of_do).half())
+
+
+@gpu
+def test_gradients_of_long_flat_rows_in_fp16():
+    """16384 keys of equal score: probabilities of 2^-14, the edge of fp16's normal values."""
+    q, k, v, do = make((1, 1, 1, 130, 16384, 64, 64), torch.float16, seed=14)
+    check_backward(q * 0, k, v, do)
+    check_backward((q * 0.1).half(), k, v, do)
+
+
+@gpu
+@pytest.mark.parametrize("group", [1, 4])
+def test_gradients_against_differences(group):
+    """Against central differences of the formula in 64 bits along random directions: <gradient, v> is the derivative along v.
+    The bound on the gradient's entries gives sum |v_i| bound_i; what the step leaves is measured by a second, halved one."""
+    t = make((2, 2 * group, 2, 9, 33, 24, 16), torch.float16, seed=15)
+    n = torch.tensor([33, 20], dtype=torch.int32, device="cuda")
+    grads = check_backward(*t, kv_len=n)[2]
+    want = formulas(*t[:3], n, 2.0 ** -11, None, t[3])
+    base = [x.double() for x in t[:3]]
+    gen = torch.Generator(device="cuda").manual_seed(1)
+
+    def value(q, k, v):
+        return float((formulas(q, k, v, n, 0.0)["o"][0] * t[3].double()).sum())
+
+    for i, name in enumerate(("dq", "dk", "dv")):
+        d = torch.randn(base[i].shape, generator=gen, device="cuda", dtype=torch.float64)
+        at = lambda h: value(*[b + h * d if j == i else b for j, b in enumerate(base)])
+        d1, d2 = (at(1e-3) - at(-1e-3)) / 2e-3, (at(5e-4) - at(-5e-4)) / 1e-3
+        have = float((grads[i].double() * d).sum())
+        assert abs(have - (4 * d2 - d1) / 3) <= float((want[name][1] * d.abs()).sum()) + abs(d1 - d2) + 1e-9, name
+
+
+@gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_gradients_same_bits_every_time_strided_and_replayed(dtype):
+    b, hq, hkv, n, m, d = 2, 8, 2, 150, 400, 64
+    q, k, v, do = make((b, hq, hkv, n, m, d, d), TYPES[dtype], seed=16)
+    lens = torch.tensor([400, 130], dtype=torch.int32, device="cuda")
+    o, lse = mm.mmee_attention(q, k, v, kv_len=lens)
+    want = mm.mmee_attention_backward(do, q, k, v, o, lse, kv_len=lens)
+    both = torch.stack((k, v), dim=3)
+    flip = lambda x: x.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
+    torch.cuda.synchronize()
+    got = [mm.mmee_attention_backward(do, q, k, v, o, lse, kv_len=lens, stream=torch.cuda.Stream()) for _ in range(3)]
+    got.append(mm.mmee_attention_backward(flip(do), flip(q), both[:, :, :, 0], both[:, :, :, 1], flip(o), lse, kv_len=lens))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o2, lse2 = mm.mmee_attention(q, k, v, kv_len=lens)
+        got.append(mm.mmee_attention_backward(do, q, k, v, o2, lse2, kv_len=lens))
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    for g in got:
+        for x, y in zip(g, want):
+            assert torch.equal(x, y)
+
+
 # --- refusals: nothing is launched, so that they need no GPU ---------------------------------------------------------
 
 class _Case:
@@ -238,6 +341,7 @@ class _Case:
         self.w = b.Workload(batch=2, q_heads=4, kv_heads=2, seq_q=3, seq_kv=5, d_qk=64, d_v=32, word_bytes=2)
         self.a = b.Attention(dtype=b.BF16, scale=0.125, q=4096, k=4096, v=4096, o=4096, q_stride=(768, 256, 64), k_stride=(640, 128, 64),
                              v_stride=(320, 64, 32), o_stride=(384, 128, 32), lse=4096)
+        self.g = b.AttentionGrad(4096, 4096, 4096, 4096, (384, 128, 32), (768, 256, 64), (640, 128, 64), (320, 64, 32), 4096, 4096)
 
 
 BAD = [("w", "batch", 0), ("w", "q_heads", 0), ("w", "kv_heads", 0), ("w", "kv_heads", 3), ("w", "seq_q", 0), ("w", "seq_kv", 0), ("w", "d_qk", 0),
@@ -254,6 +358,27 @@ def test_bad_arguments_are_refused(where, field, value):
     else:
         setattr(getattr(c, where), field, value)
     assert mm.library().mmee_attention(c.w, c.a, None) == mm.ERR_ARG
+    assert mm.library().mmee_attention_backward(c.w, c.a, c.g, None) == mm.ERR_ARG
+
+
+@pytest.mark.parametrize("field,value", [("d_o", 0), ("d_o", 4100), ("d_q", 0), ("d_k", 4104), ("d_v", 0), ("d_o_stride", (384, 0, 32)),
+                                         ("d_q_stride", (768, 256, 60)), ("d_k_stride", (0, 128, 64)), ("d_v_stride", (320, -64, 32)),
+                                         ("workspace", 0), ("workspace", 4104), ("workspace_bytes", 2 * 4 * 3 * 4 + 15)])
+def test_bad_gradient_arguments_are_refused(field, value):
+    c = _Case()
+    if isinstance(value, tuple):
+        getattr(c.g, field)[:] = value
+    else:
+        setattr(c.g, field, value)
+    assert mm.library().mmee_attention_backward(c.w, c.a, c.g, None) == mm.ERR_ARG
+
+
+def test_a_backward_call_without_its_forward_results_is_refused():
+    c, lib = _Case(), mm.library()
+    assert lib.mmee_attention_backward(c.w, c.a, None, None) == mm.ERR_ARG
+    assert lib.mmee_attention_backward_workspace(None, None) == mm.ERR_ARG
+    c.a.lse = None
+    assert lib.mmee_attention_backward(c.w, c.a, c.g, None) == mm.ERR_ARG
 
 
 @pytest.mark.parametrize("field,value", [("d_qk", 136), ("d_v", 256), ("batch", 4096), ("q_heads", 65536 * 2), ("seq_kv", 1 << 30)])
@@ -290,3 +415,7 @@ def test_shapes_that_do_not_fit_are_refused():
             mm.mmee_attention(q, k, v, kv_len=bad)
     with pytest.raises(mm.MmeeError):
         mm.mmee_attention(q, k, v, scale=-1.0)
+    o, lse = mm.mmee_attention(q, k, v)
+    for bad in [(o[:, :2], o, lse), (o, o[..., :24], lse), (o, o, lse.half()), (o, o, lse[:1]), (o.bfloat16(), o, lse)]:
+        with pytest.raises(mm.MmeeError):
+            mm.mmee_attention_backward(bad[0], q, k, v, bad[1], bad[2])
