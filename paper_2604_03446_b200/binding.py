@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 from . import build as _build
 
@@ -378,103 +379,89 @@ def _refuse(where: str, why: str):
     raise MmeeError(ERR_ARG, "%s: %s" % (where, why))
 
 
-def _chain_tensors(where: str, rank: int, **tensors):
-    """(type code, device) that the tensors of one call share: CUDA tensors of one 16-bit type on one device."""
+def _chain_code(where: str, rank: int, first, *others):
+    """The type code that the tensors of one call share: CUDA tensors of one 16-bit type on one device, of `rank` dimensions with
+    the last one contiguous."""
     import torch
-    first = next(iter(tensors.values()))
-    for name, t in tensors.items():
-        if not isinstance(t, torch.Tensor) or t.dim() != rank:
-            _refuse(where, "%s is not a tensor of %d dimensions" % (name, rank))
-        if t.dtype != first.dtype or t.device != first.device:
-            _refuse(where, "%s is of another type or on another device" % name)
-        if t.stride(-1) != 1 and t.shape[-1] > 1:
-            _refuse(where, "the last dimension of %s is not contiguous" % name)
-    if first.dtype not in (torch.bfloat16, torch.float16) or first.device.type != "cuda":
+    if not isinstance(first, torch.Tensor):
+        _refuse(where, "tensors are wanted")
+    dtype, at = first.dtype, first.get_device()
+    code = BF16 if dtype is torch.bfloat16 else F16 if dtype is torch.float16 else None
+    if code is None or at < 0:
         _refuse(where, "bfloat16 or float16 tensors on a CUDA device are wanted")
-    return (BF16 if first.dtype == torch.bfloat16 else F16), first.device
+    for t in (first,) + others:
+        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != at:
+            _refuse(where, "the tensors are not of one type on one device")
+        if t.dim() != rank or (t.stride(-1) != 1 and t.shape[-1] > 1):
+            _refuse(where, "tensors of %d dimensions are wanted, the last one contiguous" % rank)
+    return code
 
 
-def _on(device, stream):
-    """What a call on tensors of `device` runs under, so that its launches and the memory it takes are the device's and the
-    stream's; nothing where both are current already."""
-    import contextlib
+def _elsewhere(t, stream) -> bool:
+    """Whether a call on the tensor's device and the stream has to change what is current."""
     import torch
-    if stream is not None:
-        return torch.cuda.stream(stream)
-    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    return stream is not None or torch.cuda.current_device() != t.get_device()
 
 
-def _ffn_call(where, x, w_gate, w_up, w_down, activation):
-    code, device = _chain_tensors(where, 2, x=x, w_gate=w_gate, w_up=w_up, w_down=w_down)
-    tokens, d_in = x.shape
-    d_ff, d_out = w_gate.shape[0], w_down.shape[0]
-    if w_gate.shape != (d_ff, d_in) or w_up.shape != (d_ff, d_in) or w_down.shape != (d_out, d_ff):
-        _refuse(where, "w_gate and w_up are (inner, in), w_down is (out, inner), x is (tokens, in)")
-    w = Workload(batch=1, q_heads=1, kv_heads=1, seq_q=tokens, seq_kv=d_ff, d_qk=d_in, d_v=d_out, word_bytes=2)
-    f = GatedFfn(dtype=code, activation=activation, x=x.data_ptr(), w_gate=w_gate.data_ptr(), w_up=w_up.data_ptr(),
-                 w_down=w_down.data_ptr(), x_stride=x.stride(0), w_gate_stride=w_gate.stride(0), w_up_stride=w_up.stride(0),
-                 w_down_stride=w_down.stride(0))
-    return w, f, device
-
-
-def mmee_gated_ffn(x, w_gate, w_up, w_down, activation: int = ACT_SILU, save: bool = False, stream=None):
-    """y = (act(x w_gate^T) * (x w_up^T)) w_down^T: (y, saved).  x: (tokens, in), w_gate and w_up: (inner, in), w_down: (out, inner),
-    bfloat16 or float16.  saved: what mmee_gated_ffn_backward needs where `save`, otherwise None.  Asynchronous."""
+def _there(t, stream):
+    """Makes the tensor's device and the stream current: launches and the memory that a call takes are theirs."""
     import torch
-    w, f, device = _ffn_call("mmee_gated_ffn", x, w_gate, w_up, w_down, activation)
-    with _on(device, stream):
-        hidden = torch.empty((w.seq_q, w.seq_kv), dtype=x.dtype, device=device)
-        kept = torch.empty((2, w.seq_q, w.seq_kv), dtype=torch.float32, device=device) if save else None
-        y = torch.empty((w.seq_q, w.d_v), dtype=x.dtype, device=device)
-        f.hidden, f.y, f.kept = hidden.data_ptr(), y.data_ptr(), kept.data_ptr() if save else None
-        code = (_lib or library()).mmee_gated_ffn(w, f, _current_stream())
-    if code:
-        _check(code, "mmee_gated_ffn")
-    return y, ((hidden, kept) if save else None)
+    return torch.cuda.stream(stream) if stream is not None else torch.cuda.device(t.device)
 
 
-def mmee_gated_ffn_backward(d_y, x, w_gate, w_up, w_down, saved, activation: int = ACT_SILU, stream=None):
-    """The gradients (d_x, d_w_gate, d_w_up, d_w_down) of mmee_gated_ffn for a gradient d_y of y; `saved` is what the forward call
-    with the same x, weights and activation returned.  Asynchronous."""
+# The call structs as bytes, in the layouts of Workload, Attention, AttentionGrad, GatedFfn and GatedFfnGrad: filling a
+# ctypes struct field by field takes several times as long (the calls below are made once per layer and token).
+_WORKLOAD, _ATTENTION, _ATTENTION_GRAD = struct.Struct("=8I").pack, struct.Struct("=If4Q12q4Q").pack, struct.Struct("=4Q12q2Q").pack
+_FFN, _FFN_GRAD = struct.Struct("=2I4Q4q3Q").pack, struct.Struct("=Qq6Q").pack
+
+
+class _ChainCalls:
+    """The library's chain calls with structs given as bytes."""
+
+    def __init__(self):
+        L = library()
+        for name, n in (("attention", 2), ("attention_backward", 3), ("gated_ffn", 2), ("gated_ffn_backward", 3)):
+            f = L["mmee_" + name]
+            f.argtypes = [C.c_char_p] * n + [C.c_void_p]
+            setattr(self, name, f)
+        for name in ("attention_workspace", "attention_backward_workspace", "gated_ffn_workspace"):
+            f = L["mmee_" + name]
+            f.argtypes = [C.c_char_p, C.c_void_p]
+            setattr(self, name, f)
+
+
+_chain_calls = None
+
+
+def _chain():
+    global _chain_calls
+    if _chain_calls is None:
+        _chain_calls = _ChainCalls()
+    return _chain_calls
+
+
+def _space(ask, workload, like, where):
+    """Workspace for one call (None: it needs none) and its size."""
     import torch
-    where = "mmee_gated_ffn_backward"
-    w, f, device = _ffn_call(where, x, w_gate, w_up, w_down, activation)
-    _chain_tensors(where, 2, x=x, d_y=d_y)
-    hidden, kept = saved
-    if d_y.shape != (w.seq_q, w.d_v):
-        _refuse(where, "d_y is (tokens, out)")
-    if (hidden.shape != (w.seq_q, w.seq_kv) or hidden.dtype != x.dtype or kept.shape != (2, w.seq_q, w.seq_kv) or
-            kept.dtype != torch.float32 or not hidden.is_contiguous() or not kept.is_contiguous() or
-            hidden.device != device or kept.device != device):
-        _refuse(where, "saved is not what the forward call for these tensors returned")
     need = C.c_uint64()
-    _check(library().mmee_gated_ffn_workspace(w, need), where)
-    with _on(device, stream):
-        space = torch.empty(need.value, dtype=torch.uint8, device=device)
-        grads = [torch.empty(t.shape, dtype=x.dtype, device=device) for t in (x, w_gate, w_up, w_down)]
-        f.hidden, f.kept = hidden.data_ptr(), kept.data_ptr()
-        g = GatedFfnGrad(d_y.data_ptr(), d_y.stride(0), *[t.data_ptr() for t in grads], space.data_ptr(), need.value)
-        code = library().mmee_gated_ffn_backward(w, f, g, _current_stream())
+    code = ask(workload, C.addressof(need))
     if code:
         _check(code, where)
-    return tuple(grads)
+    return (torch.empty(need.value, dtype=torch.uint8, device=like.device) if need.value else None), need.value
 
 
-def _attention_call(where, q, k, v, kv_len, scale):
-    import torch
-    code, device = _chain_tensors(where, 4, q=q, k=k, v=v)
-    batch, seq_q, q_heads, d_qk = q.shape
-    seq_kv, kv_heads = k.shape[1], k.shape[2]
-    if k.shape != (batch, seq_kv, kv_heads, d_qk) or v.shape[:3] != k.shape[:3]:
+def _attention_sizes(where, q, k, v, kv_len):
+    """(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v) of tensors that fit each other."""
+    (batch, seq_q, q_heads, d_qk), (b, seq_kv, kv_heads, d) = q.shape, k.shape
+    bv, sv, hv, d_v = v.shape
+    if b != batch or bv != batch or sv != seq_kv or hv != kv_heads or d != d_qk:
         _refuse(where, "q is (batch, tokens, heads, d), k and v have one batch, length and number of heads, q and k one width")
-    if kv_len is not None and (not isinstance(kv_len, torch.Tensor) or kv_len.dtype != torch.int32 or kv_len.shape != (batch,) or
-                               kv_len.device != device or not kv_len.is_contiguous()):
-        _refuse(where, "kv_len is a contiguous int32 tensor, one entry per sequence, on the tensors' device")
-    w = Workload(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, v.shape[3], 2)
-    a = Attention(dtype=code, scale=d_qk ** -0.5 if scale is None and d_qk else scale or 0.0, q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(),
-                  q_stride=q.stride()[:3], k_stride=k.stride()[:3], v_stride=v.stride()[:3],
-                  kv_len=None if kv_len is None else kv_len.data_ptr())
-    return w, a, device
+    if kv_len is not None:
+        import torch
+        if not (isinstance(kv_len, torch.Tensor) and kv_len.dtype is torch.int32 and kv_len.shape == (batch,) and
+                kv_len.get_device() == q.get_device() and kv_len.is_contiguous()):
+            _refuse(where, "kv_len is a contiguous int32 tensor, one entry per sequence, on the tensors' device")
+    return batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v
 
 
 def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
@@ -482,21 +469,23 @@ def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
     kv_heads, d_qk), v: (batch, keys, kv_heads, d_v), bfloat16 or float16; kv_len: int32 tensor with an entry per sequence, None: all keys;
     scale: d_qk ** -0.5 unless given.  lse: float32 (batch, q_heads, tokens).  Asynchronous."""
     import torch
-    w, a, device = _attention_call("mmee_attention", q, k, v, kv_len, scale)
-    lib, need = _lib or library(), C.c_uint64()
-    with _on(device, stream):
-        code = lib.mmee_attention_workspace(w, need)
-        if code:
-            _check(code, "mmee_attention")
-        o = torch.empty((w.batch, w.seq_q, w.q_heads, w.d_v), dtype=q.dtype, device=device)
-        lse = torch.empty((w.batch, w.q_heads, w.seq_q), dtype=torch.float32, device=device)
-        if need.value:
-            space = torch.empty(need.value, dtype=torch.uint8, device=device)
-            a.workspace, a.workspace_bytes = space.data_ptr(), need.value
-        a.o, a.lse, a.o_stride[:] = o.data_ptr(), lse.data_ptr(), o.stride()[:3]
-        code = lib.mmee_attention(w, a, _current_stream())
+    where = "mmee_attention"
+    code = _chain_code(where, 4, q, k, v)
+    if _elsewhere(q, stream):
+        with _there(q, stream):
+            return mmee_attention(q, k, v, kv_len, scale)
+    batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v = _attention_sizes(where, q, k, v, kv_len)
+    calls = _chain()
+    w = _WORKLOAD(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v, 2)
+    space, need = _space(calls.attention_workspace, w, q, where)
+    o = q.new_empty((batch, seq_q, q_heads, d_v))
+    lse = torch.empty((batch, q_heads, seq_q), dtype=torch.float32, device=q.device)
+    a = _ATTENTION(code, (d_qk or 1) ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+                   *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], lse.data_ptr(),
+                   0 if kv_len is None else kv_len.data_ptr(), space.data_ptr() if need else 0, need)
+    code = calls.attention(w, a, _current_stream())
     if code:
-        _check(code, "mmee_attention")
+        _check(code, where)
     return o, lse
 
 
@@ -505,25 +494,88 @@ def mmee_attention_backward(d_o, q, k, v, o, lse, kv_len=None, scale=None, strea
     tensors returned.  Keys behind a sequence's end get zeros.  Asynchronous."""
     import torch
     where = "mmee_attention_backward"
-    w, a, device = _attention_call(where, q, k, v, kv_len, scale)
-    _chain_tensors(where, 4, q=q, o=o, d_o=d_o)
-    shape = (w.batch, w.seq_q, w.q_heads, w.d_v)
-    if o.shape != shape or d_o.shape != shape:
+    code = _chain_code(where, 4, q, k, v, o, d_o)
+    if _elsewhere(q, stream):
+        with _there(q, stream):
+            return mmee_attention_backward(d_o, q, k, v, o, lse, kv_len, scale)
+    batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v = _attention_sizes(where, q, k, v, kv_len)
+    if o.shape != (batch, seq_q, q_heads, d_v) or d_o.shape != o.shape:
         _refuse(where, "o and d_o are (batch, tokens, q_heads, d_v)")
-    if (lse.shape != (w.batch, w.q_heads, w.seq_q) or lse.dtype != torch.float32 or lse.device != device or not lse.is_contiguous()):
+    if not (isinstance(lse, torch.Tensor) and lse.shape == (batch, q_heads, seq_q) and lse.dtype is torch.float32 and
+            lse.get_device() == q.get_device() and lse.is_contiguous()):
         _refuse(where, "lse is what the forward call for these tensors returned")
-    lib, need = _lib or library(), C.c_uint64()
-    _check(lib.mmee_attention_backward_workspace(w, need), where)
-    with _on(device, stream):
-        space = torch.empty(need.value, dtype=torch.uint8, device=device)
-        grads = [torch.empty(t.shape, dtype=q.dtype, device=device) for t in (q, k, v)]
-        a.o, a.lse, a.o_stride[:] = o.data_ptr(), lse.data_ptr(), o.stride()[:3]
-        g = AttentionGrad(d_o.data_ptr(), *[t.data_ptr() for t in grads], d_o.stride()[:3], *[t.stride()[:3] for t in grads],
-                          space.data_ptr(), need.value)
-        code = lib.mmee_attention_backward(w, a, g, _current_stream())
+    calls = _chain()
+    w = _WORKLOAD(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v, 2)
+    space, need = _space(calls.attention_backward_workspace, w, q, where)
+    d_q, d_k, d_v_ = q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(v.shape)
+    a = _ATTENTION(code, (d_qk or 1) ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+                   *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], lse.data_ptr(),
+                   0 if kv_len is None else kv_len.data_ptr(), 0, 0)
+    g = _ATTENTION_GRAD(d_o.data_ptr(), d_q.data_ptr(), d_k.data_ptr(), d_v_.data_ptr(), *d_o.stride()[:3], *d_q.stride()[:3],
+                        *d_k.stride()[:3], *d_v_.stride()[:3], space.data_ptr(), need)
+    code = calls.attention_backward(w, a, g, _current_stream())
     if code:
         _check(code, where)
-    return tuple(grads)
+    return d_q, d_k, d_v_
+
+
+def _ffn_sizes(where, x, w_gate, w_up, w_down):
+    """(tokens, inner, in, out) of tensors that fit each other."""
+    (tokens, d_in), (d_ff, d), (d_out, inner) = x.shape, w_gate.shape, w_down.shape
+    if d != d_in or w_up.shape != (d_ff, d_in) or inner != d_ff:
+        _refuse(where, "w_gate and w_up are (inner, in), w_down is (out, inner), x is (tokens, in)")
+    return tokens, d_ff, d_in, d_out
+
+
+def mmee_gated_ffn(x, w_gate, w_up, w_down, activation: int = ACT_SILU, save: bool = False, stream=None):
+    """y = (act(x w_gate^T) * (x w_up^T)) w_down^T: (y, saved).  x: (tokens, in), w_gate and w_up: (inner, in), w_down: (out, inner),
+    bfloat16 or float16.  saved: what mmee_gated_ffn_backward needs where `save`, otherwise None.  Asynchronous."""
+    import torch
+    where = "mmee_gated_ffn"
+    code = _chain_code(where, 2, x, w_gate, w_up, w_down)
+    if _elsewhere(x, stream):
+        with _there(x, stream):
+            return mmee_gated_ffn(x, w_gate, w_up, w_down, activation, save)
+    tokens, d_ff, d_in, d_out = _ffn_sizes(where, x, w_gate, w_up, w_down)
+    calls = _chain()
+    w = _WORKLOAD(1, 1, 1, tokens, d_ff, d_in, d_out, 2)
+    hidden, y = x.new_empty((tokens, d_ff)), x.new_empty((tokens, d_out))
+    kept = torch.empty((2, tokens, d_ff), dtype=torch.float32, device=x.device) if save else None
+    f = _FFN(code, activation, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), x.stride(0), w_gate.stride(0),
+             w_up.stride(0), w_down.stride(0), hidden.data_ptr(), kept.data_ptr() if save else 0, y.data_ptr())
+    code = calls.gated_ffn(w, f, _current_stream())
+    if code:
+        _check(code, where)
+    return y, ((hidden, kept) if save else None)
+
+
+def mmee_gated_ffn_backward(d_y, x, w_gate, w_up, w_down, saved, activation: int = ACT_SILU, stream=None):
+    """The gradients (d_x, d_w_gate, d_w_up, d_w_down) of mmee_gated_ffn for a gradient d_y of y; `saved` is what the forward call
+    with the same x, weights and activation returned.  Asynchronous."""
+    import torch
+    where = "mmee_gated_ffn_backward"
+    code = _chain_code(where, 2, x, w_gate, w_up, w_down, d_y, saved[0])
+    if _elsewhere(x, stream):
+        with _there(x, stream):
+            return mmee_gated_ffn_backward(d_y, x, w_gate, w_up, w_down, saved, activation)
+    tokens, d_ff, d_in, d_out = _ffn_sizes(where, x, w_gate, w_up, w_down)
+    hidden, kept = saved
+    if d_y.shape != (tokens, d_out):
+        _refuse(where, "d_y is (tokens, out)")
+    if (hidden.shape != (tokens, d_ff) or not hidden.is_contiguous() or kept.shape != (2, tokens, d_ff) or
+            kept.dtype is not torch.float32 or not kept.is_contiguous() or kept.get_device() != x.get_device()):
+        _refuse(where, "saved is not what the forward call for these tensors returned")
+    calls = _chain()
+    w = _WORKLOAD(1, 1, 1, tokens, d_ff, d_in, d_out, 2)
+    space, need = _space(calls.gated_ffn_workspace, w, x, where)
+    grads = tuple([x.new_empty(t.shape) for t in (x, w_gate, w_up, w_down)])
+    f = _FFN(code, activation, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), x.stride(0), w_gate.stride(0),
+             w_up.stride(0), w_down.stride(0), hidden.data_ptr(), kept.data_ptr(), 0)
+    g = _FFN_GRAD(d_y.data_ptr(), d_y.stride(0), *[t.data_ptr() for t in grads], space.data_ptr() if need else 0, need)
+    code = calls.gated_ffn_backward(w, f, g, _current_stream())
+    if code:
+        _check(code, where)
+    return grads
 
 
 def mmee_chain_status() -> None:

@@ -13,14 +13,6 @@ namespace {
 
 __device__ uint32_t g_gave_up;
 
-// A row's sums refer to a maximum that is moved only when the scores pass it by more than this (in powers of two): the
-// results are the same up to rounding, and moving it means going through the row's sums in tensor memory.
-constexpr float kSlack = 8.f;
-// fp16 has its smallest normal value at 2^-14: probabilities are kept 2^7 larger (at most 2^15 with the slack), which the
-// division by their sum takes out again.
-template <bool BF16>
-__device__ constexpr float kBias = BF16 ? 0.f : 7.f;
-
 // --- forward --------------------------------------------------------------------------------------------------------
 
 template <int DK, int DV>
@@ -379,7 +371,10 @@ int forward(const Problem& x, cudaStream_t stream) {
 
 // Parts that the keys are cut into where the query tiles alone leave most of the multiprocessors without work: as many as fill
 // them once, of at least two tiles each.
-int choose_splits(AttentionParams* p) {
+// Up to 16 query rows to a key head take the kernel for few rows (`cluster` > 0), in `splits` parts that are joined afterwards.
+int choose_splits(AttentionParams* p, uint32_t* cluster) {
+    *cluster = 0;
+    if ((uint64_t)p->group * p->seq_q <= 16) return token_splits(*p, cluster, &p->splits);
     uint32_t sms;
     const int rc = sm_count(&sms);
     if (rc) return rc;
@@ -419,8 +414,10 @@ extern "C" int mmee_attention_workspace(const mmee_workload_t* w, uint64_t* byte
     p.seq_q = w->seq_q;
     p.seq_kv = w->seq_kv;
     p.d_v = w->d_v;
-    if (!p.batch || !p.q_heads || !p.seq_q || !p.seq_kv) return MMEE_ERR_ARG;
-    const int rc = choose_splits(&p);
+    if (!p.batch || w->q_heads < w->kv_heads || !p.seq_q || !p.seq_kv) return MMEE_ERR_ARG;
+    p.group = w->q_heads / w->kv_heads;
+    uint32_t cluster;
+    const int rc = choose_splits(&p, &cluster);
     if (!rc) *bytes = parts_bytes(p);
     return rc;
 }
@@ -428,7 +425,8 @@ extern "C" int mmee_attention_workspace(const mmee_workload_t* w, uint64_t* byte
 extern "C" int mmee_attention(const mmee_workload_t* workload, const mmee_attention_t* a, void* cuda_stream) {
     Problem x;
     int rc = check(workload, a, &x);
-    if (!rc) rc = choose_splits(&x.p);
+    uint32_t cluster;
+    if (!rc) rc = choose_splits(&x.p, &cluster);
     if (rc) return rc;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (x.p.splits > 1) {
@@ -437,7 +435,7 @@ extern "C" int mmee_attention(const mmee_workload_t* workload, const mmee_attent
         x.p.part_o = static_cast<float*>(a->workspace);
         x.p.part_lse = x.p.part_o + rows * x.p.d_v;
     }
-    if ((rc = forward(x, stream))) return rc;
+    if ((rc = cluster ? attention_tokens(x, cluster, stream) : forward(x, stream))) return rc;
     if (x.p.splits > 1) {
         const uint64_t rows = (uint64_t)x.p.batch * x.p.q_heads * x.p.seq_q;
         const uint32_t grid = (uint32_t)ceil_div(rows, 4);

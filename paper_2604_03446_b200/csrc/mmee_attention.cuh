@@ -8,10 +8,16 @@
 
 namespace mmee {
 
-namespace {
-
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr uint32_t kTile = 128;                        // query rows and keys of a tile
+
+// A row's sums refer to a maximum that is moved only when the scores pass it by more than this (in powers of two): the
+// results are the same up to rounding, and moving it means going through the row's sums in tensor memory.
+constexpr float kSlack = 8.f;
+// fp16 has its smallest normal value at 2^-14: probabilities are kept 2^7 larger (at most 2^15 with the slack), which the
+// division by their sum takes out again.
+template <bool BF16>
+__device__ constexpr float kBias = BF16 ? 0.f : 7.f;
 
 struct Strides {
     int64_t batch, token, head;        // elements
@@ -64,15 +70,15 @@ struct View {
     Strides s;
 };
 
-int view_map(CUtensorMap* map, bool bf16, uint32_t batch, const View& v) {
+inline int view_map(CUtensorMap* map, bool bf16, uint32_t batch, const View& v) {
     const uint64_t extent[4] = {v.d, v.seq, v.heads, batch};
     const int64_t stride[3] = {v.s.token, v.s.head, v.s.batch};
     return tile_map(map, bf16, v.base, 4, extent, stride, kTile);
 }
 
-Strides strides(const int64_t s[3]) { return {s[0], s[1], s[2]}; }
+inline Strides strides(const int64_t s[3]) { return {s[0], s[1], s[2]}; }
 
-int check_view(const View& v, uint32_t batch) {
+inline int check_view(const View& v, uint32_t batch) {
     if (!v.base || !aligned16(v.base)) return MMEE_ERR_ARG;
     const int64_t s[3] = {v.s.batch, v.s.token, v.s.head};
     const uint32_t n[3] = {batch, v.seq, v.heads};
@@ -87,7 +93,7 @@ struct Problem {
     bool bf16;
 };
 
-int check(const mmee_workload_t* w, const mmee_attention_t* a, Problem* out) {
+inline int check(const mmee_workload_t* w, const mmee_attention_t* a, Problem* out) {
     if (!w || !a) return MMEE_ERR_ARG;
     if (!w->batch || !w->q_heads || !w->kv_heads || !w->seq_q || !w->seq_kv || !w->d_qk || !w->d_v) return MMEE_ERR_ARG;
     if (w->q_heads % w->kv_heads || w->word_bytes != 2 || (w->d_qk | w->d_v) % 8) return MMEE_ERR_ARG;
@@ -123,6 +129,9 @@ int check(const mmee_workload_t* w, const mmee_attention_t* a, Problem* out) {
     return MMEE_OK;
 }
 
-}  // namespace
+// The kernel for up to 16 query rows to a key head (mmee_attention_token.cu): into how many parts it cuts the keys -- CTAs of a
+// cluster, and clusters -- and its launch (splits: clusters).
+int token_splits(const AttentionParams& a, uint32_t* cluster, uint32_t* clusters);
+int attention_tokens(const Problem& x, uint32_t cluster, cudaStream_t stream);
 
 }  // namespace mmee
