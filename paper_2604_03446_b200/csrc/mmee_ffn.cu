@@ -8,8 +8,7 @@
 //
 // Roundings: sums, gate, up and the gradient of h in 32 bits; h, dg and du are rounded once each to the type of the
 // operands, which the tensor cores need; results once.
-#include "mmee_chain.h"
-#include "mmee_sm100.cuh"
+#include "mmee_ffn.cuh"
 
 namespace mmee {
 
@@ -39,29 +38,6 @@ __device__ __forceinline__ void tile_of(const ProductParams& p, uint32_t i, uint
     const uint32_t rows = min(kGroupM, p.tiles_m - first), r = i - g * per;
     *tm = first + r % rows;
     *tn = r / rows;
-}
-
-// Activation and its derivative.
-__device__ __forceinline__ float act_value(uint32_t act, float g) {
-    if (act == MMEE_ACT_RELU) return g < 0.f ? 0.f : g;
-    if (act == MMEE_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
-    const float s = __fdividef(1.f, 1.f + __expf(-g));
-    return act == MMEE_ACT_SIGMOID ? s : g * s;
-}
-
-__device__ __forceinline__ void act_both(uint32_t act, float g, float* a, float* da) {
-    if (act == MMEE_ACT_RELU) {
-        *a = g < 0.f ? 0.f : g;
-        *da = g > 0.f ? 1.f : 0.f;
-    } else if (act == MMEE_ACT_GELU) {
-        const float cdf = 0.5f * (1.f + erff(g * 0.70710678118654752f));
-        *a = g * cdf;
-        *da = cdf + g * 0.39894228040143268f * __expf(-0.5f * g * g);
-    } else {
-        const float s = __fdividef(1.f, 1.f + __expf(-g));
-        *a = act == MMEE_ACT_SIGMOID ? s : g * s;
-        *da = act == MMEE_ACT_SIGMOID ? s * (1.f - s) : s * (1.f + g * (1.f - s));
-    }
 }
 
 template <int EPI, bool A_MN, bool B_MN, bool BF16>
@@ -341,6 +317,11 @@ extern "C" int mmee_gated_ffn(const mmee_workload_t* workload, const mmee_gated_
     if (!f->y || !aligned16(f->y) || (f->kept && !aligned16(f->kept))) return MMEE_ERR_ARG;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool bf16 = f->dtype == MMEE_BF16;
+    if (s.tokens <= kFewTokens) {
+        const FfnTokens few{s.tokens, s.d_in, s.d_ff, s.d_out, f->activation, f->x, f->w_gate, f->w_up, f->w_down,
+                            f->x_stride, f->w_gate_stride, f->w_up_stride, f->w_down_stride, f->hidden, f->y, f->kept};
+        return ffn_tokens(few, bf16, stream);
+    }
     const Operand x{f->x, s.tokens, s.d_in, f->x_stride}, wg{f->w_gate, s.d_ff, s.d_in, f->w_gate_stride};
     const Operand wu{f->w_up, s.d_ff, s.d_in, f->w_up_stride}, wd{f->w_down, s.d_out, s.d_ff, f->w_down_stride};
     const Operand h{f->hidden, s.tokens, s.d_ff, s.d_ff};

@@ -1,0 +1,169 @@
+// The gated feed-forward block for up to 32 tokens: every weight is read once, and that is what bounds it.
+//
+// A CTA takes 16 rows of the weights, its warps take the reduction in turns of 128.  Weights go from memory straight into the
+// registers of the matrix instructions as their 16 rows, tokens are the columns (mma.sync: the rate does not matter here, and a
+// 128-row tcgen05 tile of tokens would be mostly empty).  Which positions of the reduction a lane holds is free as long as both
+// operands agree, so that it reads sixteen consecutive bytes of a row.  The warps' sums are added in order through shared memory.
+// The second kernel is launched before the first has ended and has its first weights under way when it waits for it.
+#include "mmee_ffn.cuh"
+
+namespace mmee {
+
+namespace {
+
+constexpr uint32_t kTurn = 128;        // values of the reduction that a warp takes at a time
+constexpr uint32_t kMostWarps = 8;
+
+__device__ __forceinline__ uint4 read_once(const uint16_t* p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+// Tokens' values: they come back to L1 for the next rows.  (Not through the read-only path: an earlier kernel of the stream may
+// still be writing them when this one starts.)
+__device__ __forceinline__ uint4 read_token(const uint16_t* p) {
+    uint4 v;
+    asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void mma16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if (BF16)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// GATE: hidden from x, w_gate and w_up; otherwise y from hidden and w_down.  NT: columns of tokens by eight.
+template <bool GATE, int NT, bool BF16>
+__global__ void __launch_bounds__(kMostWarps * 32) ffn_tokens_kernel(const FfnTokens p) {
+    constexpr int kW = GATE ? 2 : 1;   // weight matrices
+    __shared__ float sums[kMostWarps][kW][16][8 * NT + 1];
+    const uint32_t warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, g = lane >> 2, c = lane & 3u;
+    const uint32_t row0 = blockIdx.x * 16, rows = GATE ? p.d_ff : p.d_out, depth = GATE ? p.d_in : p.d_ff;
+    const uint16_t *w0[kW], *w1[kW];   // this lane's two rows
+    bool in[2] = {row0 + g < rows, row0 + g + 8 < rows};
+#pragma unroll
+    for (int m = 0; m < kW; ++m) {
+        const uint16_t* const base = static_cast<const uint16_t*>(GATE ? m ? p.w_up : p.w_gate : p.w_down);
+        const int64_t stride = GATE ? m ? p.w_up_stride : p.w_gate_stride : p.w_down_stride;
+        w0[m] = base + (int64_t)(row0 + g) * stride + 8 * c;
+        w1[m] = w0[m] + 8 * stride;
+    }
+    const uint16_t* const x = static_cast<const uint16_t*>(GATE ? p.x : p.hidden);
+    const int64_t x_stride = GATE ? p.x_stride : (int64_t)p.d_ff;
+    const uint16_t* xr[NT];
+    bool token_in[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        token_in[t] = 8 * t + g < p.tokens;
+        xr[t] = x + (int64_t)(8 * t + g) * x_stride + 8 * c;
+    }
+    float acc[kW][NT][4];
+#pragma unroll
+    for (int i = 0; i < kW * NT * 4; ++i) (&acc[0][0][0])[i] = 0.f;
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    uint4 w[kTurn / 32][kW][2];
+    auto weights = [&](uint32_t k) {
+#pragma unroll
+        for (int j = 0; j < (int)kTurn / 32; ++j)
+#pragma unroll
+            for (int m = 0; m < kW; ++m) {
+                const bool deep = k + 32 * j + 8 * c < depth;
+                w[j][m][0] = in[0] && deep ? read_once(w0[m] + k + 32 * j) : none;
+                w[j][m][1] = in[1] && deep ? read_once(w1[m] + k + 32 * j) : none;
+            }
+    };
+    uint32_t k = warp * kTurn;
+    if (k < depth) weights(k);
+    if (GATE)
+        asm volatile("griddepcontrol.launch_dependents;");
+    else
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+    while (k < depth) {
+#pragma unroll
+        for (int j = 0; j < (int)kTurn / 32; ++j) {
+            const bool deep = k + 32 * j + 8 * c < depth;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const uint4 b = token_in[t] && deep ? read_token(xr[t] + k + 32 * j) : none;
+#pragma unroll
+                for (int m = 0; m < kW; ++m) {
+                    mma16<BF16>(acc[m][t], w[j][m][0].x, w[j][m][1].x, w[j][m][0].y, w[j][m][1].y, b.x, b.y);
+                    mma16<BF16>(acc[m][t], w[j][m][0].z, w[j][m][1].z, w[j][m][0].w, w[j][m][1].w, b.z, b.w);
+                }
+            }
+        }
+        k += warps * kTurn;
+        if (k < depth) weights(k);
+    }
+#pragma unroll
+    for (int m = 0; m < kW; ++m)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sums[warp][m][g + 8 * (i >> 1)][8 * t + 2 * c + (i & 1)] = acc[m][t][i];
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < 16 * p.tokens; i += blockDim.x) {
+        const uint32_t r = i % 16, token = i / 16;
+        if (row0 + r >= rows) continue;
+        float v[kW];
+#pragma unroll
+        for (int m = 0; m < kW; ++m) {
+            v[m] = 0.f;
+            for (uint32_t s = 0; s < warps; ++s) v[m] += sums[s][m][r][token];
+        }
+        const uint64_t at = (uint64_t)token * rows + row0 + r;
+        if (GATE && p.kept) {
+            p.kept[at] = v[0];
+            p.kept[(uint64_t)p.tokens * rows + at] = v[kW - 1];
+        }
+        const float out = GATE ? act_value(p.act, v[0]) * v[kW - 1] : v[0];
+        static_cast<uint16_t*>(GATE ? p.hidden : p.y)[at] = (uint16_t)pack2<BF16>(out, 0.f);
+    }
+}
+
+template <int NT, bool BF16>
+int launch(const FfnTokens& p, cudaStream_t stream) {
+    // As many warps to a CTA as keep some forty of them on a multiprocessor busy, each with a turn at least.
+    uint32_t sms;
+    const int rc = sm_count(&sms);
+    if (rc) return rc;
+    auto warps = [&](uint32_t rows, uint32_t depth) {
+        const uint64_t ctas = ceil_div(rows, 16), most = ceil_div(depth, kTurn);
+        uint32_t n = 1;
+        while (n < kMostWarps && n * 2 <= most && (n < 4 || ctas * n < 40ull * sms)) n *= 2;
+        return n;
+    };
+    ffn_tokens_kernel<true, NT, BF16><<<(uint32_t)ceil_div(p.d_ff, 16), 32 * warps(p.d_ff, p.d_in), 0, stream>>>(p);
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3((uint32_t)ceil_div(p.d_out, 16));
+    c.blockDim = dim3(32 * warps(p.d_out, p.d_ff));
+    c.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = &attr;
+    c.numAttrs = 1;
+    const cudaError_t e = cudaGetLastError();
+    return cuda_status(e != cudaSuccess ? e : cudaLaunchKernelEx(&c, ffn_tokens_kernel<false, NT, BF16>, p));
+}
+
+template <int NT>
+int launch_typed(const FfnTokens& p, bool bf16, cudaStream_t stream) {
+    return bf16 ? launch<NT, true>(p, stream) : launch<NT, false>(p, stream);
+}
+
+}  // namespace
+
+int ffn_tokens(const FfnTokens& p, bool bf16, cudaStream_t stream) {
+    return p.tokens <= 8 ? launch_typed<1>(p, bf16, stream) : p.tokens <= 16 ? launch_typed<2>(p, bf16, stream) : launch_typed<4>(p, bf16, stream);
+}
+
+}  // namespace mmee
