@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmmee.so")
 SOURCES = ["mmee_plan.cu", "mmee_search.cu", "mmee_views.cu", "mmee_api.cu", "mmee_workspace.cu", "mmee_alu_peak.cu", "mmee_static.cu", "mmee_prune.cu",
-           "mmee_chain.cu", "mmee_attention.cu", "mmee_attention_token.cu", "mmee_attention_grad.cu", "mmee_ffn.cu", "mmee_ffn_tokens.cu"]
+           "mmee_chain.cu", "mmee_attention.cu", "mmee_attention_token.cu", "mmee_attention_grad.cu", "mmee_ffn.cu", "mmee_ffn_tokens.cu", "mmee_ffn_narrow.cu"]
 HEADERS = ["mmee_plan.h", "mmee_search.h", "mmee_workspace.h", "mmee_eval.cuh", "mmee_classes.cuh", "mmee_block.cuh",
            "mmee_chain.h", "mmee_sm100.cuh", "mmee_attention.cuh", "mmee_ffn.cuh", os.path.join("..", "..", "include", "mmee.h")]
 NVCC_FLAGS = ["-t", "0", "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",

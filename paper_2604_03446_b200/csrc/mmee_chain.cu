@@ -58,9 +58,13 @@ int allow_smem(const void* kernel, uint32_t bytes) {
 }  // namespace mmee
 
 extern "C" int mmee_chain_status(void) {
-    uint32_t a = 0, g = 0, f = 0;
-    int rc = mmee::attention_gave_up(&a);
-    if (!rc) rc = mmee::attention_grad_gave_up(&g);
-    if (!rc) rc = mmee::ffn_gave_up(&f);
-    return rc ? rc : a | g | f ? MMEE_ERR_TIMEOUT : MMEE_OK;
+    int (*const words[])(uint32_t*) = {mmee::attention_gave_up, mmee::attention_grad_gave_up, mmee::ffn_gave_up, mmee::ffn_narrow_gave_up};
+    uint32_t any = 0;
+    for (const auto word : words) {
+        uint32_t w = 0;
+        const int rc = word(&w);
+        if (rc) return rc;
+        any |= w;
+    }
+    return any ? MMEE_ERR_TIMEOUT : MMEE_OK;
 }

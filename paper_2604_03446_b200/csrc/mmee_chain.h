@@ -29,5 +29,6 @@ inline uint64_t round_up(uint64_t a, uint64_t b) { return ceil_div(a, b) * b; }
 int attention_gave_up(uint32_t* word);
 int attention_grad_gave_up(uint32_t* word);
 int ffn_gave_up(uint32_t* word);
+int ffn_narrow_gave_up(uint32_t* word);
 
 }  // namespace mmee

@@ -317,10 +317,11 @@ extern "C" int mmee_gated_ffn(const mmee_workload_t* workload, const mmee_gated_
     if (!f->y || !aligned16(f->y) || (f->kept && !aligned16(f->kept))) return MMEE_ERR_ARG;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool bf16 = f->dtype == MMEE_BF16;
-    if (s.tokens <= kFewTokens) {
+    if (s.tokens <= kNarrow) {
         const FfnTokens few{s.tokens, s.d_in, s.d_ff, s.d_out, f->activation, f->x, f->w_gate, f->w_up, f->w_down,
                             f->x_stride, f->w_gate_stride, f->w_up_stride, f->w_down_stride, f->hidden, f->y, f->kept};
-        return ffn_tokens(few, bf16, stream);
+        const uint64_t bytes = 2ull * s.d_ff * (2ull * s.d_in + s.d_out);
+        return s.tokens <= kFew && bytes < kFewBytes ? ffn_tokens(few, bf16, stream) : ffn_narrow(few, bf16, stream);
     }
     const Operand x{f->x, s.tokens, s.d_in, f->x_stride}, wg{f->w_gate, s.d_ff, s.d_in, f->w_gate_stride};
     const Operand wu{f->w_up, s.d_ff, s.d_in, f->w_up_stride}, wd{f->w_down, s.d_out, s.d_ff, f->w_down_stride};

@@ -29,8 +29,12 @@ __device__ __forceinline__ void act_both(uint32_t act, float g, float* a, float*
     }
 }
 
-// The block for up to kFewTokens tokens (mmee_ffn_tokens.cu).
-constexpr uint32_t kFewTokens = 32;
+// The block for few tokens, which the weights' way from memory bounds.  Up to kNarrow tokens: mmee_ffn_narrow.cu; up to kFew
+// tokens and weights of less than kFewBytes: mmee_ffn_tokens.cu, which starts faster and reads slower.
+// One token, us (narrow, few): 12.6 MB of weights 9.1 and 14.4; 67 MB 20.6 and 22.4; 403 MB 73.7 and 68.6.  Thirteen tokens, 67 MB:
+// 28.8 and 24.1.  128 tokens (narrow, tiles of 128 x 256): 25 MB 41 and 40, 67 MB 55 and 78, 403 MB 119 and 151.
+constexpr uint32_t kFew = 8, kNarrow = 128;
+constexpr uint64_t kFewBytes = 96ull << 20;
 struct FfnTokens {
     uint32_t tokens, d_in, d_ff, d_out, act;
     const void *x, *w_gate, *w_up, *w_down;
@@ -39,5 +43,6 @@ struct FfnTokens {
     float* kept;                       // gate, then up; or null
 };
 int ffn_tokens(const FfnTokens& p, bool bf16, cudaStream_t stream);
+int ffn_narrow(const FfnTokens& p, bool bf16, cudaStream_t stream);
 
 }  // namespace mmee

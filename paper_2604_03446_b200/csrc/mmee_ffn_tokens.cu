@@ -1,4 +1,5 @@
-// The gated feed-forward block for up to 32 tokens: every weight is read once, and that is what bounds it.
+// The gated feed-forward block for up to eight tokens and weights of moderate size: every weight is read once, and that is what
+// bounds it.  (Where the weights are large, or the tokens more, mmee_ffn_narrow.cu.)
 //
 // A CTA takes 16 rows of the weights, its warps take the reduction in turns of 128.  Weights go from memory straight into the
 // registers of the matrix instructions as their 16 rows, tokens are the columns (mma.sync: the rate does not matter here, and a
@@ -11,7 +12,6 @@ namespace mmee {
 
 namespace {
 
-constexpr uint32_t kTurn = 128;        // values of the reduction that a warp takes at a time
 constexpr uint32_t kMostWarps = 8;
 
 __device__ __forceinline__ uint4 read_once(const uint16_t* p) {
@@ -40,11 +40,16 @@ __device__ __forceinline__ void mma16(float* d, uint32_t a0, uint32_t a1, uint32
             : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// GATE: hidden from x, w_gate and w_up; otherwise y from hidden and w_down.  NT: columns of tokens by eight.
-template <bool GATE, int NT, bool BF16>
-__global__ void __launch_bounds__(kMostWarps * 32) ffn_tokens_kernel(const FfnTokens p) {
+// GATE: hidden from x, w_gate and w_up; otherwise y from hidden and w_down.
+// A warp has two turns of eight sixteen-byte reads a lane under way.  Measured at 4096-16384-4096, one token: two CTAs of eight
+// warps a multiprocessor with the second turn 73.7 us; four CTAs without it 79; one turn of sixteen reads 85; three CTAs, whose
+// registers do not hold two turns, 94.
+template <bool GATE, bool BF16>
+__global__ void __launch_bounds__(kMostWarps * 32, 2) ffn_tokens_kernel(const FfnTokens p) {
     constexpr int kW = GATE ? 2 : 1;   // weight matrices
-    __shared__ float sums[kMostWarps][kW][16][8 * NT + 1];
+    constexpr int kC = 4 / kW;         // steps of 32 in a turn
+    constexpr uint32_t kTurn = 32 * kC;
+    __shared__ float sums[kMostWarps][kW][16][9];
     const uint32_t warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, g = lane >> 2, c = lane & 3u;
     const uint32_t row0 = blockIdx.x * 16, rows = GATE ? p.d_ff : p.d_out, depth = GATE ? p.d_in : p.d_ff;
     const uint16_t *w0[kW], *w1[kW];   // this lane's two rows
@@ -58,57 +63,53 @@ __global__ void __launch_bounds__(kMostWarps * 32) ffn_tokens_kernel(const FfnTo
     }
     const uint16_t* const x = static_cast<const uint16_t*>(GATE ? p.x : p.hidden);
     const int64_t x_stride = GATE ? p.x_stride : (int64_t)p.d_ff;
-    const uint16_t* xr[NT];
-    bool token_in[NT];
+    const uint16_t* const xr = x + (int64_t)g * x_stride + 8 * c;
+    const bool token_in = g < p.tokens;
+    float acc[kW][4];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        token_in[t] = 8 * t + g < p.tokens;
-        xr[t] = x + (int64_t)(8 * t + g) * x_stride + 8 * c;
-    }
-    float acc[kW][NT][4];
-#pragma unroll
-    for (int i = 0; i < kW * NT * 4; ++i) (&acc[0][0][0])[i] = 0.f;
+    for (int i = 0; i < kW * 4; ++i) (&acc[0][0])[i] = 0.f;
     const uint4 none = make_uint4(0, 0, 0, 0);
-    uint4 w[kTurn / 32][kW][2];
-    auto weights = [&](uint32_t k) {
+    uint4 w[2][kC][kW][2];
+    auto weights = [&](uint4 (&to)[kC][kW][2], uint32_t k) {
 #pragma unroll
-        for (int j = 0; j < (int)kTurn / 32; ++j)
+        for (int j = 0; j < kC; ++j)
 #pragma unroll
             for (int m = 0; m < kW; ++m) {
                 const bool deep = k + 32 * j + 8 * c < depth;
-                w[j][m][0] = in[0] && deep ? read_once(w0[m] + k + 32 * j) : none;
-                w[j][m][1] = in[1] && deep ? read_once(w1[m] + k + 32 * j) : none;
+                to[j][m][0] = in[0] && deep ? read_once(w0[m] + k + 32 * j) : none;
+                to[j][m][1] = in[1] && deep ? read_once(w1[m] + k + 32 * j) : none;
             }
     };
+    auto multiply = [&](const uint4 (&v)[kC][kW][2], uint32_t k) {
+#pragma unroll
+        for (int j = 0; j < kC; ++j) {
+            const bool deep = k + 32 * j + 8 * c < depth;
+            const uint4 b = token_in && deep ? read_token(xr + k + 32 * j) : none;
+#pragma unroll
+            for (int m = 0; m < kW; ++m) {
+                mma16<BF16>(acc[m], v[j][m][0].x, v[j][m][1].x, v[j][m][0].y, v[j][m][1].y, b.x, b.y);
+                mma16<BF16>(acc[m], v[j][m][0].z, v[j][m][1].z, v[j][m][0].w, v[j][m][1].w, b.z, b.w);
+            }
+        }
+    };
+    const uint32_t step = warps * kTurn;
     uint32_t k = warp * kTurn;
-    if (k < depth) weights(k);
+    weights(w[0], k);
+    weights(w[1], k + step);
     if (GATE)
         asm volatile("griddepcontrol.launch_dependents;");
     else
         asm volatile("griddepcontrol.wait;" ::: "memory");
-    while (k < depth) {
-#pragma unroll
-        for (int j = 0; j < (int)kTurn / 32; ++j) {
-            const bool deep = k + 32 * j + 8 * c < depth;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const uint4 b = token_in[t] && deep ? read_token(xr[t] + k + 32 * j) : none;
-#pragma unroll
-                for (int m = 0; m < kW; ++m) {
-                    mma16<BF16>(acc[m][t], w[j][m][0].x, w[j][m][1].x, w[j][m][0].y, w[j][m][1].y, b.x, b.y);
-                    mma16<BF16>(acc[m][t], w[j][m][0].z, w[j][m][1].z, w[j][m][0].w, w[j][m][1].w, b.z, b.w);
-                }
-            }
-        }
-        k += warps * kTurn;
-        if (k < depth) weights(k);
+    for (; k < depth; k += 2 * step) {
+        multiply(w[0], k);
+        weights(w[0], k + 2 * step);
+        multiply(w[1], k + step);
+        weights(w[1], k + 3 * step);
     }
 #pragma unroll
     for (int m = 0; m < kW; ++m)
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sums[warp][m][g + 8 * (i >> 1)][8 * t + 2 * c + (i & 1)] = acc[m][t][i];
+        for (int i = 0; i < 4; ++i) sums[warp][m][g + 8 * (i >> 1)][2 * c + (i & 1)] = acc[m][i];
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < 16 * p.tokens; i += blockDim.x) {
         const uint32_t r = i % 16, token = i / 16;
@@ -129,22 +130,18 @@ __global__ void __launch_bounds__(kMostWarps * 32) ffn_tokens_kernel(const FfnTo
     }
 }
 
-template <int NT, bool BF16>
+template <bool BF16>
 int launch(const FfnTokens& p, cudaStream_t stream) {
-    // As many warps to a CTA as keep some forty of them on a multiprocessor busy, each with a turn at least.
-    uint32_t sms;
-    const int rc = sm_count(&sms);
-    if (rc) return rc;
-    auto warps = [&](uint32_t rows, uint32_t depth) {
-        const uint64_t ctas = ceil_div(rows, 16), most = ceil_div(depth, kTurn);
+    // As many warps to a CTA as there are turns, eight at most.
+    auto threads = [](uint32_t depth, uint32_t turn) {
         uint32_t n = 1;
-        while (n < kMostWarps && n * 2 <= most && (n < 4 || ctas * n < 40ull * sms)) n *= 2;
-        return n;
+        while (n < kMostWarps && n * 2 * turn <= depth) n *= 2;
+        return 32 * n;
     };
-    ffn_tokens_kernel<true, NT, BF16><<<(uint32_t)ceil_div(p.d_ff, 16), 32 * warps(p.d_ff, p.d_in), 0, stream>>>(p);
+    ffn_tokens_kernel<true, BF16><<<(uint32_t)ceil_div(p.d_ff, 16), threads(p.d_in, 64), 0, stream>>>(p);
     cudaLaunchConfig_t c{};
     c.gridDim = dim3((uint32_t)ceil_div(p.d_out, 16));
-    c.blockDim = dim3(32 * warps(p.d_out, p.d_ff));
+    c.blockDim = dim3(threads(p.d_ff, 128));
     c.stream = stream;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -152,18 +149,11 @@ int launch(const FfnTokens& p, cudaStream_t stream) {
     c.attrs = &attr;
     c.numAttrs = 1;
     const cudaError_t e = cudaGetLastError();
-    return cuda_status(e != cudaSuccess ? e : cudaLaunchKernelEx(&c, ffn_tokens_kernel<false, NT, BF16>, p));
-}
-
-template <int NT>
-int launch_typed(const FfnTokens& p, bool bf16, cudaStream_t stream) {
-    return bf16 ? launch<NT, true>(p, stream) : launch<NT, false>(p, stream);
+    return cuda_status(e != cudaSuccess ? e : cudaLaunchKernelEx(&c, ffn_tokens_kernel<false, BF16>, p));
 }
 
 }  // namespace
 
-int ffn_tokens(const FfnTokens& p, bool bf16, cudaStream_t stream) {
-    return p.tokens <= 8 ? launch_typed<1>(p, bf16, stream) : p.tokens <= 16 ? launch_typed<2>(p, bf16, stream) : launch_typed<4>(p, bf16, stream);
-}
+int ffn_tokens(const FfnTokens& p, bool bf16, cudaStream_t stream) { return bf16 ? launch<true>(p, stream) : launch<false>(p, stream); }
 
 }  // namespace mmee
