@@ -1,10 +1,11 @@
 // The gated feed-forward block, run: h = act(x Wg^T) * (x Wu^T), y = h Wd^T, and its gradients.
 //
-// Every product is one kernel template: a CTA per SM goes through tiles of 128 x 256 results, operands stream through
-// shared memory by TMA, one thread issues the matrix instructions into one of two accumulators in tensor memory, four
-// warps empty the other.  Operands lie with the reduction along their rows (K-major) or along their columns (MN-major), so
-// that no product needs a transposed copy.  The gate kernel puts 128 rows of Wg and the same 128 rows of Wu into one
-// operand tile: both projections of a value of h end in one thread, which applies activation and product.
+// Every product is one kernel template: pairs of CTAs go through tiles of 256 x 256 results (single ones through smaller
+// tiles where those would be too few), operands stream through shared memory by TMA, one thread issues the matrix
+// instructions into one of two accumulators in tensor memory, four warps a CTA empty the other.  Operands lie with the
+// reduction along their rows (K-major) or along their columns (MN-major), so that no product needs a transposed copy.  The
+// gate kernel puts rows of Wg and the same rows of Wu into one operand tile: both projections of a value of h end in one
+// thread, which applies activation and product.
 //
 // Roundings: sums, gate, up and the gradient of h in 32 bits; h, dg and du are rounded once each to the type of the
 // operands, which the tensor cores need; results once.
@@ -18,37 +19,57 @@ __device__ uint32_t g_gave_up;
 
 enum Epilogue { kPlain, kGate, kGrad };
 
-struct ProductParams {
+// One product of a launch.
+struct Product {
     uint32_t m, n;                     // results: rows, columns (kGate: columns of h)
     uint32_t chunks0, chunks1;         // steps of 64 along the reduction, first and second pair of operands
-    uint32_t tiles_m, tiles_n;
+    uint32_t tiles_m, tiles_n, end;    // `end`: tiles of the launch up to here
+    uint32_t a_mn, b_mn;               // the operand lies with the reduction along its columns
     uint32_t act;
     void *out, *out2;                  // kPlain: the product; kGate: h; kGrad: dg, du
     int64_t out_stride;                // elements from row to row of out and out2
     float *gate, *up;                  // kGate: where to keep them, or null; kGrad: what was kept.  Rows of n
 };
 
-constexpr uint32_t kTileM = 128, kTileN = 256, kStages = 4;
-constexpr uint32_t kTileABytes = kTileM * kRowBytes, kTileBBytes = kTileN * kRowBytes;
-constexpr uint32_t kProductSmem = kStages * (kTileABytes + kTileBBytes) + 1024;
-constexpr uint32_t kGroupM = 16;       // tile rows that are gone through together, so that their operands stay in L2
+constexpr uint32_t kMostProducts = 4;
+struct Products {
+    CUtensorMap a0[kMostProducts], b0[kMostProducts], a1[kMostProducts], b1[kMostProducts];
+    Product of[kMostProducts];
+    uint32_t count;
+};
 
-__device__ __forceinline__ void tile_of(const ProductParams& p, uint32_t i, uint32_t* tm, uint32_t* tn) {
-    const uint32_t per = kGroupM * p.tiles_n, g = i / per, first = g * kGroupM;
-    const uint32_t rows = min(kGroupM, p.tiles_m - first), r = i - g * per;
+// A tile: 128 rows to a CTA, PAIR: of two CTAs that share the columns' operand.
+template <bool PAIR, int TN>
+struct TileShape {
+    static constexpr uint32_t kM = PAIR ? 256 : 128, kRowsB = PAIR ? TN / 2 : TN;      // rows of a tile; of B in a CTA
+    static constexpr uint32_t kA = 128 * kRowBytes, kB = kRowsB * kRowBytes;
+    static constexpr uint32_t kStages = (200 * 1024) / (kA + kB);
+    static constexpr uint32_t smem = kStages * (kA + kB) + 1024;
+};
+
+constexpr uint32_t kGroupRows = 2048;  // result rows that are gone through together, so that their operands stay in L2
+
+template <uint32_t TM>
+__device__ __forceinline__ void tile_of(const Product& p, uint32_t i, uint32_t* tm, uint32_t* tn) {
+    constexpr uint32_t kGroup = kGroupRows / TM;
+    const uint32_t per = kGroup * p.tiles_n, g = i / per, first = g * kGroup;
+    const uint32_t rows = min(kGroup, p.tiles_m - first), r = i - g * per;
     *tm = first + r % rows;
     *tn = r / rows;
 }
 
-template <int EPI, bool A_MN, bool B_MN, bool BF16>
-__global__ void __launch_bounds__(192, 1)
-product_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap b0,
-               const __grid_constant__ CUtensorMap a1, const __grid_constant__ CUtensorMap b1, const ProductParams p) {
+template <int EPI, bool PAIR, int TN, bool BF16>
+__global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__ Products ps) {
+    using Shape = TileShape<PAIR, TN>;
+    constexpr uint32_t kStages = Shape::kStages, kStage = Shape::kA + Shape::kB;
+    constexpr uint32_t kCols = EPI == kGate ? TN / 2 : TN;             // columns of the result in a tile
+    constexpr uint32_t kRowsX = EPI == kGate && !PAIR ? TN / 2 : Shape::kRowsB;    // rows of B from one matrix in a CTA
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
     __shared__ uint32_t tmem_base, gave_up;
     const uint32_t tiles = (smem_addr(raw) + 1023u) & ~1023u;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const uint32_t rank = PAIR ? cluster_rank() : 0, workers = PAIR ? gridDim.x / 2 : gridDim.x, worker = PAIR ? blockIdx.x / 2 : blockIdx.x;
     const uint32_t bar0 = smem_addr(bars);
     auto full = [&](uint32_t s) { return bar0 + 8 * s; };
     auto empty = [&](uint32_t s) { return bar0 + 8 * (kStages + s); };
@@ -63,64 +84,100 @@ product_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__ C
         }
         for (uint32_t b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);
-            mbar_init(acc_empty(b), 128);
+            mbar_init(acc_empty(b), PAIR ? 8 : 4);     // an arrival of every warp that empties it
         }
         mbar_init(drained, 1);
         mbar_init_visible();
     }
-    if (warp == 5) tmem_alloc(&tmem_base, 512);
+    if (warp == 5) {
+        if constexpr (PAIR)
+            tmem_alloc_pair(&tmem_base, 2 * TN);
+        else
+            tmem_alloc(&tmem_base, 2 * TN);
+    }
     tcgen05_fence_before();
-    __syncthreads();
+    if constexpr (PAIR)
+        cluster_barrier();
+    else
+        __syncthreads();
     tcgen05_fence_after();
     const uint32_t tmem = tmem_base;
     volatile uint32_t* const lost = &gave_up;
-    const uint32_t n_tiles = p.tiles_m * p.tiles_n, chunks = p.chunks0 + p.chunks1;
-    constexpr uint32_t kCols = EPI == kGate ? kTileN / 2 : kTileN;      // columns of the result in a tile
+    const uint32_t n_tiles = ps.of[ps.count - 1].end;
+    // The product that tile i is part of, and the tile's number there.
+    auto product_of = [&](uint32_t i, uint32_t* at) {
+        uint32_t k = 0;
+        while (i >= ps.of[k].end) ++k;
+        *at = i - (k ? ps.of[k - 1].end : 0);
+        return k;
+    };
+
+    auto commit = [](uint32_t bar) {
+        if constexpr (PAIR)
+            mma_commit_pair(bar);
+        else
+            mma_commit(bar);
+    };
 
     if (warp == 4) {                                   // operands
         if (elect_one()) {
             uint32_t it = 0;
             bool sound = true;
-            for (uint32_t i = blockIdx.x; i < n_tiles && sound; i += gridDim.x) {
-                uint32_t tm, tn;
-                tile_of(p, i, &tm, &tn);
-                const int32_t m0 = (int32_t)(tm * kTileM), n0 = (int32_t)(tn * kCols);
-                for (uint32_t c = 0; c < chunks; ++c, ++it) {
+            for (uint32_t i = worker; i < n_tiles && sound; i += workers) {
+                uint32_t at, tm, tn;
+                const uint32_t k = product_of(i, &at);
+                const Product& p = ps.of[k];
+                tile_of<Shape::kM>(p, at, &tm, &tn);
+                const int32_t m0 = (int32_t)(tm * Shape::kM + rank * 128), n0 = (int32_t)(tn * kCols + (EPI == kGate ? 0 : rank * Shape::kRowsB));
+                for (uint32_t c = 0; c < p.chunks0 + p.chunks1; ++c, ++it) {
                     const uint32_t s = it % kStages;
                     if (!mbar_wait(empty(s), ((it / kStages) & 1) ^ 1, lost)) {
                         sound = false;
                         break;
                     }
-                    const CUtensorMap *ma = c < p.chunks0 ? &a0 : &a1, *mb = c < p.chunks0 || EPI == kGate ? &b0 : &b1;
-                    const int32_t k = (int32_t)((c < p.chunks0 ? c : c - p.chunks0) * 64);
-                    const uint32_t sa = tiles + s * (kTileABytes + kTileBBytes), sb = sa + kTileABytes, f = full(s);
-                    mbar_expect(f, kTileABytes + kTileBBytes);
-                    if (A_MN) {
-                        for (int32_t j = 0; j < 2; ++j) tma_load_2d(sa + j * 64 * kRowBytes, ma, f, m0 + 64 * j, k);
+                    const bool one = c < p.chunks0;
+                    const CUtensorMap *ma = one ? &ps.a0[k] : &ps.a1[k], *mb = one ? &ps.b0[k] : &ps.b1[k];
+                    if (EPI == kGate) mb = PAIR && rank ? &ps.b1[k] : &ps.b0[k];
+                    const int32_t d = (int32_t)((one ? c : c - p.chunks0) * 64);
+                    const uint32_t sa = tiles + s * kStage, sb = sa + Shape::kA;
+                    // The leader's barrier counts both CTAs' bytes (the other's may come before it is told how many).
+                    const uint32_t f = PAIR ? pair_leader(full(s)) : full(s);
+                    if (rank == 0) mbar_expect(full(s), (PAIR ? 2 : 1) * kStage);
+                    auto load = [&](uint32_t to, const CUtensorMap* map, int32_t x, int32_t y) {
+                        if constexpr (PAIR)
+                            tma_load_2d_pair(to, map, f, x, y);
+                        else
+                            tma_load_2d(to, map, f, x, y);
+                    };
+                    if (p.a_mn) {
+                        for (int32_t j = 0; j < 2; ++j) load(sa + j * 64 * kRowBytes, ma, m0 + 64 * j, d);
                     } else {
-                        tma_load_2d(sa, ma, f, k, m0);
+                        load(sa, ma, d, m0);
                     }
-                    if (EPI == kGate) {
-                        tma_load_2d(sb, &b0, f, k, n0);
-                        tma_load_2d(sb + 128 * kRowBytes, &b1, f, k, n0);
-                    } else if (B_MN) {
-                        for (int32_t j = 0; j < 4; ++j) tma_load_2d(sb + j * 64 * kRowBytes, mb, f, n0 + 64 * j, k);
+                    if (p.b_mn) {
+                        for (int32_t j = 0; j < (int32_t)Shape::kRowsB / 64; ++j) load(sb + j * 64 * kRowBytes, mb, n0 + 64 * j, d);
                     } else {
-                        for (int32_t j = 0; j < 2; ++j) tma_load_2d(sb + j * 128 * kRowBytes, mb, f, k, n0 + 128 * j);
+                        // (boxes of 128 rows, of 64 where a CTA holds no more)
+                        constexpr int32_t kBox = kRowsX < 128 ? kRowsX : 128;
+                        for (int32_t j = 0; j < (int32_t)kRowsX / kBox; ++j) load(sb + j * kBox * kRowBytes, mb, d, n0 + kBox * j);
+                        if (EPI == kGate && !PAIR) load(sb + kRowsX * kRowBytes, &ps.b1[k], d, n0);
                     }
                 }
             }
-            if (!sound)                                // what is in flight lands before the CTA ends
+            if (!sound && rank == 0)                   // what is in flight lands before the CTA ends
                 for (uint32_t s = 0; s < kStages; ++s)
                     if (it > s) mbar_wait(full(s), ((it - 1 - s) / kStages) & 1, nullptr);
         }
         __syncwarp();
-    } else if (warp == 5) {                            // matrix instructions
-        constexpr uint32_t desc = mma_desc(BF16, kTileM, kTileN, A_MN, B_MN);
+    } else if (warp == 5) {                            // matrix instructions, of a pair the leader's
         uint32_t it = 0, n = 0;
-        bool sound = true;
-        for (uint32_t i = blockIdx.x; i < n_tiles && sound; i += gridDim.x, ++n) {
+        bool sound = rank == 0;
+        for (uint32_t i = worker; i < n_tiles && sound; i += workers, ++n) {
             const uint32_t b = n & 1;
+            uint32_t at;
+            const Product& p = ps.of[product_of(i, &at)];
+            const uint32_t chunks = p.chunks0 + p.chunks1, desc = mma_desc(BF16, Shape::kM, TN, p.a_mn, p.b_mn);
+            const uint64_t step_a = p.a_mn ? kStepMN : kStepK, step_b = p.b_mn ? kStepMN : kStepK;
             if (!mbar_wait(acc_empty(b), ((n >> 1) & 1) ^ 1, lost)) break;
             tcgen05_fence_after();
             for (uint32_t c = 0; c < chunks; ++c, ++it) {
@@ -130,34 +187,39 @@ product_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__ C
                     break;
                 }
                 tcgen05_fence_after();
-                const uint32_t sa = tiles + s * (kTileABytes + kTileBBytes), sb = sa + kTileABytes;
-                const uint64_t da = tile_desc(sa, A_MN ? 64 * kRowBytes : 16), db = tile_desc(sb, B_MN ? 64 * kRowBytes : 16);
+                const uint32_t sa = tiles + s * kStage, sb = sa + Shape::kA;
+                const uint64_t da = tile_desc(sa, p.a_mn ? 64 * kRowBytes : 16), db = tile_desc(sb, p.b_mn ? 64 * kRowBytes : 16);
                 if (elect_one()) {
-                    for (uint32_t k = 0; k < 4; ++k)
-                        mma_ss(tmem + b * kTileN, da + k * (A_MN ? kStepMN : kStepK), db + k * (B_MN ? kStepMN : kStepK), desc, c | k);
-                    mma_commit(empty(s));
-                    if (c + 1 == chunks) mma_commit(acc_full(b));
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) {
+                        if constexpr (PAIR)
+                            mma_ss_pair(tmem + b * TN, da + k * step_a, db + k * step_b, desc, c | k);
+                        else
+                            mma_ss(tmem + b * TN, da + k * step_a, db + k * step_b, desc, c | k);
+                    }
+                    commit(empty(s));
+                    if (c + 1 == chunks) commit(acc_full(b));
                 }
                 __syncwarp();
             }
         }
     } else {                                           // results
         uint32_t n = 0;
-        const uint32_t row_in = warp * 32 + lane;
-        for (uint32_t i = blockIdx.x; i < n_tiles; i += gridDim.x, ++n) {
+        for (uint32_t i = worker; i < n_tiles; i += workers, ++n) {
             const uint32_t b = n & 1;
-            uint32_t tm, tn;
-            tile_of(p, i, &tm, &tn);
+            uint32_t at, tm, tn;
+            const Product& p = ps.of[product_of(i, &at)];
+            tile_of<Shape::kM>(p, at, &tm, &tn);
             if (!mbar_wait(acc_full(b), (n >> 1) & 1, lost)) break;
             tcgen05_fence_after();
-            const uint32_t acc = tmem + b * kTileN + ((warp * 32) << 16);
-            const uint32_t row = tm * kTileM + row_in;
+            const uint32_t acc = tmem + b * TN + ((warp * 32) << 16);
+            const uint32_t row = tm * Shape::kM + rank * 128 + warp * 32 + lane;
             const bool in = row < p.m;
             for (uint32_t c = 0; c < kCols; c += 32) {
                 const uint32_t col = tn * kCols + c;
                 uint32_t x[32], y[32];
                 tmem_load32(acc + c, x);
-                if (EPI == kGate) tmem_load32(acc + kTileN / 2 + c, y);
+                if (EPI == kGate) tmem_load32(acc + TN / 2 + c, y);
                 tmem_loaded32(x);
                 if (EPI == kGate) tmem_loaded32(y);
                 if (in && col < p.n) {
@@ -218,21 +280,38 @@ product_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__ C
                 __syncwarp();
             }
             tcgen05_fence_before();
-            mbar_arrive(acc_empty(b));
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (PAIR)
+                    mbar_arrive_cluster(pair_leader(acc_empty(b)));
+                else
+                    mbar_arrive(acc_empty(b));
+            }
         }
     }
-    __syncthreads();
+    __syncwarp();
+    tcgen05_fence_before();
+    // (of a pair: neither's shared or tensor memory goes away while the other uses it)
+    if constexpr (PAIR)
+        cluster_barrier();
+    else
+        __syncthreads();
     if (warp == 5) {
         if (gave_up) {                                 // matrix instructions in flight end before their memory is freed
             if (elect_one()) {
                 g_gave_up = 1;
-                mma_commit(drained);
-                mbar_wait(drained, 0, nullptr);
+                if (rank == 0) {
+                    commit(drained);
+                    mbar_wait(drained, 0, nullptr);
+                }
             }
             __syncwarp();
         }
         tcgen05_fence_after();
-        tmem_free(tmem, 512);
+        if constexpr (PAIR)
+            tmem_free_pair(tmem, 2 * TN);
+        else
+            tmem_free(tmem, 2 * TN);
     }
 }
 
@@ -240,37 +319,80 @@ struct Operand {
     const void* base;
     uint64_t rows, cols;               // as it lies in memory: `cols` values side by side
     int64_t stride;
+    bool mn;                           // the reduction is along its rows
 };
 
-int operand_map(CUtensorMap* map, bool bf16, const Operand& o, uint32_t box_rows) {
-    const uint64_t extent[2] = {o.cols, o.rows};
-    return tile_map(map, bf16, o.base, 2, extent, &o.stride, box_rows);
+// Adds a product to a launch.  a1, b1: the second pair of operands (kGate: b1 is the second projection; kPlain: added), or null.
+void add_product(Products* ps, Operand* (&ops)[kMostProducts][4], Product p, Operand* a0, Operand* b0, Operand* a1, Operand* b1) {
+    p.a_mn = a0->mn;
+    p.b_mn = b0->mn;
+    p.chunks0 = (uint32_t)ceil_div(a0->mn ? a0->rows : a0->cols, 64);
+    p.chunks1 = a1 ? (uint32_t)ceil_div(a1->mn ? a1->rows : a1->cols, 64) : 0;
+    Operand* const all[4] = {a0, b0, a1, b1};
+    for (int i = 0; i < 4; ++i) ops[ps->count][i] = all[i];
+    ps->of[ps->count++] = p;
 }
 
-// One product.  a1, b1: the second pair of operands (kGate: b1 is the second projection; kPlain: added), or null.
-template <int EPI, bool A_MN, bool B_MN>
-int product(bool bf16, const Operand& a0, const Operand& b0, const Operand* a1, const Operand* b1, ProductParams p, cudaStream_t stream) {
-    CUtensorMap ma0, mb0, ma1, mb1;
-    const uint32_t rows_a = A_MN ? 64 : 128, rows_b = B_MN ? 64 : 128;
-    int rc = operand_map(&ma0, bf16, a0, rows_a);
-    if (!rc) rc = operand_map(&mb0, bf16, b0, rows_b);
-    if (!rc) rc = operand_map(&ma1, bf16, a1 ? *a1 : a0, rows_a);
-    if (!rc) rc = operand_map(&mb1, bf16, b1 ? *b1 : b0, rows_b);
+template <int EPI, bool PAIR, int TN, bool BF16>
+int launch_products(Products& ps, Operand* (&ops)[kMostProducts][4], uint32_t sms, cudaStream_t stream) {
+    using Shape = TileShape<PAIR, TN>;
+    constexpr uint32_t kRowsX = EPI == kGate && !PAIR ? TN / 2 : Shape::kRowsB;
+    uint32_t end = 0;
+    int rc = MMEE_OK;
+    for (uint32_t i = 0; i < ps.count && !rc; ++i) {
+        Product& p = ps.of[i];
+        p.tiles_m = (uint32_t)ceil_div(p.m, Shape::kM);
+        p.tiles_n = (uint32_t)ceil_div(p.n, EPI == kGate ? TN / 2 : TN);
+        p.end = end += p.tiles_m * p.tiles_n;
+        CUtensorMap* const maps[4] = {&ps.a0[i], &ps.b0[i], &ps.a1[i], &ps.b1[i]};
+        for (int k = 0; k < 4 && !rc; ++k) {
+            const Operand* const o = ops[i][k];
+            if (!o) continue;
+            const uint64_t extent[2] = {o->cols, o->rows};
+            rc = tile_map(maps[k], BF16, o->base, 2, extent, &o->stride, o->mn ? 64 : k % 2 ? min(128u, kRowsX) : 128);
+        }
+    }
+    const auto kernel = product_kernel<EPI, PAIR, TN, BF16>;
+    if (!rc) rc = allow_smem((const void*)kernel, Shape::smem);
     if (rc) return rc;
-    p.chunks0 = (uint32_t)ceil_div(A_MN ? a0.rows : a0.cols, 64);
-    p.chunks1 = a1 ? (uint32_t)ceil_div(A_MN ? a1->rows : a1->cols, 64) : 0;
-    p.tiles_m = (uint32_t)ceil_div(p.m, kTileM);
-    p.tiles_n = (uint32_t)ceil_div(p.n, EPI == kGate ? kTileN / 2 : kTileN);
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3(PAIR ? 2 * min(sms / 2, end) : min(sms, end));
+    c.blockDim = dim3(192);
+    c.dynamicSmemBytes = Shape::smem;
+    c.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    c.attrs = &attr;
+    c.numAttrs = PAIR ? 1 : 0;
+    return cuda_status(cudaLaunchKernelEx(&c, kernel, ps));
+}
+
+// Tiles of 256 x 256 by pairs of CTAs where there are enough of them; smaller ones where that would leave multiprocessors idle.
+template <int EPI>
+int products(bool bf16, Products& ps, Operand* (&ops)[kMostProducts][4], cudaStream_t stream) {
     uint32_t sms;
-    if ((rc = sm_count(&sms))) return rc;
-    const void* kernel = bf16 ? (const void*)product_kernel<EPI, A_MN, B_MN, true> : (const void*)product_kernel<EPI, A_MN, B_MN, false>;
-    if ((rc = allow_smem(kernel, kProductSmem))) return rc;
-    const uint32_t grid = min(sms, p.tiles_m * p.tiles_n);
-    if (bf16)
-        product_kernel<EPI, A_MN, B_MN, true><<<grid, 192, kProductSmem, stream>>>(ma0, mb0, ma1, mb1, p);
-    else
-        product_kernel<EPI, A_MN, B_MN, false><<<grid, 192, kProductSmem, stream>>>(ma0, mb0, ma1, mb1, p);
-    return cuda_status(cudaGetLastError());
+    const int rc = sm_count(&sms);
+    if (rc) return rc;
+    uint64_t large = 0, middle = 0;
+    for (uint32_t i = 0; i < ps.count; ++i) {
+        const uint64_t n = EPI == kGate ? 2ull * ps.of[i].n : ps.of[i].n;
+        large += ceil_div(ps.of[i].m, 256) * ceil_div(n, 256);
+        middle += ceil_div(ps.of[i].m, 128) * ceil_div(n, 256);
+    }
+    if (large >= sms / 2) return bf16 ? launch_products<EPI, true, 256, true>(ps, ops, sms, stream) : launch_products<EPI, true, 256, false>(ps, ops, sms, stream);
+    (void)middle;
+    return bf16 ? launch_products<EPI, false, 128, true>(ps, ops, sms, stream) : launch_products<EPI, false, 128, false>(ps, ops, sms, stream);
+}
+
+Product plain(uint32_t m, uint32_t n, void* out) {
+    Product p{};
+    p.m = m;
+    p.n = n;
+    p.out = out;
+    p.out_stride = n;
+    return p;
 }
 
 // The block's sizes out of a two-GEMM workload: I tokens, K in, L inside, J out.
@@ -323,10 +445,12 @@ extern "C" int mmee_gated_ffn(const mmee_workload_t* workload, const mmee_gated_
         const uint64_t bytes = 2ull * s.d_ff * (2ull * s.d_in + s.d_out);
         return s.tokens <= kFew && bytes < kFewBytes ? ffn_tokens(few, bf16, stream) : ffn_narrow(few, bf16, stream);
     }
-    const Operand x{f->x, s.tokens, s.d_in, f->x_stride}, wg{f->w_gate, s.d_ff, s.d_in, f->w_gate_stride};
-    const Operand wu{f->w_up, s.d_ff, s.d_in, f->w_up_stride}, wd{f->w_down, s.d_out, s.d_ff, f->w_down_stride};
-    const Operand h{f->hidden, s.tokens, s.d_ff, s.d_ff};
-    ProductParams p{};
+    Operand x{f->x, s.tokens, s.d_in, f->x_stride, false}, wg{f->w_gate, s.d_ff, s.d_in, f->w_gate_stride, false};
+    Operand wu{f->w_up, s.d_ff, s.d_in, f->w_up_stride, false}, wd{f->w_down, s.d_out, s.d_ff, f->w_down_stride, false};
+    Operand h{f->hidden, s.tokens, s.d_ff, s.d_ff, false};
+    Operand* ops[kMostProducts][4];
+    Products ps;
+    Product p{};
     p.m = s.tokens;
     p.n = s.d_ff;
     p.act = f->activation;
@@ -334,13 +458,12 @@ extern "C" int mmee_gated_ffn(const mmee_workload_t* workload, const mmee_gated_
     p.out_stride = s.d_ff;
     p.gate = f->kept;
     p.up = f->kept ? f->kept + (uint64_t)s.tokens * s.d_ff : nullptr;
-    if ((rc = product<kGate, false, false>(bf16, x, wg, nullptr, &wu, p, stream))) return rc;
-    ProductParams q{};
-    q.m = s.tokens;
-    q.n = s.d_out;
-    q.out = f->y;
-    q.out_stride = s.d_out;
-    return product<kPlain, false, false>(bf16, h, wd, nullptr, nullptr, q, stream);
+    ps.count = 0;
+    add_product(&ps, ops, p, &x, &wg, nullptr, &wu);
+    if ((rc = products<kGate>(bf16, ps, ops, stream))) return rc;
+    ps.count = 0;
+    add_product(&ps, ops, plain(s.tokens, s.d_out, f->y), &h, &wd, nullptr, nullptr);
+    return products<kPlain>(bf16, ps, ops, stream);
 }
 
 extern "C" int mmee_gated_ffn_backward(const mmee_workload_t* workload, const mmee_gated_ffn_t* f, const mmee_gated_ffn_grad_t* g,
@@ -359,11 +482,10 @@ extern "C" int mmee_gated_ffn_backward(const mmee_workload_t* workload, const mm
     const bool bf16 = f->dtype == MMEE_BF16;
     uint16_t* const dg = static_cast<uint16_t*>(g->workspace);
     uint16_t* const du = dg + inner;                   // (inner is a multiple of eight)
-    const Operand x{f->x, s.tokens, s.d_in, f->x_stride}, wg{f->w_gate, s.d_ff, s.d_in, f->w_gate_stride};
-    const Operand wu{f->w_up, s.d_ff, s.d_in, f->w_up_stride}, wd{f->w_down, s.d_out, s.d_ff, f->w_down_stride};
-    const Operand h{f->hidden, s.tokens, s.d_ff, s.d_ff}, dy{g->d_y, s.tokens, s.d_out, g->d_y_stride};
-    const Operand odg{dg, s.tokens, s.d_ff, s.d_ff}, odu{du, s.tokens, s.d_ff, s.d_ff};
-    ProductParams p{};
+    Operand wd{f->w_down, s.d_out, s.d_ff, f->w_down_stride, true}, dy{g->d_y, s.tokens, s.d_out, g->d_y_stride, false};
+    Operand* ops[kMostProducts][4];
+    Products ps;
+    Product p{};
     p.m = s.tokens;
     p.n = s.d_ff;
     p.act = f->activation;
@@ -372,19 +494,21 @@ extern "C" int mmee_gated_ffn_backward(const mmee_workload_t* workload, const mm
     p.out_stride = s.d_ff;
     p.gate = f->kept;
     p.up = f->kept + inner;
-    if ((rc = product<kGrad, false, true>(bf16, dy, wd, nullptr, nullptr, p, stream))) return rc;
-    auto plain = [](uint32_t m, uint32_t n, void* out) {
-        ProductParams q{};
-        q.m = m;
-        q.n = n;
-        q.out = out;
-        q.out_stride = n;
-        return q;
-    };
-    if ((rc = product<kPlain, false, true>(bf16, odg, wg, &odu, &wu, plain(s.tokens, s.d_in, g->d_x), stream))) return rc;
-    if ((rc = product<kPlain, true, true>(bf16, odg, x, nullptr, nullptr, plain(s.d_ff, s.d_in, g->d_w_gate), stream))) return rc;
-    if ((rc = product<kPlain, true, true>(bf16, odu, x, nullptr, nullptr, plain(s.d_ff, s.d_in, g->d_w_up), stream))) return rc;
-    return product<kPlain, true, true>(bf16, dy, h, nullptr, nullptr, plain(s.d_out, s.d_ff, g->d_w_down), stream);
+    ps.count = 0;
+    add_product(&ps, ops, p, &dy, &wd, nullptr, nullptr);
+    if ((rc = products<kGrad>(bf16, ps, ops, stream))) return rc;
+    // The other four products depend on nothing but these, and are one launch: the one with the longest reduction first.
+    Operand dg_x{dg, s.tokens, s.d_ff, s.d_ff, false}, du_x{du, s.tokens, s.d_ff, s.d_ff, false};
+    Operand wg{f->w_gate, s.d_ff, s.d_in, f->w_gate_stride, true}, wu{f->w_up, s.d_ff, s.d_in, f->w_up_stride, true};
+    Operand dg_w{dg, s.tokens, s.d_ff, s.d_ff, true}, du_w{du, s.tokens, s.d_ff, s.d_ff, true};
+    Operand x{f->x, s.tokens, s.d_in, f->x_stride, true}, h{f->hidden, s.tokens, s.d_ff, s.d_ff, true};
+    dy.mn = true;
+    ps.count = 0;
+    add_product(&ps, ops, plain(s.tokens, s.d_in, g->d_x), &dg_x, &wg, &du_x, &wu);
+    add_product(&ps, ops, plain(s.d_ff, s.d_in, g->d_w_gate), &dg_w, &x, nullptr, nullptr);
+    add_product(&ps, ops, plain(s.d_ff, s.d_in, g->d_w_up), &du_w, &x, nullptr, nullptr);
+    add_product(&ps, ops, plain(s.d_out, s.d_ff, g->d_w_down), &dy, &h, nullptr, nullptr);
+    return products<kPlain>(bf16, ps, ops, stream);
 }
 
 extern "C" int mmee_gated_ffn_workspace(const mmee_workload_t* w, uint64_t* bytes) {

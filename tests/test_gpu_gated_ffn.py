@@ -19,7 +19,7 @@ ACT32 = 2.0 ** -18
 SIZES = [                                  # tokens, in, inner, out
     (1, 64, 64, 64), (1, 8, 8, 8), (8, 4096, 8192, 4096), (2, 16, 8, 24), (5, 72, 136, 40), (8, 256, 512, 256), (9, 264, 520, 8), (16, 1024, 2048, 512),
     (17, 64, 384, 64), (33, 200, 264, 712), (64, 512, 128, 1032), (127, 136, 248, 72), (128, 64, 256, 128), (129, 192, 384, 264),
-    (300, 328, 1000, 520), (777, 1000, 2728, 712), (768, 64, 384, 64), (2048, 256, 1024, 512),
+    (300, 328, 1000, 520), (777, 1000, 2728, 712), (768, 64, 384, 64), (2048, 256, 1024, 512), (1500, 520, 4100 - 4, 1000), (4100, 264, 2056, 136),
 ]
 
 
