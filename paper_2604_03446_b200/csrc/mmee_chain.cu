@@ -24,20 +24,21 @@ EncodeTiled encode_tiled() {
 
 }  // namespace
 
-int tile_map(CUtensorMap* map, bool bf16, const void* base, uint32_t rank, const uint64_t* extent, const int64_t* stride, uint32_t rows) {
+int tile_map(CUtensorMap* map, Values type, const void* base, uint32_t rank, const uint64_t* extent, const int64_t* stride, uint32_t rows) {
     const EncodeTiled encode = encode_tiled();
     if (!encode) return cuda_status(cudaErrorNotSupported);
+    const uint32_t size = type == Values::f32 ? 4 : 2;
     cuuint64_t dims[5], bytes[5];
     cuuint32_t box[5], step[5];
     for (uint32_t i = 0; i < rank; ++i) {
         dims[i] = extent[i];
-        box[i] = i == 0 ? 64 : i == 1 ? rows : 1;
+        box[i] = i == 0 ? 128 / size : i == 1 ? rows : 1;
         step[i] = 1;
     }
     // (a dimension of one entry may carry any stride: a legal one stands in)
-    for (uint32_t i = 0; i + 1 < rank; ++i) bytes[i] = extent[i + 1] == 1 ? 16 : (cuuint64_t)stride[i] * 2;
-    const CUresult r = encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank,
-                              const_cast<void*>(base), dims, bytes, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    for (uint32_t i = 0; i + 1 < rank; ++i) bytes[i] = extent[i + 1] == 1 ? 16 : (cuuint64_t)stride[i] * size;
+    const CUresult r = encode(map, type == Values::f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : type == Values::bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                              rank, const_cast<void*>(base), dims, bytes, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? MMEE_OK : MMEE_ERR_ARG;
 }

@@ -11,9 +11,13 @@ namespace mmee {
 
 int cuda_status(cudaError_t e);                // mmee_api.cu
 
-// Tensor map of a 16-bit tensor, innermost dimension contiguous, with 128-byte swizzle and boxes of 64 values by `rows` (by one
-// in further dimensions).  extent: rank entries, innermost first; stride: rank - 1 entries in elements.
-int tile_map(CUtensorMap* map, bool bf16, const void* base, uint32_t rank, const uint64_t* extent, const int64_t* stride, uint32_t rows);
+// Tensor map of a tensor, innermost dimension contiguous, with 128-byte swizzle and boxes of 128 bytes by `rows` (by one in
+// further dimensions).  extent: rank entries, innermost first; stride: rank - 1 entries in elements.
+enum class Values { f16, bf16, f32 };
+int tile_map(CUtensorMap* map, Values type, const void* base, uint32_t rank, const uint64_t* extent, const int64_t* stride, uint32_t rows);
+inline int tile_map(CUtensorMap* map, bool bf16, const void* base, uint32_t rank, const uint64_t* extent, const int64_t* stride, uint32_t rows) {
+    return tile_map(map, bf16 ? Values::bf16 : Values::f16, base, rank, extent, stride, rows);
+}
 
 // Streaming multiprocessors of the current device.
 int sm_count(uint32_t* out);

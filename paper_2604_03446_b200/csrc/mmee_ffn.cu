@@ -34,17 +34,24 @@ struct Product {
 constexpr uint32_t kMostProducts = 4;
 struct Products {
     CUtensorMap a0[kMostProducts], b0[kMostProducts], a1[kMostProducts], b1[kMostProducts];
+    CUtensorMap out[kMostProducts];
+    CUtensorMap out2, gate, up;        // kGate, kGrad: of the only product
     Product of[kMostProducts];
     uint32_t count;
 };
 
 // A tile: 128 rows to a CTA, PAIR: of two CTAs that share the columns' operand.
-template <bool PAIR, int TN>
+// Results leave through shared memory: each warp lays 32 rows of 128 bytes down and has the TMA store them, so that memory sees
+// whole lines (a thread has a row, its sixteen-byte stores would each be a line of their own, in the way of the operands as well:
+// of the training step of 4096 tokens, 4096-16384-4096, the gradient's kernel, which reads what was kept the same way, took 771 us).
+constexpr uint32_t kPart = 32 * kRowBytes;             // a warp's rows
+template <int EPI, bool PAIR, int TN>
 struct TileShape {
     static constexpr uint32_t kM = PAIR ? 256 : 128, kRowsB = PAIR ? TN / 2 : TN;      // rows of a tile; of B in a CTA
     static constexpr uint32_t kA = 128 * kRowBytes, kB = kRowsB * kRowBytes;
-    static constexpr uint32_t kStages = (200 * 1024) / (kA + kB);
-    static constexpr uint32_t smem = kStages * (kA + kB) + 1024;
+    // A warp's places: kPlain two of the product; kGate two of h, gate and up each; kGrad one of dg and du each, two of gate and up.
+    static constexpr uint32_t kParts = EPI == kPlain ? 2 : 6, kStages = (226 * 1024 - 4 * kParts * kPart) / (kA + kB);
+    static constexpr uint32_t smem = kStages * (kA + kB) + 4 * kParts * kPart + 1024;
 };
 
 constexpr uint32_t kGroupRows = 2048;  // result rows that are gone through together, so that their operands stay in L2
@@ -60,12 +67,12 @@ __device__ __forceinline__ void tile_of(const Product& p, uint32_t i, uint32_t* 
 
 template <int EPI, bool PAIR, int TN, bool BF16>
 __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__ Products ps) {
-    using Shape = TileShape<PAIR, TN>;
+    using Shape = TileShape<EPI, PAIR, TN>;
     constexpr uint32_t kStages = Shape::kStages, kStage = Shape::kA + Shape::kB;
     constexpr uint32_t kCols = EPI == kGate ? TN / 2 : TN;             // columns of the result in a tile
     constexpr uint32_t kRowsX = EPI == kGate && !PAIR ? TN / 2 : Shape::kRowsB;    // rows of B from one matrix in a CTA
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 5 + 8];
     __shared__ uint32_t tmem_base, gave_up;
     const uint32_t tiles = (smem_addr(raw) + 1023u) & ~1023u;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
@@ -76,6 +83,7 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
     auto acc_full = [&](uint32_t b) { return bar0 + 8 * (2 * kStages + b); };
     auto acc_empty = [&](uint32_t b) { return bar0 + 8 * (2 * kStages + 2 + b); };
     const uint32_t drained = bar0 + 8 * (2 * kStages + 4);
+    auto kept_full = [&](uint32_t w, uint32_t b) { return drained + 8 * (1 + 2 * w + b); };
     if (threadIdx.x == 0) {
         gave_up = 0;
         for (uint32_t s = 0; s < kStages; ++s) {
@@ -87,6 +95,8 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
             mbar_init(acc_empty(b), PAIR ? 8 : 4);     // an arrival of every warp that empties it
         }
         mbar_init(drained, 1);
+        for (uint32_t w = 0; w < 4; ++w)
+            for (uint32_t b = 0; b < 2; ++b) mbar_init(kept_full(w, b), 1);
         mbar_init_visible();
     }
     if (warp == 5) {
@@ -204,80 +214,129 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
             }
         }
     } else {                                           // results
-        uint32_t n = 0;
+        uint32_t n = 0, stores = 0, kept = 0;          // tiles, groups of stores, pieces of gate and up asked for
+        const uint32_t mine = tiles + kStages * kStage + warp * Shape::kParts * kPart;
+        auto part = [&](uint32_t i) { return mine + i * kPart; };
+        // Lays a row of 64 results down, two to a word.
+        auto lay = [&](uint32_t to, const uint32_t* v) {
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) store_shared16(swizzled(to, lane, j), v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        };
+        auto ready = [] {
+            fence_async_shared();
+            __syncwarp();
+        };
         for (uint32_t i = worker; i < n_tiles; i += workers, ++n) {
             const uint32_t b = n & 1;
             uint32_t at, tm, tn;
-            const Product& p = ps.of[product_of(i, &at)];
+            const uint32_t k = product_of(i, &at);
+            const Product& p = ps.of[k];
             tile_of<Shape::kM>(p, at, &tm, &tn);
-            if (!mbar_wait(acc_full(b), (n >> 1) & 1, lost)) break;
+            const uint32_t row0 = tm * Shape::kM + rank * 128 + warp * 32, col0 = tn * kCols;
+            const uint32_t cols = row0 < p.m ? min(kCols, p.n - col0) : 0;     // of this warp's rows, inside
+            auto ask_kept = [&](uint32_t c, uint32_t piece) {          // gate and up of 32 columns
+                if (lane == 0 && c < cols) {
+                    const uint32_t q = piece & 1, bar = kept_full(warp, q);
+                    mbar_expect(bar, 2 * kPart);
+                    tma_load_2d(part(2 + 2 * q), &ps.gate, bar, (int32_t)(col0 + c), (int32_t)row0);
+                    tma_load_2d(part(3 + 2 * q), &ps.up, bar, (int32_t)(col0 + c), (int32_t)row0);
+                }
+            };
+            if (EPI == kGrad) {
+                ask_kept(0, kept);
+                ask_kept(32, kept + 1);
+            }
+            if (!mbar_wait(acc_full(b), (n >> 1) & 1, lost)) {
+                if (EPI == kGrad && lane == 0)         // what is in flight lands before the CTA ends
+                    for (uint32_t c = 0; c < min(64u, cols); c += 32) mbar_wait(kept_full(warp, (kept + c / 32) & 1), ((kept + c / 32) >> 1) & 1, nullptr);
+                break;
+            }
             tcgen05_fence_after();
             const uint32_t acc = tmem + b * TN + ((warp * 32) << 16);
-            const uint32_t row = tm * Shape::kM + rank * 128 + warp * 32 + lane;
-            const bool in = row < p.m;
-            for (uint32_t c = 0; c < kCols; c += 32) {
-                const uint32_t col = tn * kCols + c;
-                uint32_t x[32], y[32];
-                tmem_load32(acc + c, x);
-                if (EPI == kGate) tmem_load32(acc + TN / 2 + c, y);
-                tmem_loaded32(x);
-                if (EPI == kGate) tmem_loaded32(y);
-                if (in && col < p.n) {
-                    uint32_t o[16], o2[16];
+#pragma unroll 1
+            for (uint32_t c = 0; c < kCols; c += 64) {
+                uint32_t o[32], o2[32];
+#pragma unroll
+                for (uint32_t half = 0; half < 2; ++half) {
+                    uint32_t x[32], y[32];
+                    const uint32_t d = c + 32 * half;
+                    tmem_load32(acc + d, x);
+                    if (EPI == kGate) tmem_load32(acc + TN / 2 + d, y);
+                    tmem_loaded32(x);
+                    if (EPI == kGate) tmem_loaded32(y);
                     if (EPI == kPlain) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) o[j] = pack2<BF16>(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
+                        for (int j = 0; j < 16; ++j) o[16 * half + j] = pack2<BF16>(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
                     } else if (EPI == kGate) {
-                        if (p.gate) {
-                            float4* const g = reinterpret_cast<float4*>(p.gate + (uint64_t)row * p.n + col);
-                            float4* const u = reinterpret_cast<float4*>(p.up + (uint64_t)row * p.n + col);
+                        if (p.gate && d < cols) {
+                            // (this half's places: the stores of the same half of the step before have been read)
+                            if (lane == 0) tma_store_read<1>();
+                            __syncwarp();
 #pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                if (col + 4 * j < p.n) {
-                                    g[j] = make_float4(__uint_as_float(x[4 * j]), __uint_as_float(x[4 * j + 1]), __uint_as_float(x[4 * j + 2]), __uint_as_float(x[4 * j + 3]));
-                                    u[j] = make_float4(__uint_as_float(y[4 * j]), __uint_as_float(y[4 * j + 1]), __uint_as_float(y[4 * j + 2]), __uint_as_float(y[4 * j + 3]));
-                                }
-                        }
-#pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            o[j] = pack2<BF16>(act_value(p.act, __uint_as_float(x[2 * j])) * __uint_as_float(y[2 * j]),
-                                               act_value(p.act, __uint_as_float(x[2 * j + 1])) * __uint_as_float(y[2 * j + 1]));
-                    } else {
-                        const float4* const g = reinterpret_cast<const float4*>(p.gate + (uint64_t)row * p.n + col);
-                        const float4* const u = reinterpret_cast<const float4*>(p.up + (uint64_t)row * p.n + col);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            if (col + 4 * j >= p.n) break;
-                            const float4 gv = g[j], uv = u[j];
-                            const float gg[4] = {gv.x, gv.y, gv.z, gv.w}, uu[4] = {uv.x, uv.y, uv.z, uv.w};
-                            float dg[4], du[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                float a, da;
-                                act_both(p.act, gg[e], &a, &da);
-                                const float dh = __uint_as_float(x[4 * j + e]);
-                                dg[e] = dh * uu[e] * da;
-                                du[e] = dh * a;
+                            for (uint32_t j = 0; j < 8; ++j) {
+                                store_shared16(swizzled(part(2 + 2 * half), lane, j), x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+                                store_shared16(swizzled(part(3 + 2 * half), lane, j), y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
                             }
-                            o[2 * j] = pack2<BF16>(dg[0], dg[1]);
-                            o[2 * j + 1] = pack2<BF16>(dg[2], dg[3]);
-                            o2[2 * j] = pack2<BF16>(du[0], du[1]);
-                            o2[2 * j + 1] = pack2<BF16>(du[2], du[3]);
+                            ready();
+                            if (lane == 0) {
+                                tma_store_2d(&ps.gate, part(2 + 2 * half), (int32_t)(col0 + d), (int32_t)row0);
+                                tma_store_2d(&ps.up, part(3 + 2 * half), (int32_t)(col0 + d), (int32_t)row0);
+                                if (half == 0) tma_store_commit();     // (the second half's go with h)
+                            }
                         }
-                    }
-                    // (rows are multiples of eight values long, so that sixteen bytes are inside or outside as one)
-                    uint4* const to = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + (int64_t)row * p.out_stride + col);
+                        with_act(p.act, [&](auto kind) {
+                            constexpr uint32_t kAct = decltype(kind)::value;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (col + 8 * j < p.n) to[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
-                    if (EPI == kGrad) {
-                        uint4* const to2 = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out2) + (int64_t)row * p.out_stride + col);
+                            for (int j = 0; j < 16; ++j)
+                                o[16 * half + j] = pack2<BF16>(act_value<kAct>(__uint_as_float(x[2 * j])) * __uint_as_float(y[2 * j]),
+                                                               act_value<kAct>(__uint_as_float(x[2 * j + 1])) * __uint_as_float(y[2 * j + 1]));
+                        });
+                    } else if (d < cols) {
+                        const uint32_t q = kept & 1;
+                        mbar_wait(kept_full(warp, q), (kept >> 1) & 1, lost);
+                        with_act(p.act, [&](auto kind) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (col + 8 * j < p.n) to2[j] = make_uint4(o2[4 * j], o2[4 * j + 1], o2[4 * j + 2], o2[4 * j + 3]);
+                            for (uint32_t j = 0; j < 8; ++j) {
+                                const float4 gv = load_shared16(swizzled(part(2 + 2 * q), lane, j)), uv = load_shared16(swizzled(part(3 + 2 * q), lane, j));
+                                const float gg[4] = {gv.x, gv.y, gv.z, gv.w}, uu[4] = {uv.x, uv.y, uv.z, uv.w};
+                                float dg[4], du[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    float a, da;
+                                    act_both<decltype(kind)::value>(gg[e], &a, &da);
+                                    const float dh = __uint_as_float(x[4 * j + e]);
+                                    dg[e] = dh * uu[e] * da;
+                                    du[e] = dh * a;
+                                }
+                                o[16 * half + 2 * j] = pack2<BF16>(dg[0], dg[1]);
+                                o[16 * half + 2 * j + 1] = pack2<BF16>(dg[2], dg[3]);
+                                o2[16 * half + 2 * j] = pack2<BF16>(du[0], du[1]);
+                                o2[16 * half + 2 * j + 1] = pack2<BF16>(du[2], du[3]);
+                            }
+                        });
+                        __syncwarp();                  // all have read these places: the next but one goes there
+                        ask_kept(d + 64, kept);
+                        ++kept;
                     }
                 }
+                if (c >= cols) continue;               // (the same for the whole warp)
+                const uint32_t to = EPI == kGrad ? part(0) : part(stores & 1);
+                if (lane == 0) {
+                    if (EPI == kGrad)
+                        tma_store_read<0>();
+                    else
+                        tma_store_read<1>();
+                }
                 __syncwarp();
+                lay(to, o);
+                if (EPI == kGrad) lay(part(1), o2);
+                ready();
+                if (lane == 0) {
+                    tma_store_2d(&ps.out[k], to, (int32_t)(col0 + c), (int32_t)row0);
+                    if (EPI == kGrad) tma_store_2d(&ps.out2, part(1), (int32_t)(col0 + c), (int32_t)row0);
+                    tma_store_commit();
+                }
+                ++stores;
             }
             tcgen05_fence_before();
             __syncwarp();
@@ -288,6 +347,7 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
                     mbar_arrive(acc_empty(b));
             }
         }
+        if (lane == 0) tma_store_read<0>();            // shared memory stays until it has been read
     }
     __syncwarp();
     tcgen05_fence_before();
@@ -335,7 +395,7 @@ void add_product(Products* ps, Operand* (&ops)[kMostProducts][4], Product p, Ope
 
 template <int EPI, bool PAIR, int TN, bool BF16>
 int launch_products(Products& ps, Operand* (&ops)[kMostProducts][4], uint32_t sms, cudaStream_t stream) {
-    using Shape = TileShape<PAIR, TN>;
+    using Shape = TileShape<EPI, PAIR, TN>;
     constexpr uint32_t kRowsX = EPI == kGate && !PAIR ? TN / 2 : Shape::kRowsB;
     uint32_t end = 0;
     int rc = MMEE_OK;
@@ -351,6 +411,12 @@ int launch_products(Products& ps, Operand* (&ops)[kMostProducts][4], uint32_t sm
             const uint64_t extent[2] = {o->cols, o->rows};
             rc = tile_map(maps[k], BF16, o->base, 2, extent, &o->stride, o->mn ? 64 : k % 2 ? min(128u, kRowsX) : 128);
         }
+        const uint64_t result[2] = {p.n, p.m};
+        if (!rc) rc = tile_map(&ps.out[i], BF16, p.out, 2, result, &p.out_stride, 32);
+        if (!rc && EPI == kGrad) rc = tile_map(&ps.out2, BF16, p.out2, 2, result, &p.out_stride, 32);
+        const int64_t n = p.n;
+        if (!rc && p.gate) rc = tile_map(&ps.gate, Values::f32, p.gate, 2, result, &n, 32);
+        if (!rc && p.gate) rc = tile_map(&ps.up, Values::f32, p.up, 2, result, &n, 32);
     }
     const auto kernel = product_kernel<EPI, PAIR, TN, BF16>;
     if (!rc) rc = allow_smem((const void*)kernel, Shape::smem);

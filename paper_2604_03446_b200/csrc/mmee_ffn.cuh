@@ -6,27 +6,52 @@
 
 namespace mmee {
 
-// Activation and its derivative.
-__device__ __forceinline__ float act_value(uint32_t act, float g) {
-    if (act == MMEE_ACT_RELU) return g < 0.f ? 0.f : g;
-    if (act == MMEE_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
-    const float s = __fdividef(1.f, 1.f + __expf(-g));
-    return act == MMEE_ACT_SIGMOID ? s : g * s;
-}
-
-__device__ __forceinline__ void act_both(uint32_t act, float g, float* a, float* da) {
-    if (act == MMEE_ACT_RELU) {
+// Activation and its derivative.  The kind is a constant where many values go through it: with a choice at every value, none starts
+// before the one before it is done (the gradient's kernel of 4096 tokens, 4096-16384-4096, took 575 us so).
+template <uint32_t ACT>
+__device__ __forceinline__ void act_both(float g, float* a, float* da) {
+    if (ACT == MMEE_ACT_RELU) {
         *a = g < 0.f ? 0.f : g;
         *da = g > 0.f ? 1.f : 0.f;
-    } else if (act == MMEE_ACT_GELU) {
+    } else if (ACT == MMEE_ACT_GELU) {
         const float cdf = 0.5f * (1.f + erff(g * 0.70710678118654752f));
         *a = g * cdf;
         *da = cdf + g * 0.39894228040143268f * __expf(-0.5f * g * g);
     } else {
         const float s = __fdividef(1.f, 1.f + __expf(-g));
-        *a = act == MMEE_ACT_SIGMOID ? s : g * s;
-        *da = act == MMEE_ACT_SIGMOID ? s * (1.f - s) : s * (1.f + g * (1.f - s));
+        *a = ACT == MMEE_ACT_SIGMOID ? s : g * s;
+        *da = ACT == MMEE_ACT_SIGMOID ? s * (1.f - s) : s * (1.f + g * (1.f - s));
     }
+}
+
+template <uint32_t ACT>
+__device__ __forceinline__ float act_value(float g) {
+    float a, da;
+    act_both<ACT>(g, &a, &da);
+    return a;
+}
+
+template <uint32_t V>
+struct Kind {
+    static constexpr uint32_t value = V;
+};
+
+template <typename F>
+__device__ __forceinline__ void with_act(uint32_t act, F f) {
+    if (act == MMEE_ACT_SILU)
+        f(Kind<MMEE_ACT_SILU>());
+    else if (act == MMEE_ACT_GELU)
+        f(Kind<MMEE_ACT_GELU>());
+    else if (act == MMEE_ACT_RELU)
+        f(Kind<MMEE_ACT_RELU>());
+    else
+        f(Kind<MMEE_ACT_SIGMOID>());
+}
+
+__device__ __forceinline__ float act_value(uint32_t act, float g) {
+    float a;
+    with_act(act, [&](auto kind) { a = act_value<decltype(kind)::value>(g); });
+    return a;
 }
 
 // The block for few tokens, which the weights' way from memory bounds.  Up to kNarrow tokens: mmee_ffn_narrow.cu; up to kFew

@@ -92,6 +92,17 @@ __device__ __forceinline__ void tma_load_4d(uint32_t to, const CUtensorMap* map,
                  : "memory");
 }
 
+// From shared memory; the thread's stores so far are a group after tma_store_commit.
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t from, int32_t x, int32_t y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(from), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// Waits until all of the thread's groups but the last `LEFT` have been read from shared memory.
+template <int LEFT>
+__device__ __forceinline__ void tma_store_read() {
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory");
+}
+
 // By a CTA of a pair that works on one tile: the bytes are counted at `bar`, which may be the other CTA's (pair_leader).
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t to, const CUtensorMap* map, uint32_t bar, int32_t x, int32_t y) {
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(to),
@@ -191,6 +202,19 @@ __device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t* r) {
 }
 
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Sixteen bytes of a swizzled row: the row's piece j lies at j xor (row mod 8).
+__device__ __forceinline__ uint32_t swizzled(uint32_t tile, uint32_t row, uint32_t piece) { return tile + row * kRowBytes + ((piece ^ (row & 7u)) << 4); }
+
+__device__ __forceinline__ void store_shared16(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+__device__ __forceinline__ float4 load_shared16(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
 
 // --- matrix instructions --------------------------------------------------------------------------------------------
 
