@@ -22,15 +22,21 @@ struct ForwardShape {
     static constexpr uint32_t smem(uint32_t tiles) { return tiles * kQ + kRing * (kQ + kV) + 1024; }
 };
 
+// A warpgroup to a query tile, then one warp each for the loads and the matrix instructions; with two query tiles two more that make
+// their warpgroup whole: it hands registers on, so that a row's 128 scores fit a thread (8 warps of 208 and 4 of 88 from 12 of 168).
+// With one, two CTAs share a multiprocessor: a thread holds half of the scores and reads the others twice.
+constexpr uint32_t forward_threads(uint32_t tiles) { return tiles == 2 ? 384 : 192; }
+
 template <int DK, int DV, int TILES, bool BF16>
-__global__ void __launch_bounds__(TILES * 128 + 64, 1)
+__global__ void __launch_bounds__(forward_threads(TILES), TILES == 2 ? 1 : 2)
 attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                  const AttentionParams p) {
     using Shape = ForwardShape<DK, DV>;
     constexpr uint32_t kRing = Shape::kRing, kLoad = TILES * 4, kMma = kLoad + 1;
+    constexpr int kHeld = TILES == 2 ? 128 : 64;       // scores of a row that stay in registers
     constexpr uint32_t kColumns = TILES * (128 + DV) <= 256 ? 256 : 512;
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t bars[TILES * 4 + 4 * kRing + 1];
+    __shared__ __align__(8) uint64_t bars[TILES * 5 + 4 * kRing + 1];
     __shared__ uint32_t tmem_base, gave_up;
 
     const uint32_t b = blockIdx.z / p.splits, split = blockIdx.z % p.splits, head = blockIdx.y;
@@ -45,13 +51,13 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     const uint32_t bar0 = smem_addr(bars);
     auto q_full = [&](uint32_t t) { return bar0 + 8 * t; };
     auto s_full = [&](uint32_t t) { return bar0 + 8 * (TILES + t); };
-    auto p_full = [&](uint32_t t) { return bar0 + 8 * (2 * TILES + t); };
-    auto o_full = [&](uint32_t t) { return bar0 + 8 * (3 * TILES + t); };
-    auto k_full = [&](uint32_t s) { return bar0 + 8 * (4 * TILES + s); };
-    auto k_empty = [&](uint32_t s) { return bar0 + 8 * (4 * TILES + kRing + s); };
-    auto v_full = [&](uint32_t s) { return bar0 + 8 * (4 * TILES + 2 * kRing + s); };
-    auto v_empty = [&](uint32_t s) { return bar0 + 8 * (4 * TILES + 3 * kRing + s); };
-    const uint32_t drained = bar0 + 8 * (4 * TILES + 4 * kRing);
+    auto o_full = [&](uint32_t t) { return bar0 + 8 * (2 * TILES + t); };
+    auto p_full = [&](uint32_t t, uint32_t h) { return bar0 + 8 * (3 * TILES + 2 * t + h); };
+    auto k_full = [&](uint32_t s) { return bar0 + 8 * (5 * TILES + s); };
+    auto k_empty = [&](uint32_t s) { return bar0 + 8 * (5 * TILES + kRing + s); };
+    auto v_full = [&](uint32_t s) { return bar0 + 8 * (5 * TILES + 2 * kRing + s); };
+    auto v_empty = [&](uint32_t s) { return bar0 + 8 * (5 * TILES + 3 * kRing + s); };
+    const uint32_t drained = bar0 + 8 * (5 * TILES + 4 * kRing);
     auto q_tile = [&](uint32_t t) { return base + t * Shape::kQ; };
     auto k_tile = [&](uint32_t s) { return base + TILES * Shape::kQ + s * Shape::kQ; };
     auto v_tile = [&](uint32_t s) { return base + (TILES + kRing) * Shape::kQ + s * Shape::kV; };
@@ -61,7 +67,8 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         for (uint32_t t = 0; t < TILES; ++t) {
             mbar_init(q_full(t), 1);
             mbar_init(s_full(t), 1);
-            mbar_init(p_full(t), 128);
+            mbar_init(p_full(t, 0), 4);
+            mbar_init(p_full(t, 1), 4);
             mbar_init(o_full(t), 1);
         }
         for (uint32_t s = 0; s < kRing; ++s) {
@@ -82,7 +89,9 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     auto s_col = [&](uint32_t t) { return tmem + t * 128; };
     auto o_col = [&](uint32_t t) { return tmem + TILES * 128 + t * DV; };
 
-    if (warp == kLoad) {
+    if (warp >= kLoad) {
+        if constexpr (TILES == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp == kLoad) {
         if (elect_one() && n) {
             const int32_t h = (int32_t)head, hk = (int32_t)(head / p.group), bb = (int32_t)b;
             uint32_t k_sent = 0, v_sent = 0;
@@ -120,11 +129,7 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         const uint32_t desc_o = mma_desc(BF16, kTile, (p.d_v + 15) / 16 * 16, false, true);
         const uint32_t steps_s = (p.d_qk + 15) / 16;
         auto scores = [&](uint32_t t, uint32_t s) {    // S_t = Q_t K^T
-            const uint64_t dq = tile_desc(q_tile(t), 16), dk = tile_desc(k_tile(s), 16);
-            for (uint32_t k = 0; k < steps_s; ++k) {
-                const uint64_t at = (uint64_t)(k / 4) * (kTile * kRowBytes >> 4) + (k % 4) * kStepK;
-                mma_ss(s_col(t), dq + at, dk + at, desc_s, k);
-            }
+            tile_product<DK>(s_col(t), q_tile(t), k_tile(s), desc_s, steps_s);
             mma_commit(s_full(t));
         };
         bool sound = n > 0;
@@ -147,11 +152,17 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             if (valid % 16) zero_rows(v_tile(s), DV / 64, valid, steps_o * 16);
             if (i + 1 < n && !(sound = mbar_wait(k_full(s1), ((i + 1) / kRing) & 1, lost))) break;
             for (uint32_t t = 0; t < tiles; ++t) {
-                if (!(sound = mbar_wait(p_full(t), i & 1, lost))) break;
-                tcgen05_fence_after();
+                // P V in two halves of 64 keys, the first while the second is still scores.
+                for (uint32_t h = 0; h < 2 && sound; ++h) {
+                    if (!(sound = mbar_wait(p_full(t, h), i & 1, lost))) break;
+                    tcgen05_fence_after();
+                    if (elect_one()) {
+                        turned_product<4, 32>(o_col(t), s_col(t) + 32 * h, v_tile(s) + h * 64 * kRowBytes, desc_o, max(steps_o, 4 * h) - 4 * h, i | h);
+                    }
+                    __syncwarp();
+                }
+                if (!sound) break;
                 if (elect_one()) {
-                    const uint64_t dv = tile_desc(v_tile(s), kTile * kRowBytes);
-                    for (uint32_t k = 0; k < steps_o; ++k) mma_ts(o_col(t), s_col(t) + 8 * k, dv + k * kStepMN, desc_o, i | k);
                     if (t + 1 == tiles) mma_commit(v_empty(s));
                     if (i + 1 < n) {
                         scores(t, s1);
@@ -163,23 +174,20 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                 __syncwarp();
             }
         }
-    } else if (warp / 4 < tiles) {
+    }
+    } else {
+        if constexpr (TILES == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        if (warp / 4 < tiles) {
         const uint32_t t = warp / 4, row = (warp % 4) * 32 + lane, lanes = ((warp % 4) * 32) << 16;
         const float sl2 = p.scale * kLog2e;
         float m = -INFINITY, l = 0.f;                  // reference and sum, in powers of two
         bool sound = true;
+        const uint32_t from_s = s_col(t) + lanes;
+#pragma unroll 1
         for (uint32_t i = 0; i < n; ++i) {
             if (!(sound = mbar_wait(s_full(t), i & 1, lost))) break;
             tcgen05_fence_after();
-            // The first 64 scores stay in registers; the others are read for the maximum and once more for their
-            // probabilities, while the tensor memory is idle (128 at once would spill).
             const int valid = (int)min(kTile, keys - (t0 + i) * kTile);
-            uint32_t x[64], y[32];
-            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            auto take_most = [&](const uint32_t* v) {
-#pragma unroll
-                for (int c = 0; c < 32; ++c) top[c & 3] = fmaxf(top[c & 3], __uint_as_float(v[c]));
-            };
             auto cut = [&](uint32_t* v, int from) {    // scores of keys behind the end
                 if (valid < from + 32) {
 #pragma unroll
@@ -187,24 +195,29 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                         if (from + c >= valid) v[c] = 0xff800000u;
                 }
             };
-            tmem_load32(s_col(t) + lanes + 96, y);
-            tmem_load32(s_col(t) + lanes + 64, x);
-            tmem_loaded32(y);
-            tmem_loaded32(x);
-            cut(y, 96);
-            take_most(y);
-            tmem_load32(s_col(t) + lanes, y);
-            cut(x, 64);
-            take_most(x);
-            tmem_load32(s_col(t) + lanes + 32, x + 32);
-            tmem_loaded32(y);
-            tmem_loaded32(x + 32);
+            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            auto take_most = [&](const uint32_t* v) {
 #pragma unroll
-            for (int c = 0; c < 32; ++c) x[c] = y[c];
-            cut(x, 0);
-            take_most(x);
-            cut(x + 32, 32);
-            take_most(x + 32);
+                for (int c = 0; c < 32; c += 2) top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+            };
+            uint32_t x[kHeld], y[32];
+#pragma unroll
+            for (int c = 0; c < kHeld; c += 32) tmem_load32(from_s + c, x + c);
+#pragma unroll
+            for (int c = 0; c < kHeld; c += 32) tmem_loaded32(x + c);
+#pragma unroll
+            for (int c = kHeld; c < 128; c += 32) {
+                tmem_load32(from_s + c, y);
+                tmem_loaded32(y);
+                cut(y, c);
+                take_most(y);
+            }
+            if (valid < (int)kTile) {
+#pragma unroll
+                for (int c = 0; c < kHeld; c += 32) cut(x + c, c);
+            }
+#pragma unroll
+            for (int c = 0; c < kHeld; c += 32) take_most(x + c);
             const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sl2;
             if (i == 0) {
                 m = most;
@@ -223,34 +236,37 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                     tmem_store16(o_col(t) + lanes + c, o);
                 }
             }
-            const float from = (m == -INFINITY ? 0.f : m) - kBias<BF16>;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-            auto turn = [&](const uint32_t* v, int at) {       // 32 scores into probabilities
+            const float from = kBias<BF16> - (m == -INFINITY ? 0.f : m);
+            const uint64_t scale2 = pair(sl2, sl2), from2 = pair(from, from);
+            uint64_t sum[2] = {0, 0};
+            auto turn = [&](const uint32_t* v, int c) {        // 32 scores into probabilities, over scores that have been read
                 uint32_t pk[16];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const float a = exp2_fast(fmaf(__uint_as_float(v[2 * j]), sl2, -from));
-                    const float e = exp2_fast(fmaf(__uint_as_float(v[2 * j + 1]), sl2, -from));
-                    sum[j & 3] += a + e;
-                    pk[j] = pack2<BF16>(a, e);
+                    float2 w = unpair(fma_pair(pair(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), scale2, from2));
+                    w.x = exp2_fast(w.x), w.y = exp2_fast(w.y);
+                    sum[j & 1] = add_pair(sum[j & 1], pair(w.x, w.y));
+                    pk[j] = pack2<BF16>(w.x, w.y);
                 }
-                tmem_store16(s_col(t) + lanes + at / 2, pk);
+                tmem_store16(from_s + c / 2, pk);
+                if (c == 32 || c == 96) {
+                    tmem_stored();
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_full(t, c / 64));
+                }
             };
-            // (the probabilities of columns 0 to 63 lie over the scores of 0 to 31: those are read by now)
-            turn(x, 0);
-            tmem_load32(s_col(t) + lanes + 64, y);
-            turn(x + 32, 32);
-            tmem_loaded32(y);
-            cut(y, 64);
-            tmem_load32(s_col(t) + lanes + 96, x);
-            turn(y, 64);
-            tmem_loaded32(x);
-            cut(x, 96);
-            turn(x, 96);
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            tmem_stored();
-            tcgen05_fence_before();
-            mbar_arrive(p_full(t));
+#pragma unroll
+            for (int c = 0; c < kHeld; c += 32) turn(x + c, c);
+#pragma unroll
+            for (int c = kHeld; c < 128; c += 32) {
+                tmem_load32(from_s + c, y);
+                tmem_loaded32(y);
+                cut(y, c);
+                turn(y, c);
+            }
+            const float2 sums = unpair(add_pair(sum[0], sum[1]));
+            l += sums.x + sums.y;
         }
         const uint32_t token = q0 + t * kTile + row;
         if (n && sound) sound = mbar_wait(o_full(t), 0, lost);
@@ -292,6 +308,7 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                 __syncwarp();
             }
         }
+    }
     }
     tcgen05_fence_before();
     __syncthreads();
@@ -353,7 +370,7 @@ int launch_forward(const Problem& x, cudaStream_t stream) {
     if (!rc) rc = allow_smem((const void*)attention_kernel<DK, DV, TILES, BF16>, smem);
     if (rc) return rc;
     const dim3 grid((uint32_t)ceil_div(x.p.seq_q, TILES * kTile), x.p.q_heads, x.p.batch * x.p.splits);
-    attention_kernel<DK, DV, TILES, BF16><<<grid, TILES * 128 + 64, smem, stream>>>(mq, mk, mv, x.p);
+    attention_kernel<DK, DV, TILES, BF16><<<grid, forward_threads(TILES), smem, stream>>>(mq, mk, mv, x.p);
     return cuda_status(cudaGetLastError());
 }
 

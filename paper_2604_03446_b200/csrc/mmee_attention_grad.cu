@@ -104,22 +104,6 @@ struct GradShape {
     static constexpr uint32_t smem = (1 + kRing) * (kQ + kV) + 1024;
 };
 
-// Products of two tiles in shared memory, both with the reduction along their rows.
-__device__ __forceinline__ void tile_product(uint32_t to, uint32_t a, uint32_t b, uint32_t desc, uint32_t steps) {
-    const uint64_t da = tile_desc(a, 16), db = tile_desc(b, 16);
-    for (uint32_t k = 0; k < steps; ++k) {
-        const uint64_t at = (uint64_t)(k / 4) * (kTile * kRowBytes >> 4) + (k % 4) * kStepK;
-        mma_ss(to, da + at, db + at, desc, k);
-    }
-}
-
-// Adds the product of a 128 x 128 operand in tensor memory (two halves of 64 columns, each packed into its first 32) and a tile
-// whose rows are the reduction.
-__device__ __forceinline__ void turned_product(uint32_t to, uint32_t a, uint32_t b, uint32_t desc, uint32_t steps, bool add) {
-    const uint64_t db = tile_desc(b, kTile * kRowBytes);
-    for (uint32_t k = 0; k < steps; ++k) mma_ts(to, a + (k / 4) * 64 + (k % 4) * 8, db + k * kStepMN, desc, add || k);
-}
-
 // --- dK and dV ------------------------------------------------------------------------------------------------------
 
 template <int DK, int DV, bool BF16>
@@ -202,9 +186,9 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         if (sound) {
             tcgen05_fence_after();
             if (elect_one()) {
-                tile_product(s_col, k_tile, q_tile(0), desc, steps_k);
+                tile_product<DK>(s_col, k_tile, q_tile(0), desc, steps_k);
                 mma_commit(s_full);
-                tile_product(dp_col, v_tile, o_tile(0), desc, steps_v);
+                tile_product<DV>(dp_col, v_tile, o_tile(0), desc, steps_v);
                 mma_commit(dp_full);
             }
             __syncwarp();
@@ -213,13 +197,13 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             const uint32_t s = i % kRing, s1 = (i + 1) % kRing;
             if (!(sound = mbar_wait(p_full, i & 1, lost))) break;
             tcgen05_fence_after();
-            if (elect_one()) turned_product(dv_col, s_col, o_tile(s), desc_dv, 8, i);
+            if (elect_one()) turned_product<8, 64>(dv_col, s_col, o_tile(s), desc_dv, 8, i);
             __syncwarp();
             if (i + 1 < n) {
                 if (!(sound = mbar_wait(full(s1), ((i + 1) / kRing) & 1, lost))) break;
                 tcgen05_fence_after();
                 if (elect_one()) {
-                    tile_product(s_col, k_tile, q_tile(s1), desc, steps_k);
+                    tile_product<DK>(s_col, k_tile, q_tile(s1), desc, steps_k);
                     mma_commit(s_full);
                 }
                 __syncwarp();
@@ -227,10 +211,10 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             if (!(sound = mbar_wait(ds_full, i & 1, lost))) break;
             tcgen05_fence_after();
             if (elect_one()) {
-                turned_product(dk_col, dp_col, q_tile(s), desc_dk, 8, i);
+                turned_product<8, 64>(dk_col, dp_col, q_tile(s), desc_dk, 8, i);
                 mma_commit(empty(s));
                 if (i + 1 < n) {
-                    tile_product(dp_col, v_tile, o_tile(s1), desc, steps_v);
+                    tile_product<DV>(dp_col, v_tile, o_tile(s1), desc, steps_v);
                     mma_commit(dp_full);
                 } else {
                     mma_commit(sums_full);
@@ -448,9 +432,9 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
         bool sound = n > 0 && mbar_wait(q_full, 0, lost) && landed(0);
         if (sound) {
             if (elect_one()) {
-                tile_product(s_col(0), q_tile, k_tile(0), desc, steps_k);
+                tile_product<DK>(s_col(0), q_tile, k_tile(0), desc, steps_k);
                 mma_commit(s_full(0));
-                tile_product(dp_col, o_tile, v_tile(0), desc, steps_v);
+                tile_product<DV>(dp_col, o_tile, v_tile(0), desc, steps_v);
                 mma_commit(dp_full);
             }
             __syncwarp();
@@ -460,7 +444,7 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             if (i + 1 < n) {
                 if (!(sound = landed(i + 1))) break;
                 if (elect_one()) {
-                    tile_product(s_col((i + 1) & 1), q_tile, k_tile(s1), desc, steps_k);
+                    tile_product<DK>(s_col((i + 1) & 1), q_tile, k_tile(s1), desc, steps_k);
                     mma_commit(s_full((i + 1) & 1));
                 }
                 __syncwarp();
@@ -469,10 +453,10 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             tcgen05_fence_after();
             if (elect_one()) {
                 if (i + 1 < n) {
-                    tile_product(dp_col, o_tile, v_tile(s1), desc, steps_v);
+                    tile_product<DV>(dp_col, o_tile, v_tile(s1), desc, steps_v);
                     mma_commit(dp_full);
                 }
-                turned_product(dq_col, s_col(i & 1), k_tile(s), desc_dq, (min(kTile, keys - i * kTile) + 15) / 16, i);
+                turned_product<8, 64>(dq_col, s_col(i & 1), k_tile(s), desc_dq, (min(kTile, keys - i * kTile) + 15) / 16, i);
                 mma_commit(empty(s));
                 if (i + 1 == n) mma_commit(sums_full);
             }

@@ -54,24 +54,20 @@ __device__ __forceinline__ uint64_t global_ns() {
 
 constexpr uint64_t kWaitNs = 4000000000ull;    // no wait of a sound launch comes near this
 
-static __device__ __noinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up) {
-    const uint64_t begin = global_ns();
-    while (!mbar_try(bar, parity)) {
-        if (gave_up && *gave_up) return false;
-        if (global_ns() - begin > kWaitNs) {
+// Waits until the barrier's phase of this parity is over.  False: the wait ran out, here or in another role of the CTA
+// (`gave_up`, one word of shared memory); the role then leaves its loop.  With gave_up = nullptr: a wait of its own.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up) {
+    uint64_t end = 0;
+    for (uint32_t tries = 1; !mbar_try(bar, parity); ++tries) {
+        if (tries % 256) continue;                     // (a look at the clock would delay what waits)
+        const uint64_t now = global_ns();
+        if (!end) end = now + kWaitNs;
+        if ((gave_up && *gave_up) || now > end) {
             if (gave_up) *gave_up = 1;
             return false;
         }
     }
     return true;
-}
-
-// Waits until the barrier's phase of this parity is over.  False: the wait ran out, here or in another role of the CTA
-// (`gave_up`, one word of shared memory); the role then leaves its loop.  With gave_up = nullptr: a wait of its own.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up) {
-    for (int i = 0; i < 64; ++i)
-        if (mbar_try(bar, parity)) return true;
-    return mbar_wait_long(bar, parity, gave_up);
 }
 
 // --- TMA ------------------------------------------------------------------------------------------------------------
@@ -268,6 +264,33 @@ __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// Two 32-bit values in one register pair.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.ftz.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 
 template <bool BF16>
