@@ -82,11 +82,18 @@ __global__ void __launch_bounds__(256) grad_rows_kernel(const GradParams p) {
             }
         }
     }
-    if (!BF16) {
+    if (!BF16) {                                       // (one atomic a block and value: their number is what they cost)
+        __shared__ float largest[2][8];
         for (int i = 0; i < 2; ++i) {
             float m = most[i];
             for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-            if ((threadIdx.x & 31u) == 0) atomicMax(p.most + i, __float_as_uint(m));
+            if ((threadIdx.x & 31u) == 0) largest[i][threadIdx.x >> 5] = m;
+        }
+        __syncthreads();
+        if (threadIdx.x < 2) {
+            float m = 0.f;
+            for (int w = 0; w < 8; ++w) m = fmaxf(m, largest[threadIdx.x][w]);
+            atomicMax(p.most + threadIdx.x, __float_as_uint(m));
         }
     }
 }
@@ -100,8 +107,19 @@ __device__ __forceinline__ float row_log(const GradParams& p, uint64_t at, bool 
 
 template <int DK, int DV>
 struct GradShape {
-    static constexpr uint32_t kQ = (DK / 64) * kTile * kRowBytes, kV = (DV / 64) * kTile * kRowBytes, kRing = 2;
-    static constexpr uint32_t smem = (1 + kRing) * (kQ + kV) + 1024;
+    // Tiles that stay, and rings of those that stream: the operand of d_qk values serves the first and the last product of a turn, so
+    // that three are needed for its load to be hidden (with two, and one barrier for both operands, every turn waited for its loads:
+    // dQ of 2 x 32 heads, 2048 queries, 4096 keys, d 128: 478 us).
+    static constexpr uint32_t kQ = (DK / 64) * kTile * kRowBytes, kV = (DV / 64) * kTile * kRowBytes, kRingQ = 3, kRingV = 2;
+    static constexpr uint32_t tiles = (1 + kRingQ) * kQ + (1 + kRingV) * kV, smem = tiles + 1024;
+    // The kernel for keys has 2 KB beside: the largest tiles leave no whole KB for their alignment, but less is needed behind that.
+    struct Beside {
+        float row_stats[kRingV][2][kTile];             // with each query tile: log2 of the sums, delta; both negative
+        uint64_t bars[2 * kRingQ + 2 * kRingV + 7];
+        uint32_t tmem_base, gave_up;
+    };
+    static constexpr uint32_t kMost = 227 * 1024, smem_keys = smem + sizeof(Beside) < kMost ? smem : kMost - sizeof(Beside);
+    static_assert(round_up(sizeof(Beside), 1024) + tiles <= kMost);
 };
 
 // --- dK and dV ------------------------------------------------------------------------------------------------------
@@ -111,11 +129,11 @@ __global__ void __launch_bounds__(320, 1)
 grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                  const __grid_constant__ CUtensorMap mo, const GradParams p) {
     using Shape = GradShape<DK, DV>;
-    constexpr uint32_t kRing = Shape::kRing;
+    constexpr uint32_t kRingQ = Shape::kRingQ, kRingV = Shape::kRingV;
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(16) float row_stats[2][2][kTile];         // [turn][lse, delta]
-    __shared__ __align__(8) uint64_t bars[2 * kRing + 7];
-    __shared__ uint32_t tmem_base, gave_up;
+    __shared__ __align__(16) typename Shape::Beside beside;
+    auto& row_stats = beside.row_stats;
+    auto& gave_up = beside.gave_up;
 
     const AttentionParams& a = p.a;
     const uint32_t b = blockIdx.z, head = blockIdx.y, k0 = blockIdx.x * kTile;
@@ -125,64 +143,84 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
 
     const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
     const uint32_t k_tile = base, v_tile = base + Shape::kQ;
-    auto q_tile = [&](uint32_t s) { return base + (1 + s) * (Shape::kQ + Shape::kV); };
-    auto o_tile = [&](uint32_t s) { return q_tile(s) + Shape::kQ; };
-    const uint32_t bar0 = smem_addr(bars);
-    auto full = [&](uint32_t s) { return bar0 + 8 * s; };
-    auto empty = [&](uint32_t s) { return bar0 + 8 * (kRing + s); };
-    const uint32_t kv_full = bar0 + 8 * 2 * kRing, s_full = kv_full + 8, dp_full = kv_full + 16, p_full = kv_full + 24, ds_full = kv_full + 32,
+    auto q_tile = [&](uint32_t i) { return base + Shape::kV + (1 + i % kRingQ) * Shape::kQ; };
+    auto o_tile = [&](uint32_t i) { return base + (1 + kRingQ) * Shape::kQ + (1 + i % kRingV) * Shape::kV; };
+    const uint32_t bar0 = smem_addr(beside.bars);
+    auto q_full = [&](uint32_t i) { return bar0 + 8 * (i % kRingQ); };
+    auto q_empty = [&](uint32_t i) { return bar0 + 8 * (kRingQ + i % kRingQ); };
+    auto o_full = [&](uint32_t i) { return bar0 + 8 * (2 * kRingQ + i % kRingV); };
+    auto o_empty = [&](uint32_t i) { return bar0 + 8 * (2 * kRingQ + kRingV + i % kRingV); };
+    auto q_turn = [](uint32_t i) { return (i / kRingQ) & 1; };
+    auto o_turn = [](uint32_t i) { return (i / kRingV) & 1; };
+    const uint32_t kv_full = bar0 + 8 * (2 * kRingQ + 2 * kRingV), s_full = kv_full + 8, dp_full = kv_full + 16, p_full = kv_full + 24, ds_full = kv_full + 32,
                    sums_full = kv_full + 40, drained = kv_full + 48;
     if (threadIdx.x == 0) {
         gave_up = 0;
-        for (uint32_t s = 0; s < kRing; ++s) {
-            mbar_init(full(s), 1);
-            mbar_init(empty(s), 1);
-        }
+        for (uint32_t i = 0; i < 2 * kRingQ + 2 * kRingV; ++i) mbar_init(bar0 + 8 * i, 1);
         mbar_init(kv_full, 1);
         mbar_init(s_full, 1);
         mbar_init(dp_full, 1);
-        mbar_init(p_full, 256);
-        mbar_init(ds_full, 256);
+        mbar_init(p_full, 8);                          // (an arrival of every warp)
+        mbar_init(ds_full, 8);
         mbar_init(sums_full, 1);
         mbar_init(drained, 1);
         mbar_init_visible();
     }
-    if (warp == 9) tmem_alloc(&tmem_base, 512);
+    if (warp == 9) tmem_alloc(&beside.tmem_base, 512);
     tcgen05_fence_before();
     __syncthreads();
     tcgen05_fence_after();
-    const uint32_t tmem = tmem_base, s_col = tmem, dp_col = tmem + 128, dv_col = tmem + 256, dk_col = dv_col + DV;
+    const uint32_t tmem = beside.tmem_base, s_col = tmem, dp_col = tmem + 128, dv_col = tmem + 256, dk_col = dv_col + DV;
     volatile uint32_t* const lost = &gave_up;
 
     if (warp == 8) {
-        if (elect_one() && n) {
-            const int32_t bb = (int32_t)b, hk = (int32_t)head;
+        const int32_t bb = (int32_t)b, hk = (int32_t)head;
+        if (lane == 0 && n) {
             mbar_expect(kv_full, Shape::kQ + Shape::kV);
             for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(k_tile + j * kTile * kRowBytes, &mk, kv_full, 64 * j, (int32_t)k0, hk, bb);
             for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(v_tile + j * kTile * kRowBytes, &mv, kv_full, 64 * j, (int32_t)k0, hk, bb);
-            uint32_t sent = 0;
-            bool sound = true;
-            for (uint32_t i = 0; i < n; ++i) {
-                const uint32_t s = i % kRing;
-                if (!(sound = mbar_wait(empty(s), ((i / kRing) & 1) ^ 1, lost))) break;
-                const int32_t h = (int32_t)(head * a.group + i / tiles_q), row = (int32_t)(i % tiles_q * kTile);
-                mbar_expect(full(s), Shape::kQ + Shape::kV);
-                for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(q_tile(s) + j * kTile * kRowBytes, &mq, full(s), 64 * j, row, h, bb);
-                for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(o_tile(s) + j * kTile * kRowBytes, &mo, full(s), 64 * j, row, h, bb);
-                ++sent;
+        }
+        uint32_t q_sent = 0, o_sent = 0;
+        bool sound = true;
+        for (uint32_t i = 0; i < n; ++i) {
+            const uint32_t s = i % kRingV, h = head * a.group + i / tiles_q, row = i % tiles_q * kTile;
+            const uint64_t at = ((uint64_t)b * a.q_heads + h) * a.seq_q + row + 4 * lane;
+            float logs[4], deltas[4];
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                const bool in = row + 4 * lane + j < a.seq_q;
+                logs[j] = kPShift<BF16> - row_log(p, at + j, in);
+                deltas[j] = in ? -p.delta[at + j] : 0.f;
             }
-            if (!sound) {                              // what is in flight lands before the CTA ends
-                mbar_wait(kv_full, 0, nullptr);
-                for (uint32_t s = 0; s < kRing; ++s)
-                    if (sent > s) mbar_wait(full(s), ((sent - 1 - s) / kRing) & 1, nullptr);
+            if (!(sound = mbar_wait(q_empty(i), q_turn(i) ^ 1, lost))) break;
+            if (lane == 0) {
+                mbar_expect(q_full(i), Shape::kQ);
+                for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(q_tile(i) + j * kTile * kRowBytes, &mq, q_full(i), 64 * j, (int32_t)row, (int32_t)h, bb);
             }
+            ++q_sent;
+            if (!(sound = mbar_wait(o_empty(i), o_turn(i) ^ 1, lost))) break;
+            *reinterpret_cast<float4*>(&row_stats[s][0][4 * lane]) = make_float4(logs[0], logs[1], logs[2], logs[3]);
+            *reinterpret_cast<float4*>(&row_stats[s][1][4 * lane]) = make_float4(deltas[0], deltas[1], deltas[2], deltas[3]);
+            __syncwarp();
+            if (lane == 0) {
+                mbar_expect(o_full(i), Shape::kV);
+                for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(o_tile(i) + j * kTile * kRowBytes, &mo, o_full(i), 64 * j, (int32_t)row, (int32_t)h, bb);
+            }
+            ++o_sent;
+        }
+        if (!sound) {                                  // what is in flight lands before the CTA ends
+            mbar_wait(kv_full, 0, nullptr);
+            for (uint32_t s = 1; s <= kRingQ; ++s)
+                if (q_sent >= s) mbar_wait(q_full(q_sent - s), q_turn(q_sent - s), nullptr);
+            for (uint32_t s = 1; s <= kRingV; ++s)
+                if (o_sent >= s) mbar_wait(o_full(o_sent - s), o_turn(o_sent - s), nullptr);
         }
         __syncwarp();
     } else if (warp == 9) {
         constexpr uint32_t desc = mma_desc(BF16, kTile, kTile, false, false);
         const uint32_t steps_k = (a.d_qk + 15) / 16, steps_v = (a.d_v + 15) / 16;
         const uint32_t desc_dv = mma_desc(BF16, kTile, 16 * steps_v, false, true), desc_dk = mma_desc(BF16, kTile, 16 * steps_k, false, true);
-        bool sound = n > 0 && mbar_wait(kv_full, 0, lost) && mbar_wait(full(0), 0, lost);
+        bool sound = n > 0 && mbar_wait(kv_full, 0, lost) && mbar_wait(q_full(0), 0, lost) && mbar_wait(o_full(0), 0, lost);
         if (sound) {
             tcgen05_fence_after();
             if (elect_one()) {
@@ -194,16 +232,18 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             __syncwarp();
         }
         for (uint32_t i = 0; i < n && sound; ++i) {
-            const uint32_t s = i % kRing, s1 = (i + 1) % kRing;
+            const bool more = i + 1 < n;
             if (!(sound = mbar_wait(p_full, i & 1, lost))) break;
             tcgen05_fence_after();
-            if (elect_one()) turned_product<8, 64>(dv_col, s_col, o_tile(s), desc_dv, 8, i);
+            if (elect_one()) {
+                turned_product<8, 64>(dv_col, s_col, o_tile(i), desc_dv, 8, i);
+            }
             __syncwarp();
-            if (i + 1 < n) {
-                if (!(sound = mbar_wait(full(s1), ((i + 1) / kRing) & 1, lost))) break;
+            if (more) {
+                if (!(sound = mbar_wait(q_full(i + 1), q_turn(i + 1), lost))) break;
                 tcgen05_fence_after();
                 if (elect_one()) {
-                    tile_product<DK>(s_col, k_tile, q_tile(s1), desc, steps_k);
+                    tile_product<DK>(s_col, k_tile, q_tile(i + 1), desc, steps_k);
                     mma_commit(s_full);
                 }
                 __syncwarp();
@@ -211,98 +251,96 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             if (!(sound = mbar_wait(ds_full, i & 1, lost))) break;
             tcgen05_fence_after();
             if (elect_one()) {
-                turned_product<8, 64>(dk_col, dp_col, q_tile(s), desc_dk, 8, i);
-                mma_commit(empty(s));
-                if (i + 1 < n) {
-                    tile_product<DV>(dp_col, v_tile, o_tile(s1), desc, steps_v);
-                    mma_commit(dp_full);
-                } else {
-                    mma_commit(sums_full);
-                }
+                turned_product<8, 64>(dk_col, dp_col, q_tile(i), desc_dk, 8, i);
+                mma_commit(q_empty(i));
+                mma_commit(o_empty(i));                // (with the rows' numbers, which dS needs)
+                if (!more) mma_commit(sums_full);
             }
             __syncwarp();
+            if (more) {
+                if (!(sound = mbar_wait(o_full(i + 1), o_turn(i + 1), lost))) break;
+                tcgen05_fence_after();
+                if (elect_one()) {
+                    tile_product<DV>(dp_col, v_tile, o_tile(i + 1), desc, steps_v);
+                    mma_commit(dp_full);
+                }
+                __syncwarp();
+            }
         }
     } else {
         const uint32_t half = warp / 4, row = (warp % 4) * 32 + lane, lanes = ((warp % 4) * 32) << 16;
         const float sl2 = a.scale * kLog2e;
         const int shift = n ? ds_shift<BF16>(p) : 0;
         const float ds_scale = exp2f((float)shift - kPShift<BF16>);
-        const bool valid = k0 + row < keys;
-        auto stats_of = [&](uint32_t i, float* l, float* d) {
-            const uint32_t h = head * a.group + i / tiles_q, token = i % tiles_q * kTile + threadIdx.x;
-            const uint64_t at = ((uint64_t)b * a.q_heads + h) * a.seq_q + token;
-            const bool in = token < a.seq_q;
-            *l = row_log(p, at, in) - kPShift<BF16>;
-            *d = in ? p.delta[at] : 0.f;
+        const bool valid = k0 + row < keys, whole = k0 + kTile <= keys;
+        const uint64_t scale2 = pair(sl2, sl2), ds_scale2 = pair(ds_scale, ds_scale);
+        const uint32_t s_at = s_col + lanes + 64 * half, dp_at = dp_col + lanes + 64 * half;
+        auto hand_over = [&](uint32_t bar) {
+            tmem_stored();
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
         };
-        float next_l = 0.f, next_d = 0.f;
-        if (n && threadIdx.x < kTile) {
-            stats_of(0, &next_l, &next_d);
-            row_stats[0][0][threadIdx.x] = next_l;
-            row_stats[0][1][threadIdx.x] = next_d;
-        }
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        bool sound = true;
-        for (uint32_t i = 0; i < n; ++i) {
-            if (i + 1 < n && threadIdx.x < kTile) stats_of(i + 1, &next_l, &next_d);
-            const float* const logs = &row_stats[i & 1][0][64 * half];
-            const float* const deltas = &row_stats[i & 1][1][64 * half];
-            float pr[64];
-            if (!(sound = mbar_wait(s_full, i & 1, lost))) break;
-            tcgen05_fence_after();
+        // (keys behind the end: their rows of P and dS are nothing, whatever K and V hold there)
+        auto only_valid = [&](uint32_t* pk) {
+            if (!whole && !valid) {
 #pragma unroll
-            for (int c = 0; c < 64; c += 32) {
-                uint32_t x[32], pk[16];
-                tmem_load32(s_col + lanes + 64 * half + c, x);
-                tmem_loaded32(x);
+                for (int j = 0; j < 16; ++j) pk[j] = 0;
+            }
+        };
+        bool sound = true;
+#pragma unroll 1
+        for (uint32_t i = 0; i < n; ++i) {
+            const uint32_t s = i % kRingV;
+            const float* const logs = &row_stats[s][0][64 * half];
+            const float* const deltas = &row_stats[s][1][64 * half];
+            uint32_t x[64], pk[16];
+            uint64_t pr[32];
+            if (!(sound = mbar_wait(o_full(i), o_turn(i), lost)) || !(sound = mbar_wait(s_full, i & 1, lost))) break;
+            tcgen05_fence_after();
+            tmem_load32(s_at, x);
+            tmem_load32(s_at + 32, x + 32);
+            tmem_loaded32(x);
+            tmem_loaded32(x + 32);
+#pragma unroll
+            for (int c = 0; c < 64; c += 32) {         // P over scores that have been read
 #pragma unroll
                 for (int j = 0; j < 32; j += 4) {
                     const float4 l = *reinterpret_cast<const float4*>(logs + c + j);
-                    const float ls[4] = {l.x, l.y, l.z, l.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float v = exp2_fast(fmaf(__uint_as_float(x[j + e]), sl2, -ls[e]));
-                        pr[c + j + e] = valid && ls[e] != INFINITY ? v : 0.f;
-                    }
-                    pk[j / 2] = pack2<BF16>(pr[c + j], pr[c + j + 1]);
-                    pk[j / 2 + 1] = pack2<BF16>(pr[c + j + 2], pr[c + j + 3]);
+                    const float2 a0 = unpair(fma_pair(pair(__uint_as_float(x[c + j]), __uint_as_float(x[c + j + 1])), scale2, pair(l.x, l.y)));
+                    const float2 a1 = unpair(fma_pair(pair(__uint_as_float(x[c + j + 2]), __uint_as_float(x[c + j + 3])), scale2, pair(l.z, l.w)));
+                    const float w[4] = {exp2_fast(a0.x), exp2_fast(a0.y), exp2_fast(a1.x), exp2_fast(a1.y)};
+                    pr[(c + j) / 2] = pair(w[0], w[1]);
+                    pr[(c + j) / 2 + 1] = pair(w[2], w[3]);
+                    pk[j / 2] = pack2<BF16>(w[0], w[1]);
+                    pk[j / 2 + 1] = pack2<BF16>(w[2], w[3]);
                 }
-                // (32 columns of P over the first 32 of this half's 64 of S: what each store covers has been read)
-                tmem_store16(s_col + lanes + 64 * half + c / 2, pk);
+                only_valid(pk);
+                tmem_store16(s_at + c / 2, pk);
             }
-            tmem_stored();
-            tcgen05_fence_before();
-            mbar_arrive(p_full);
+            hand_over(p_full);
             if (!(sound = mbar_wait(dp_full, i & 1, lost))) break;
             tcgen05_fence_after();
+            tmem_load32(dp_at, x);
+            tmem_load32(dp_at + 32, x + 32);
+            tmem_loaded32(x);
+            tmem_loaded32(x + 32);
 #pragma unroll
             for (int c = 0; c < 64; c += 32) {
-                uint32_t x[32], pk[16];
-                tmem_load32(dp_col + lanes + 64 * half + c, x);
-                tmem_loaded32(x);
 #pragma unroll
                 for (int j = 0; j < 32; j += 4) {
                     const float4 d = *reinterpret_cast<const float4*>(deltas + c + j);
-                    const float ds[4] = {d.x, d.y, d.z, d.w};
-                    float v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        v[e] = pr[c + j + e] * (__uint_as_float(x[j + e]) - ds[e]) * ds_scale;
-                        if (!valid) v[e] = 0.f;
-                    }
-                    pk[j / 2] = pack2<BF16>(v[0], v[1]);
-                    pk[j / 2 + 1] = pack2<BF16>(v[2], v[3]);
+                    uint64_t v0 = mul_pair(pr[(c + j) / 2], add_pair(pair(__uint_as_float(x[c + j]), __uint_as_float(x[c + j + 1])), pair(d.x, d.y)));
+                    uint64_t v1 = mul_pair(pr[(c + j) / 2 + 1], add_pair(pair(__uint_as_float(x[c + j + 2]), __uint_as_float(x[c + j + 3])), pair(d.z, d.w)));
+                    if (!BF16) v0 = mul_pair(v0, ds_scale2), v1 = mul_pair(v1, ds_scale2);
+                    const float2 w0 = unpair(v0), w1 = unpair(v1);
+                    pk[j / 2] = pack2<BF16>(w0.x, w0.y);
+                    pk[j / 2 + 1] = pack2<BF16>(w1.x, w1.y);
                 }
-                tmem_store16(dp_col + lanes + 64 * half + c / 2, pk);
+                only_valid(pk);
+                tmem_store16(dp_at + c / 2, pk);
             }
-            tmem_stored();
-            tcgen05_fence_before();
-            mbar_arrive(ds_full);
-            if (i + 1 < n && threadIdx.x < kTile) {
-                row_stats[(i + 1) & 1][0][threadIdx.x] = next_l;
-                row_stats[(i + 1) & 1][1][threadIdx.x] = next_d;
-            }
-            asm volatile("bar.sync 1, 256;" ::: "memory");
+            hand_over(ds_full);
         }
         if (n && sound) sound = mbar_wait(sums_full, 0, lost);
         tcgen05_fence_after();
@@ -352,9 +390,9 @@ __global__ void __launch_bounds__(320, 1)
 grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                     const __grid_constant__ CUtensorMap mo, const GradParams p) {
     using Shape = GradShape<DK, DV>;
-    constexpr uint32_t kRing = Shape::kRing;
+    constexpr uint32_t kRingK = Shape::kRingQ, kRingV = Shape::kRingV;
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t bars[2 * kRing + 7];
+    __shared__ __align__(8) uint64_t bars[2 * kRingK + 2 * kRingV + 7];
     __shared__ uint32_t tmem_base, gave_up;
 
     const AttentionParams& a = p.a;
@@ -364,24 +402,25 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
 
     const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
     const uint32_t q_tile = base, o_tile = base + Shape::kQ;
-    auto k_tile = [&](uint32_t s) { return base + (1 + s) * (Shape::kQ + Shape::kV); };
-    auto v_tile = [&](uint32_t s) { return k_tile(s) + Shape::kQ; };
+    auto k_tile = [&](uint32_t i) { return base + Shape::kV + (1 + i % kRingK) * Shape::kQ; };
+    auto v_tile = [&](uint32_t i) { return base + (1 + kRingK) * Shape::kQ + (1 + i % kRingV) * Shape::kV; };
     const uint32_t bar0 = smem_addr(bars);
-    auto full = [&](uint32_t s) { return bar0 + 8 * s; };
-    auto empty = [&](uint32_t s) { return bar0 + 8 * (kRing + s); };
-    const uint32_t q_full = bar0 + 8 * 2 * kRing, dp_full = q_full + 24, ds_full = q_full + 32, sums_full = q_full + 40, drained = q_full + 48;
+    auto k_full = [&](uint32_t i) { return bar0 + 8 * (i % kRingK); };
+    auto k_empty = [&](uint32_t i) { return bar0 + 8 * (kRingK + i % kRingK); };
+    auto v_full = [&](uint32_t i) { return bar0 + 8 * (2 * kRingK + i % kRingV); };
+    auto v_empty = [&](uint32_t i) { return bar0 + 8 * (2 * kRingK + kRingV + i % kRingV); };
+    auto k_turn = [](uint32_t i) { return (i / kRingK) & 1; };
+    auto v_turn = [](uint32_t i) { return (i / kRingV) & 1; };
+    const uint32_t q_full = bar0 + 8 * (2 * kRingK + 2 * kRingV), dp_full = q_full + 24, ds_full = q_full + 32, sums_full = q_full + 40, drained = q_full + 48;
     auto s_full = [&](uint32_t t) { return q_full + 8 + 8 * t; };
     if (threadIdx.x == 0) {
         gave_up = 0;
-        for (uint32_t s = 0; s < kRing; ++s) {
-            mbar_init(full(s), 1);
-            mbar_init(empty(s), 1);
-        }
+        for (uint32_t i = 0; i < 2 * kRingK + 2 * kRingV; ++i) mbar_init(bar0 + 8 * i, 1);
         mbar_init(q_full, 1);
         mbar_init(s_full(0), 1);
         mbar_init(s_full(1), 1);
         mbar_init(dp_full, 1);
-        mbar_init(ds_full, 256);
+        mbar_init(ds_full, 8);                         // (an arrival of every warp)
         mbar_init(sums_full, 1);
         mbar_init(drained, 1);
         mbar_init_visible();
@@ -400,20 +439,24 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             mbar_expect(q_full, Shape::kQ + Shape::kV);
             for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(q_tile + j * kTile * kRowBytes, &mq, q_full, 64 * j, (int32_t)q0, h, bb);
             for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(o_tile + j * kTile * kRowBytes, &mo, q_full, 64 * j, (int32_t)q0, h, bb);
-            uint32_t sent = 0;
+            uint32_t k_sent = 0, v_sent = 0;
             bool sound = true;
             for (uint32_t i = 0; i < n; ++i) {
-                const uint32_t s = i % kRing;
-                if (!(sound = mbar_wait(empty(s), ((i / kRing) & 1) ^ 1, lost))) break;
-                mbar_expect(full(s), Shape::kQ + Shape::kV);
-                for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(k_tile(s) + j * kTile * kRowBytes, &mk, full(s), 64 * j, (int32_t)(i * kTile), hk, bb);
-                for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(v_tile(s) + j * kTile * kRowBytes, &mv, full(s), 64 * j, (int32_t)(i * kTile), hk, bb);
-                ++sent;
+                if (!(sound = mbar_wait(k_empty(i), k_turn(i) ^ 1, lost))) break;
+                mbar_expect(k_full(i), Shape::kQ);
+                for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(k_tile(i) + j * kTile * kRowBytes, &mk, k_full(i), 64 * j, (int32_t)(i * kTile), hk, bb);
+                ++k_sent;
+                if (!(sound = mbar_wait(v_empty(i), v_turn(i) ^ 1, lost))) break;
+                mbar_expect(v_full(i), Shape::kV);
+                for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(v_tile(i) + j * kTile * kRowBytes, &mv, v_full(i), 64 * j, (int32_t)(i * kTile), hk, bb);
+                ++v_sent;
             }
             if (!sound) {                              // what is in flight lands before the CTA ends
                 mbar_wait(q_full, 0, nullptr);
-                for (uint32_t s = 0; s < kRing; ++s)
-                    if (sent > s) mbar_wait(full(s), ((sent - 1 - s) / kRing) & 1, nullptr);
+                for (uint32_t s = 1; s <= kRingK; ++s)
+                    if (k_sent >= s) mbar_wait(k_full(k_sent - s), k_turn(k_sent - s), nullptr);
+                for (uint32_t s = 1; s <= kRingV; ++s)
+                    if (v_sent >= s) mbar_wait(v_full(v_sent - s), v_turn(v_sent - s), nullptr);
             }
         }
         __syncwarp();
@@ -421,12 +464,23 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
         constexpr uint32_t desc = mma_desc(BF16, kTile, kTile, false, false);
         const uint32_t steps_k = (a.d_qk + 15) / 16, steps_v = (a.d_v + 15) / 16;
         const uint32_t desc_dq = mma_desc(BF16, kTile, 16 * steps_k, false, true);
-        // Tile i has landed; keys behind the end become zeros (in dS K they meet zeros).
+        // Tile i of K has landed; keys behind the end become zeros (in dS K they meet zeros).
         auto landed = [&](uint32_t i) {
-            if (!mbar_wait(full(i % kRing), (i / kRing) & 1, lost)) return false;
+            if (!mbar_wait(k_full(i), k_turn(i), lost)) return false;
             const uint32_t left = keys - i * kTile;
-            if (left < kTile && left % 16) zero_rows(k_tile(i % kRing), DK / 64, left, (left + 15) / 16 * 16);
+            if (left < kTile && left % 16) zero_rows(k_tile(i), DK / 64, left, (left + 15) / 16 * 16);
             tcgen05_fence_after();
+            return true;
+        };
+        auto gradient_of_p = [&](uint32_t i) {            // dP of tile i
+            if (!mbar_wait(v_full(i), v_turn(i), lost)) return false;
+            tcgen05_fence_after();
+            if (elect_one()) {
+                tile_product<DV>(dp_col, o_tile, v_tile(i), desc, steps_v);
+                mma_commit(dp_full);
+                mma_commit(v_empty(i));
+            }
+            __syncwarp();
             return true;
         };
         bool sound = n > 0 && mbar_wait(q_full, 0, lost) && landed(0);
@@ -434,30 +488,25 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             if (elect_one()) {
                 tile_product<DK>(s_col(0), q_tile, k_tile(0), desc, steps_k);
                 mma_commit(s_full(0));
-                tile_product<DV>(dp_col, o_tile, v_tile(0), desc, steps_v);
-                mma_commit(dp_full);
             }
             __syncwarp();
+            sound = gradient_of_p(0);
         }
         for (uint32_t i = 0; i < n && sound; ++i) {
-            const uint32_t s = i % kRing, s1 = (i + 1) % kRing;
             if (i + 1 < n) {
                 if (!(sound = landed(i + 1))) break;
                 if (elect_one()) {
-                    tile_product<DK>(s_col((i + 1) & 1), q_tile, k_tile(s1), desc, steps_k);
+                    tile_product<DK>(s_col((i + 1) & 1), q_tile, k_tile(i + 1), desc, steps_k);
                     mma_commit(s_full((i + 1) & 1));
                 }
                 __syncwarp();
             }
             if (!(sound = mbar_wait(ds_full, i & 1, lost))) break;
             tcgen05_fence_after();
+            if (i + 1 < n && !(sound = gradient_of_p(i + 1))) break;
             if (elect_one()) {
-                if (i + 1 < n) {
-                    tile_product<DV>(dp_col, o_tile, v_tile(s1), desc, steps_v);
-                    mma_commit(dp_full);
-                }
-                turned_product<8, 64>(dq_col, s_col(i & 1), k_tile(s), desc_dq, (min(kTile, keys - i * kTile) + 15) / 16, i);
-                mma_commit(empty(s));
+                turned_product<8, 64>(dq_col, s_col(i & 1), k_tile(i), desc_dq, (min(kTile, keys - i * kTile) + 15) / 16, i);
+                mma_commit(k_empty(i));
                 if (i + 1 == n) mma_commit(sums_full);
             }
             __syncwarp();
@@ -468,43 +517,47 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
         const int shift = n ? ds_shift<BF16>(p) : 0;
         const uint64_t at = ((uint64_t)b * a.q_heads + head) * a.seq_q + token;
         const bool in = token < a.seq_q;
-        // dS = 2^shift exp2(S sl2 - log) (dP - delta): the power goes into the exponent.
-        const float log = row_log(p, at, in), from = log - (float)shift, delta = in ? p.delta[at] : 0.f;
-        const bool counts = log != INFINITY;
+        // dS = 2^shift exp2(S sl2 - log) (dP - delta): the power goes into the exponent.  Rows that count nothing: exp2(-infinity).
+        const float from = (float)shift - row_log(p, at, in), delta = in ? -p.delta[at] : 0.f;
+        const uint64_t scale2 = pair(sl2, sl2), from2 = pair(from, from), delta2 = pair(delta, delta);
         bool sound = true;
+#pragma unroll 1
         for (uint32_t i = 0; i < n; ++i) {
-            const int valid = counts ? (int)min(kTile, keys - i * kTile) - 64 * (int)half : 0;      // columns of this half that count
-            float pr[64];
+            const int valid = (int)(keys - i * kTile) - 64 * (int)half;        // columns of this half that count
+            const uint32_t s = s_col(i & 1) + lanes + 64 * half;
+            uint32_t x[64];
+            uint64_t pr[32];
             if (!(sound = mbar_wait(s_full(i & 1), (i >> 1) & 1, lost))) break;
             tcgen05_fence_after();
-            const uint32_t s = s_col(i & 1) + lanes + 64 * half;
-            uint32_t x[32];
+            tmem_load32(s, x);
+            tmem_load32(s + 32, x + 32);
+            tmem_loaded32(x);
+            tmem_loaded32(x + 32);
 #pragma unroll
-            for (int c = 0; c < 64; c += 32) {
-                tmem_load32(s + c, x);
-                tmem_loaded32(x);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) pr[c + j] = exp2_fast(fmaf(__uint_as_float(x[j]), sl2, -from));
+            for (int j = 0; j < 32; ++j) {
+                const float2 w = unpair(fma_pair(pair(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), scale2, from2));
+                pr[j] = pair(exp2_fast(w.x), exp2_fast(w.y));
             }
             if (!(sound = mbar_wait(dp_full, i & 1, lost))) break;
             tcgen05_fence_after();
+            tmem_load32(dp_col + lanes + 64 * half, x);
+            tmem_load32(dp_col + lanes + 64 * half + 32, x + 32);
+            tmem_loaded32(x);
+            tmem_loaded32(x + 32);
 #pragma unroll
-            for (int c = 0; c < 64; c += 32) {
-                uint32_t pk[16];
-                tmem_load32(dp_col + lanes + 64 * half + c, x);
-                tmem_loaded32(x);
-#pragma unroll
-                for (int j = 0; j < 32; j += 2) {
-                    float v0 = pr[c + j] * (__uint_as_float(x[j]) - delta), v1 = pr[c + j + 1] * (__uint_as_float(x[j + 1]) - delta);
-                    if (c + j >= valid) v0 = 0.f;
-                    if (c + j + 1 >= valid) v1 = 0.f;
-                    pk[j / 2] = pack2<BF16>(v0, v1);
-                }
-                tmem_store16(s + c / 2, pk);
+            for (int j = 0; j < 32; ++j) {
+                const float2 w = unpair(mul_pair(pr[j], add_pair(pair(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), delta2)));
+                x[j] = pack2<BF16>(w.x, w.y);
             }
+            if (valid < 64) {                          // keys behind the end: nothing, whatever K and V hold there
+#pragma unroll
+                for (int j = 0; j < 32; ++j) x[j] = 2 * j >= valid ? 0u : 2 * j + 1 >= valid ? x[j] & 0xffffu : x[j];
+            }
+            tmem_store32(s, x);
             tmem_stored();
             tcgen05_fence_before();
-            mbar_arrive(ds_full);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ds_full);
         }
         if (n && sound) sound = mbar_wait(sums_full, 0, lost);
         tcgen05_fence_after();
@@ -552,8 +605,8 @@ int launch_grads(const Problem& x, const View& d_o, const GradParams& p, cudaStr
     if (!rc) rc = view_map(&mk, BF16, a.batch, x.k);
     if (!rc) rc = view_map(&mv, BF16, a.batch, x.v);
     if (!rc) rc = view_map(&mo, BF16, a.batch, d_o);
-    constexpr uint32_t smem = GradShape<DK, DV>::smem;
-    if (!rc) rc = allow_smem((const void*)grad_keys_kernel<DK, DV, BF16>, smem);
+    constexpr uint32_t smem = GradShape<DK, DV>::smem, smem_keys = GradShape<DK, DV>::smem_keys;
+    if (!rc) rc = allow_smem((const void*)grad_keys_kernel<DK, DV, BF16>, smem_keys);
     if (!rc) rc = allow_smem((const void*)grad_queries_kernel<DK, DV, BF16>, smem);
     if (rc) return rc;
     if (!BF16 && (rc = cuda_status(cudaMemsetAsync(p.most, 0, 8, stream)))) return rc;
@@ -561,7 +614,7 @@ int launch_grads(const Problem& x, const View& d_o, const GradParams& p, cudaStr
     uint32_t sms;
     if ((rc = sm_count(&sms))) return rc;
     grad_rows_kernel<BF16><<<(uint32_t)min(ceil_div(rows, 16), (uint64_t)sms * 8), 256, 0, stream>>>(p);
-    grad_keys_kernel<DK, DV, BF16><<<dim3((uint32_t)ceil_div(a.seq_kv, kTile), p.kv_heads, a.batch), 320, smem, stream>>>(mq, mk, mv, mo, p);
+    grad_keys_kernel<DK, DV, BF16><<<dim3((uint32_t)ceil_div(a.seq_kv, kTile), p.kv_heads, a.batch), 320, smem_keys, stream>>>(mq, mk, mv, mo, p);
     grad_queries_kernel<DK, DV, BF16><<<dim3((uint32_t)ceil_div(a.seq_q, kTile), a.q_heads, a.batch), 320, smem, stream>>>(mq, mk, mv, mo, p);
     return cuda_status(cudaGetLastError());
 }

@@ -26,8 +26,8 @@ int sm_count(uint32_t* out);
 int allow_smem(const void* kernel, uint32_t bytes);
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
-inline uint64_t round_up(uint64_t a, uint64_t b) { return ceil_div(a, b) * b; }
+constexpr uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+constexpr uint64_t round_up(uint64_t a, uint64_t b) { return ceil_div(a, b) * b; }
 
 // The words that kernels set when a wait ran out, read and cleared (one for each file with such kernels).
 int attention_gave_up(uint32_t* word);
