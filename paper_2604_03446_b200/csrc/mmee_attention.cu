@@ -86,6 +86,7 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     tcgen05_fence_after();
     const uint32_t tmem = tmem_base;
     volatile uint32_t* const lost = &gave_up;
+    asm volatile("griddepcontrol.launch_dependents;");        // (the joining kernel's launch, where there is one)
     auto s_col = [&](uint32_t t) { return tmem + t * 128; };
     auto o_col = [&](uint32_t t) { return tmem + TILES * 128 + t * DV; };
 
@@ -326,25 +327,27 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     }
 }
 
-// Joins the parts of the keys: a warp per query row.  Every row's parts are added in the same order.
+// Joins the parts of the keys (32 at most): a warp per query row, a lane's part each for the weights.  Every row's parts are added
+// in the same order.
 template <bool BF16>
 __global__ void __launch_bounds__(128) attention_join_kernel(const AttentionParams p) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint64_t rows = (uint64_t)p.batch * p.q_heads * p.seq_q;
     const uint64_t at = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     const uint32_t lane = threadIdx.x & 31u;
     if (at >= rows) return;
-    float top = -INFINITY;
-    for (uint32_t s = lane; s < p.splits; s += 32) top = fmaxf(top, p.part_lse[s * rows + at]);
+    const float part = lane < p.splits ? p.part_lse[lane * rows + at] : -INFINITY;
+    float top = part;
     for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    const float from = top == -INFINITY ? 0.f : top;
+    const float from = top == -INFINITY ? 0.f : top, weight = exp2f(part - from);
+    const float* const from_o = p.part_o + at * p.d_v + 4 * lane;
     float v[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
+#pragma unroll 4
     for (uint32_t s = 0; s < p.splits; ++s) {
-        const float part = p.part_lse[s * rows + at];
-        if (part == -INFINITY) continue;               // no valid key: its values were not written
-        const float w = exp2f(part - from);
+        const float w = __shfl_sync(0xffffffffu, weight, (int)s);
         sum += w;
-        if (4 * lane < p.d_v) {
-            const float4 o = *reinterpret_cast<const float4*>(p.part_o + (s * rows + at) * p.d_v + 4 * lane);
+        if (w != 0.f && 4 * lane < p.d_v) {            // (w = 0: no valid key, its values may not have been written)
+            const float4 o = *reinterpret_cast<const float4*>(from_o + s * rows * p.d_v);
             v[0] += w * o.x, v[1] += w * o.y, v[2] += w * o.z, v[3] += w * o.w;
         }
     }
@@ -374,9 +377,22 @@ int launch_forward(const Problem& x, cudaStream_t stream) {
     return cuda_status(cudaGetLastError());
 }
 
+// Two query tiles a CTA, or one, of which two share a multiprocessor if the widths allow it: the former where both take as many
+// turns of the multiprocessors, as its tiles share the loads of the keys.
+template <int DK, int DV>
+bool single_tiles(const AttentionParams& p, uint32_t sms) {
+    if (p.seq_q <= kTile) return true;
+    if (DK + DV > 128) return false;
+    const uint64_t heads = (uint64_t)p.q_heads * p.batch * p.splits;
+    return ceil_div(ceil_div(p.seq_q, kTile) * heads, 2 * sms) < ceil_div(ceil_div(p.seq_q, 2 * kTile) * heads, sms);
+}
+
 template <int DK, int DV>
 int forward_typed(const Problem& x, cudaStream_t stream) {
-    if (x.p.seq_q <= kTile) return x.bf16 ? launch_forward<DK, DV, 1, true>(x, stream) : launch_forward<DK, DV, 1, false>(x, stream);
+    uint32_t sms;
+    const int rc = sm_count(&sms);
+    if (rc) return rc;
+    if (single_tiles<DK, DV>(x.p, sms)) return x.bf16 ? launch_forward<DK, DV, 1, true>(x, stream) : launch_forward<DK, DV, 1, false>(x, stream);
     return x.bf16 ? launch_forward<DK, DV, 2, true>(x, stream) : launch_forward<DK, DV, 2, false>(x, stream);
 }
 
@@ -456,11 +472,16 @@ extern "C" int mmee_attention(const mmee_workload_t* workload, const mmee_attent
     if (x.p.splits > 1) {
         const uint64_t rows = (uint64_t)x.p.batch * x.p.q_heads * x.p.seq_q;
         const uint32_t grid = (uint32_t)ceil_div(rows, 4);
-        if (x.bf16)
-            attention_join_kernel<true><<<grid, 128, 0, stream>>>(x.p);
-        else
-            attention_join_kernel<false><<<grid, 128, 0, stream>>>(x.p);
-        rc = cuda_status(cudaGetLastError());
+        cudaLaunchAttribute early;
+        early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        early.val.programmaticStreamSerializationAllowed = 1;
+        cudaLaunchConfig_t c{};
+        c.gridDim = dim3(grid);
+        c.blockDim = dim3(128);
+        c.stream = stream;
+        c.attrs = &early;
+        c.numAttrs = 1;
+        rc = cuda_status(x.bf16 ? cudaLaunchKernelEx(&c, attention_join_kernel<true>, x.p) : cudaLaunchKernelEx(&c, attention_join_kernel<false>, x.p));
     }
     return rc;
 }

@@ -42,45 +42,49 @@ __device__ __forceinline__ int ds_shift(const GradParams& p) {
 }
 
 // delta of every query row, half a warp to a row; in fp16 also the largest sizes in dO and in V's valid rows (their order
-// does not matter).
+// does not matter).  A block takes 64 tokens of a head.
+constexpr uint32_t kRowsOfBlock = 64;
 template <bool BF16>
 __global__ void __launch_bounds__(256) grad_rows_kernel(const GradParams p) {
+    asm volatile("griddepcontrol.launch_dependents;");
     const AttentionParams& a = p.a;
-    const uint64_t rows = (uint64_t)a.batch * a.q_heads * a.seq_q, keys = BF16 ? 0 : (uint64_t)a.batch * p.kv_heads * a.seq_kv;
-    const uint32_t lane = threadIdx.x & 15u;
+    const uint32_t lane = threadIdx.x & 15u, head = blockIdx.y, b = blockIdx.z, t0 = blockIdx.x * kRowsOfBlock + (threadIdx.x >> 4);
+    const uint16_t* const d_o = static_cast<const uint16_t*>(p.d_o) + (int64_t)b * p.dos.batch + (int64_t)head * p.dos.head + 8 * lane;
+    const uint16_t* const o = static_cast<const uint16_t*>(a.o) + (int64_t)b * a.os.batch + (int64_t)head * a.os.head + 8 * lane;
+    const uint16_t* const v = static_cast<const uint16_t*>(p.v) + (int64_t)b * p.vs.batch + (int64_t)head * p.vs.head + 8 * lane;
+    const uint32_t keys = BF16 || head >= p.kv_heads ? 0 : valid_keys(a.kv_len, b, a.seq_kv);
+    const bool in = 8 * lane < a.d_v;
     float most[2] = {0.f, 0.f};
-    for (uint64_t r = ((uint64_t)blockIdx.x * 256 + threadIdx.x) >> 4; r < rows + keys; r += (uint64_t)gridDim.x * 16) {
-        if (r < rows) {
-            const uint32_t token = (uint32_t)(r % a.seq_q), head = (uint32_t)(r / a.seq_q % a.q_heads);
-            const int64_t b = (int64_t)(r / ((uint64_t)a.seq_q * a.q_heads));
-            float sum = 0.f;
-            if (8 * lane < a.d_v) {
-                const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.d_o) + b * p.dos.batch + (int64_t)token * p.dos.token + (int64_t)head * p.dos.head + 8 * lane);
-                const uint4 y = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.o) + b * a.os.batch + (int64_t)token * a.os.token + (int64_t)head * a.os.head + 8 * lane);
-                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+    uint4 x[kRowsOfBlock / 16], y[kRowsOfBlock / 16], z[kRowsOfBlock / 16];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 f = unpack2<BF16>(xs[j]), g = unpack2<BF16>(ys[j]);
-                    sum += f.x * g.x + f.y * g.y;
-                    if (!BF16) most[0] = fmaxf(most[0], fmaxf(fabsf(f.x), fabsf(f.y)));
-                }
-            }
-            for (int d = 8; d; d >>= 1) sum += __shfl_xor_sync(0xffffu << (threadIdx.x & 16u), sum, d);
-            if (lane == 0) p.delta[r] = sum;
-        } else {
-            const uint64_t k = r - rows;
-            const uint32_t token = (uint32_t)(k % a.seq_kv), head = (uint32_t)(k / a.seq_kv % p.kv_heads);
-            const uint32_t b = (uint32_t)(k / ((uint64_t)a.seq_kv * p.kv_heads));
-            if (token < valid_keys(a.kv_len, b, a.seq_kv) && 8 * lane < a.d_v) {
-                const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.v) + (int64_t)b * p.vs.batch + (int64_t)token * p.vs.token + (int64_t)head * p.vs.head + 8 * lane);
-                const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+    for (uint32_t i = 0; i < kRowsOfBlock / 16; ++i) {
+        const uint32_t token = t0 + 16 * i;
+        const uint4 none = make_uint4(0, 0, 0, 0);
+        x[i] = in && token < a.seq_q ? *reinterpret_cast<const uint4*>(d_o + (int64_t)token * p.dos.token) : none;
+        y[i] = in && token < a.seq_q ? *reinterpret_cast<const uint4*>(o + (int64_t)token * a.os.token) : none;
+        if (!BF16) z[i] = in && token < keys ? *reinterpret_cast<const uint4*>(v + (int64_t)token * p.vs.token) : none;
+    }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 f = unpack2<BF16>(xs[j]);
-                    most[1] = fmaxf(most[1], fmaxf(fabsf(f.x), fabsf(f.y)));
-                }
+    for (uint32_t i = 0; i < kRowsOfBlock / 16; ++i) {
+        const uint32_t token = t0 + 16 * i;
+        const uint32_t xs[4] = {x[i].x, x[i].y, x[i].z, x[i].w}, ys[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 f = unpack2<BF16>(xs[j]), g = unpack2<BF16>(ys[j]);
+            sum += f.x * g.x + f.y * g.y;
+            if (!BF16) most[0] = fmaxf(most[0], fmaxf(fabsf(f.x), fabsf(f.y)));
+        }
+        if (!BF16) {
+            const uint32_t zs[4] = {z[i].x, z[i].y, z[i].z, z[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = unpack2<BF16>(zs[j]);
+                most[1] = fmaxf(most[1], fmaxf(fabsf(f.x), fabsf(f.y)));
             }
         }
+        for (int d = 8; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == 0 && token < a.seq_q) p.delta[((uint64_t)b * a.q_heads + head) * a.seq_q + token] = sum;
     }
     if (!BF16) {                                       // (one atomic a block and value: their number is what they cost)
         __shared__ float largest[2][8];
@@ -172,6 +176,9 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     tcgen05_fence_after();
     const uint32_t tmem = beside.tmem_base, s_col = tmem, dp_col = tmem + 128, dv_col = tmem + 256, dk_col = dv_col + DV;
     volatile uint32_t* const lost = &gave_up;
+    // The rows' kernel is done from here on.  The kernel of dQ, which needs it too, may start where this one leaves room.
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
 
     if (warp == 8) {
         const int32_t bb = (int32_t)b, hk = (int32_t)head;
@@ -579,6 +586,8 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             }
         }
     }
+    // (it was launched beside the kernel of dK and dV, and ends after it: what follows in the stream needs both)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     tcgen05_fence_before();
     __syncthreads();
     if (warp == 9) {
@@ -610,13 +619,23 @@ int launch_grads(const Problem& x, const View& d_o, const GradParams& p, cudaStr
     if (!rc) rc = allow_smem((const void*)grad_queries_kernel<DK, DV, BF16>, smem);
     if (rc) return rc;
     if (!BF16 && (rc = cuda_status(cudaMemsetAsync(p.most, 0, 8, stream)))) return rc;
-    const uint64_t rows = (uint64_t)a.batch * a.q_heads * a.seq_q + (BF16 ? 0 : (uint64_t)a.batch * p.kv_heads * a.seq_kv);
-    uint32_t sms;
-    if ((rc = sm_count(&sms))) return rc;
-    grad_rows_kernel<BF16><<<(uint32_t)min(ceil_div(rows, 16), (uint64_t)sms * 8), 256, 0, stream>>>(p);
-    grad_keys_kernel<DK, DV, BF16><<<dim3((uint32_t)ceil_div(a.seq_kv, kTile), p.kv_heads, a.batch), 320, smem_keys, stream>>>(mq, mk, mv, mo, p);
-    grad_queries_kernel<DK, DV, BF16><<<dim3((uint32_t)ceil_div(a.seq_q, kTile), a.q_heads, a.batch), 320, smem, stream>>>(mq, mk, mv, mo, p);
-    return cuda_status(cudaGetLastError());
+    const uint32_t longest = BF16 ? a.seq_q : max(a.seq_q, a.seq_kv);
+    grad_rows_kernel<BF16><<<dim3((uint32_t)ceil_div(longest, kRowsOfBlock), a.q_heads, a.batch), 256, 0, stream>>>(p);
+    if ((rc = cuda_status(cudaGetLastError()))) return rc;
+    cudaLaunchAttribute beside;
+    beside.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    beside.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t c{};
+    c.blockDim = dim3(320);
+    c.stream = stream;
+    c.attrs = &beside;
+    c.numAttrs = 1;
+    c.gridDim = dim3((uint32_t)ceil_div(a.seq_kv, kTile), p.kv_heads, a.batch);
+    c.dynamicSmemBytes = smem_keys;
+    if ((rc = cuda_status(cudaLaunchKernelEx(&c, grad_keys_kernel<DK, DV, BF16>, mq, mk, mv, mo, p)))) return rc;
+    c.gridDim = dim3((uint32_t)ceil_div(a.seq_q, kTile), a.q_heads, a.batch);
+    c.dynamicSmemBytes = smem;
+    return cuda_status(cudaLaunchKernelEx(&c, grad_queries_kernel<DK, DV, BF16>, mq, mk, mv, mo, p));
 }
 
 template <int DK, int DV>

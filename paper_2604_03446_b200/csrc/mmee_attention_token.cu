@@ -56,6 +56,7 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 3 : 2) attention_token_
     constexpr uint32_t kRows = 8 * NT, kPitch = DV + 4;
     __shared__ __align__(16) float sums[kWarps][kRows][kPitch];
     __shared__ float tops[kWarps][kRows], totals[kWarps][kRows];
+    asm volatile("griddepcontrol.launch_dependents;");        // (the joining kernel's launch, where there is one)
     const AttentionParams& a = p.a;
     const uint32_t head = blockIdx.y, b = blockIdx.z, parts = gridDim.x, part = blockIdx.x;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, g = lane >> 2, c = lane & 3u;
