@@ -379,28 +379,40 @@ def _refuse(where: str, why: str):
     raise MmeeError(ERR_ARG, "%s: %s" % (where, why))
 
 
-def _chain_code(where: str, rank: int, first, *others):
+_torch = None
+_type_codes = {}
+
+
+def _chain_code(where: str, rank: int, *tensors):
     """The type code that the tensors of one call share: CUDA tensors of one 16-bit type on one device, of `rank` dimensions with
     the last one contiguous."""
-    import torch
-    if not isinstance(first, torch.Tensor):
-        _refuse(where, "tensors are wanted")
-    dtype, at = first.dtype, first.get_device()
-    code = BF16 if dtype is torch.bfloat16 else F16 if dtype is torch.float16 else None
-    if code is None or at < 0:
-        _refuse(where, "bfloat16 or float16 tensors on a CUDA device are wanted")
-    for t in (first,) + others:
-        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != at:
-            _refuse(where, "the tensors are not of one type on one device")
-        if t.dim() != rank or (t.stride(-1) != 1 and t.shape[-1] > 1):
-            _refuse(where, "tensors of %d dimensions are wanted, the last one contiguous" % rank)
-    return code
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+        _type_codes.update({torch.bfloat16: BF16, torch.float16: F16})
+    try:
+        dtype, at = tensors[0].dtype, tensors[0].get_device()
+        code = _type_codes[dtype]
+        for t in tensors:
+            steps = t.stride()
+            if t.dtype is not dtype or t.get_device() != at or len(steps) != rank or (steps[-1] != 1 and t.shape[-1] > 1):
+                break
+        else:
+            if at >= 0:
+                return code
+    except (AttributeError, KeyError, TypeError):
+        pass
+    _refuse(where, "tensors of %d dimensions, the last one contiguous, of bfloat16 or float16 all, on one CUDA device are wanted" % rank)
 
 
-def _elsewhere(t, stream) -> bool:
-    """Whether a call on the tensor's device and the stream has to change what is current."""
+def _current_device():
+    """The current device's number; afterwards without torch's own wrapper around the question (1 us a call)."""
+    global _current_device
     import torch
-    return stream is not None or torch.cuda.current_device() != t.get_device()
+    n = torch.cuda.current_device()
+    _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return n
 
 
 def _there(t, stream):
@@ -442,12 +454,11 @@ def _chain():
 
 def _space(ask, workload, like, where):
     """Workspace for one call (None: it needs none) and its size."""
-    import torch
     need = C.c_uint64()
     code = ask(workload, C.addressof(need))
     if code:
         _check(code, where)
-    return (torch.empty(need.value, dtype=torch.uint8, device=like.device) if need.value else None), need.value
+    return (_torch.empty(need.value, dtype=_torch.uint8, device=like.device) if need.value else None), need.value
 
 
 def _attention_sizes(where, q, k, v, kv_len):
@@ -457,8 +468,7 @@ def _attention_sizes(where, q, k, v, kv_len):
     if b != batch or bv != batch or sv != seq_kv or hv != kv_heads or d != d_qk:
         _refuse(where, "q is (batch, tokens, heads, d), k and v have one batch, length and number of heads, q and k one width")
     if kv_len is not None:
-        import torch
-        if not (isinstance(kv_len, torch.Tensor) and kv_len.dtype is torch.int32 and kv_len.shape == (batch,) and
+        if not (isinstance(kv_len, _torch.Tensor) and kv_len.dtype is _torch.int32 and kv_len.shape == (batch,) and
                 kv_len.get_device() == q.get_device() and kv_len.is_contiguous()):
             _refuse(where, "kv_len is a contiguous int32 tensor, one entry per sequence, on the tensors' device")
     return batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v
@@ -468,10 +478,9 @@ def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
     """softmax(scale q k^T) v over each sequence's first kv_len keys: (o, lse).  q: (batch, tokens, q_heads, d_qk), k: (batch, keys,
     kv_heads, d_qk), v: (batch, keys, kv_heads, d_v), bfloat16 or float16; kv_len: int32 tensor with an entry per sequence, None: all keys;
     scale: d_qk ** -0.5 unless given.  lse: float32 (batch, q_heads, tokens).  Asynchronous."""
-    import torch
     where = "mmee_attention"
     code = _chain_code(where, 4, q, k, v)
-    if _elsewhere(q, stream):
+    if stream is not None or _current_device() != q.get_device():
         with _there(q, stream):
             return mmee_attention(q, k, v, kv_len, scale)
     batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v = _attention_sizes(where, q, k, v, kv_len)
@@ -479,7 +488,7 @@ def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
     w = _WORKLOAD(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v, 2)
     space, need = _space(calls.attention_workspace, w, q, where)
     o = q.new_empty((batch, seq_q, q_heads, d_v))
-    lse = torch.empty((batch, q_heads, seq_q), dtype=torch.float32, device=q.device)
+    lse = _torch.empty((batch, q_heads, seq_q), dtype=_torch.float32, device=q.device)
     a = _ATTENTION(code, (d_qk or 1) ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
                    *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], lse.data_ptr(),
                    0 if kv_len is None else kv_len.data_ptr(), space.data_ptr() if need else 0, need)
@@ -492,16 +501,15 @@ def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
 def mmee_attention_backward(d_o, q, k, v, o, lse, kv_len=None, scale=None, stream=None):
     """The gradients (d_q, d_k, d_v) of mmee_attention for a gradient d_o of o; o and lse are what the forward call with the same
     tensors returned.  Keys behind a sequence's end get zeros.  Asynchronous."""
-    import torch
     where = "mmee_attention_backward"
     code = _chain_code(where, 4, q, k, v, o, d_o)
-    if _elsewhere(q, stream):
+    if stream is not None or _current_device() != q.get_device():
         with _there(q, stream):
             return mmee_attention_backward(d_o, q, k, v, o, lse, kv_len, scale)
     batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v = _attention_sizes(where, q, k, v, kv_len)
     if o.shape != (batch, seq_q, q_heads, d_v) or d_o.shape != o.shape:
         _refuse(where, "o and d_o are (batch, tokens, q_heads, d_v)")
-    if not (isinstance(lse, torch.Tensor) and lse.shape == (batch, q_heads, seq_q) and lse.dtype is torch.float32 and
+    if not (isinstance(lse, _torch.Tensor) and lse.shape == (batch, q_heads, seq_q) and lse.dtype is _torch.float32 and
             lse.get_device() == q.get_device() and lse.is_contiguous()):
         _refuse(where, "lse is what the forward call for these tensors returned")
     calls = _chain()
@@ -530,17 +538,16 @@ def _ffn_sizes(where, x, w_gate, w_up, w_down):
 def mmee_gated_ffn(x, w_gate, w_up, w_down, activation: int = ACT_SILU, save: bool = False, stream=None):
     """y = (act(x w_gate^T) * (x w_up^T)) w_down^T: (y, saved).  x: (tokens, in), w_gate and w_up: (inner, in), w_down: (out, inner),
     bfloat16 or float16.  saved: what mmee_gated_ffn_backward needs where `save`, otherwise None.  Asynchronous."""
-    import torch
     where = "mmee_gated_ffn"
     code = _chain_code(where, 2, x, w_gate, w_up, w_down)
-    if _elsewhere(x, stream):
+    if stream is not None or _current_device() != x.get_device():
         with _there(x, stream):
             return mmee_gated_ffn(x, w_gate, w_up, w_down, activation, save)
     tokens, d_ff, d_in, d_out = _ffn_sizes(where, x, w_gate, w_up, w_down)
     calls = _chain()
     w = _WORKLOAD(1, 1, 1, tokens, d_ff, d_in, d_out, 2)
     hidden, y = x.new_empty((tokens, d_ff)), x.new_empty((tokens, d_out))
-    kept = torch.empty((2, tokens, d_ff), dtype=torch.float32, device=x.device) if save else None
+    kept = _torch.empty((2, tokens, d_ff), dtype=_torch.float32, device=x.device) if save else None
     f = _FFN(code, activation, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), x.stride(0), w_gate.stride(0),
              w_up.stride(0), w_down.stride(0), hidden.data_ptr(), kept.data_ptr() if save else 0, y.data_ptr())
     code = calls.gated_ffn(w, f, _current_stream())
@@ -552,10 +559,11 @@ def mmee_gated_ffn(x, w_gate, w_up, w_down, activation: int = ACT_SILU, save: bo
 def mmee_gated_ffn_backward(d_y, x, w_gate, w_up, w_down, saved, activation: int = ACT_SILU, stream=None):
     """The gradients (d_x, d_w_gate, d_w_up, d_w_down) of mmee_gated_ffn for a gradient d_y of y; `saved` is what the forward call
     with the same x, weights and activation returned.  Asynchronous."""
-    import torch
     where = "mmee_gated_ffn_backward"
+    if not isinstance(saved, tuple) or len(saved) != 2:
+        _refuse(where, "saved is what the forward call with save=True returned")
     code = _chain_code(where, 2, x, w_gate, w_up, w_down, d_y, saved[0])
-    if _elsewhere(x, stream):
+    if stream is not None or _current_device() != x.get_device():
         with _there(x, stream):
             return mmee_gated_ffn_backward(d_y, x, w_gate, w_up, w_down, saved, activation)
     tokens, d_ff, d_in, d_out = _ffn_sizes(where, x, w_gate, w_up, w_down)
@@ -563,7 +571,7 @@ def mmee_gated_ffn_backward(d_y, x, w_gate, w_up, w_down, saved, activation: int
     if d_y.shape != (tokens, d_out):
         _refuse(where, "d_y is (tokens, out)")
     if (hidden.shape != (tokens, d_ff) or not hidden.is_contiguous() or kept.shape != (2, tokens, d_ff) or
-            kept.dtype is not torch.float32 or not kept.is_contiguous() or kept.get_device() != x.get_device()):
+            kept.dtype is not _torch.float32 or not kept.is_contiguous() or kept.get_device() != x.get_device()):
         _refuse(where, "saved is not what the forward call for these tensors returned")
     calls = _chain()
     w = _WORKLOAD(1, 1, 1, tokens, d_ff, d_in, d_out, 2)

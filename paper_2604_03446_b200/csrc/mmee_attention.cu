@@ -369,12 +369,10 @@ int launch_forward(const Problem& x, cudaStream_t stream) {
     int rc = view_map(&mq, BF16, x.p.batch, x.q);
     if (!rc) rc = view_map(&mk, BF16, x.p.batch, x.k);
     if (!rc) rc = view_map(&mv, BF16, x.p.batch, x.v);
-    constexpr uint32_t smem = ForwardShape<DK, DV>::smem(TILES);
-    if (!rc) rc = allow_smem((const void*)attention_kernel<DK, DV, TILES, BF16>, smem);
     if (rc) return rc;
-    const dim3 grid((uint32_t)ceil_div(x.p.seq_q, TILES * kTile), x.p.q_heads, x.p.batch * x.p.splits);
-    attention_kernel<DK, DV, TILES, BF16><<<grid, forward_threads(TILES), smem, stream>>>(mq, mk, mv, x.p);
-    return cuda_status(cudaGetLastError());
+    const LaunchAt at{dim3((uint32_t)ceil_div(x.p.seq_q, TILES * kTile), x.p.q_heads, x.p.batch * x.p.splits), forward_threads(TILES),
+                      ForwardShape<DK, DV>::smem(TILES), 1, false, stream};
+    return launch<attention_kernel<DK, DV, TILES, BF16>>(at, mq, mk, mv, x.p);
 }
 
 // Two query tiles a CTA, or one, of which two share a multiprocessor if the widths allow it: the former where both take as many
@@ -472,16 +470,8 @@ extern "C" int mmee_attention(const mmee_workload_t* workload, const mmee_attent
     if (x.p.splits > 1) {
         const uint64_t rows = (uint64_t)x.p.batch * x.p.q_heads * x.p.seq_q;
         const uint32_t grid = (uint32_t)ceil_div(rows, 4);
-        cudaLaunchAttribute early;
-        early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        early.val.programmaticStreamSerializationAllowed = 1;
-        cudaLaunchConfig_t c{};
-        c.gridDim = dim3(grid);
-        c.blockDim = dim3(128);
-        c.stream = stream;
-        c.attrs = &early;
-        c.numAttrs = 1;
-        rc = cuda_status(x.bf16 ? cudaLaunchKernelEx(&c, attention_join_kernel<true>, x.p) : cudaLaunchKernelEx(&c, attention_join_kernel<false>, x.p));
+        const LaunchAt at{dim3(grid), 128, 0, 1, true, stream};
+        rc = x.bf16 ? launch<attention_join_kernel<true>>(at, x.p) : launch<attention_join_kernel<false>>(at, x.p);
     }
     return rc;
 }

@@ -52,7 +52,8 @@ __global__ void __launch_bounds__(256) grad_rows_kernel(const GradParams p) {
     const uint16_t* const d_o = static_cast<const uint16_t*>(p.d_o) + (int64_t)b * p.dos.batch + (int64_t)head * p.dos.head + 8 * lane;
     const uint16_t* const o = static_cast<const uint16_t*>(a.o) + (int64_t)b * a.os.batch + (int64_t)head * a.os.head + 8 * lane;
     const uint16_t* const v = static_cast<const uint16_t*>(p.v) + (int64_t)b * p.vs.batch + (int64_t)head * p.vs.head + 8 * lane;
-    const uint32_t keys = BF16 || head >= p.kv_heads ? 0 : valid_keys(a.kv_len, b, a.seq_kv);
+    uint32_t keys = 0;
+    if constexpr (!BF16) keys = head < p.kv_heads ? valid_keys(a.kv_len, b, a.seq_kv) : 0;
     const bool in = 8 * lane < a.d_v;
     float most[2] = {0.f, 0.f};
     uint4 x[kRowsOfBlock / 16], y[kRowsOfBlock / 16], z[kRowsOfBlock / 16];
@@ -62,7 +63,7 @@ __global__ void __launch_bounds__(256) grad_rows_kernel(const GradParams p) {
         const uint4 none = make_uint4(0, 0, 0, 0);
         x[i] = in && token < a.seq_q ? *reinterpret_cast<const uint4*>(d_o + (int64_t)token * p.dos.token) : none;
         y[i] = in && token < a.seq_q ? *reinterpret_cast<const uint4*>(o + (int64_t)token * a.os.token) : none;
-        if (!BF16) z[i] = in && token < keys ? *reinterpret_cast<const uint4*>(v + (int64_t)token * p.vs.token) : none;
+        if constexpr (!BF16) z[i] = in && token < keys ? *reinterpret_cast<const uint4*>(v + (int64_t)token * p.vs.token) : none;
     }
 #pragma unroll
     for (uint32_t i = 0; i < kRowsOfBlock / 16; ++i) {
@@ -614,28 +615,16 @@ int launch_grads(const Problem& x, const View& d_o, const GradParams& p, cudaStr
     if (!rc) rc = view_map(&mk, BF16, a.batch, x.k);
     if (!rc) rc = view_map(&mv, BF16, a.batch, x.v);
     if (!rc) rc = view_map(&mo, BF16, a.batch, d_o);
-    constexpr uint32_t smem = GradShape<DK, DV>::smem, smem_keys = GradShape<DK, DV>::smem_keys;
-    if (!rc) rc = allow_smem((const void*)grad_keys_kernel<DK, DV, BF16>, smem_keys);
-    if (!rc) rc = allow_smem((const void*)grad_queries_kernel<DK, DV, BF16>, smem);
     if (rc) return rc;
     if (!BF16 && (rc = cuda_status(cudaMemsetAsync(p.most, 0, 8, stream)))) return rc;
     const uint32_t longest = BF16 ? a.seq_q : max(a.seq_q, a.seq_kv);
-    grad_rows_kernel<BF16><<<dim3((uint32_t)ceil_div(longest, kRowsOfBlock), a.q_heads, a.batch), 256, 0, stream>>>(p);
-    if ((rc = cuda_status(cudaGetLastError()))) return rc;
-    cudaLaunchAttribute beside;
-    beside.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    beside.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t c{};
-    c.blockDim = dim3(320);
-    c.stream = stream;
-    c.attrs = &beside;
-    c.numAttrs = 1;
-    c.gridDim = dim3((uint32_t)ceil_div(a.seq_kv, kTile), p.kv_heads, a.batch);
-    c.dynamicSmemBytes = smem_keys;
-    if ((rc = cuda_status(cudaLaunchKernelEx(&c, grad_keys_kernel<DK, DV, BF16>, mq, mk, mv, mo, p)))) return rc;
-    c.gridDim = dim3((uint32_t)ceil_div(a.seq_q, kTile), a.q_heads, a.batch);
-    c.dynamicSmemBytes = smem;
-    return cuda_status(cudaLaunchKernelEx(&c, grad_queries_kernel<DK, DV, BF16>, mq, mk, mv, mo, p));
+    using Shape = GradShape<DK, DV>;
+    const LaunchAt rows{dim3((uint32_t)ceil_div(longest, kRowsOfBlock), a.q_heads, a.batch), 256, 0, 1, false, stream};
+    const LaunchAt keys{dim3((uint32_t)ceil_div(a.seq_kv, kTile), p.kv_heads, a.batch), 320, Shape::smem_keys, 1, true, stream};
+    const LaunchAt queries{dim3((uint32_t)ceil_div(a.seq_q, kTile), a.q_heads, a.batch), 320, Shape::smem, 1, true, stream};
+    rc = launch<grad_rows_kernel<BF16>>(rows, p);
+    if (!rc) rc = launch<grad_keys_kernel<DK, DV, BF16>>(keys, mq, mk, mv, mo, p);
+    return rc ? rc : launch<grad_queries_kernel<DK, DV, BF16>>(queries, mq, mk, mv, mo, p);
 }
 
 template <int DK, int DV>

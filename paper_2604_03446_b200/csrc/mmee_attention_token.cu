@@ -86,8 +86,9 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 3 : 2) attention_token_
     }
     const float sl2 = a.scale * kLog2e;
 
-    for (uint32_t key = begin + warp * kStep; key < end; key += kWarps * kStep) {
-        uint4 kf[2][DK / 32], vf[DV / 64][4];
+    // The next step's keys are under way while this one's probabilities are made, its values while the next scores are.
+    uint4 kf[2][DK / 32], vf[DV / 64][4];
+    auto load_keys = [&](uint32_t key) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t at = key + g + 8 * i;
@@ -95,6 +96,8 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 3 : 2) attention_token_
 #pragma unroll
             for (int j = 0; j < DK / 32; ++j) kf[i][j] = at < end && 32 * j + 8 * c < a.d_qk ? read16(row + 32 * j) : none;
         }
+    };
+    auto load_values = [&](uint32_t key) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t at = key + 2 * c + (i & 1) + 8 * (i >> 1);
@@ -102,6 +105,10 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 3 : 2) attention_token_
 #pragma unroll
             for (int j = 0; j < DV / 64; ++j) vf[j][i] = at < end && 64 * j + 8 * g < a.d_v ? read16(row + 64 * j) : none;
         }
+    };
+    load_keys(begin + warp * kStep);
+    load_values(begin + warp * kStep);
+    for (uint32_t key = begin + warp * kStep; key < end; key += kWarps * kStep) {
         float s[NT][4];
         bool more = false;
 #pragma unroll
@@ -117,6 +124,7 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 3 : 2) attention_token_
             for (int i = 0; i < 4; ++i) s[t][i] = key + g + 8 * (i >> 1) < end ? s[t][i] * sl2 : -INFINITY;
             more |= fmaxf(s[t][0], s[t][2]) > m[t][0] + kSlack || fmaxf(s[t][1], s[t][3]) > m[t][1] + kSlack;
         }
+        load_keys(key + kWarps * kStep);
         if (__any_sync(0xffffffffu, more)) {           // the reference moves, for the columns that need it
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -158,6 +166,7 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 3 : 2) attention_token_
 #pragma unroll
                 for (int t = 0; t < NT; ++t) mma16<BF16>(acc[t][j][i], a0, a1, a2, a3, pr[t][0], pr[t][1]);
             }
+        load_values(key + kWarps * kStep);
     }
 
     // The warps' parts, each relative to its own reference.
@@ -226,18 +235,8 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 3 : 2) attention_token_
 
 template <int DK, int DV, int NT>
 int launch_tokens(const TokenParams& p, bool bf16, cudaStream_t stream) {
-    cudaLaunchConfig_t c{};
-    c.gridDim = dim3(p.cluster * p.a.splits, p.a.q_heads / p.a.group, p.a.batch);
-    c.blockDim = dim3(kWarps * 32);
-    c.stream = stream;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = p.cluster;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    c.attrs = &attr;
-    c.numAttrs = p.cluster > 1;
-    return cuda_status(bf16 ? cudaLaunchKernelEx(&c, attention_token_kernel<DK, DV, NT, true>, p)
-                            : cudaLaunchKernelEx(&c, attention_token_kernel<DK, DV, NT, false>, p));
+    const LaunchAt at{dim3(p.cluster * p.a.splits, p.a.q_heads / p.a.group, p.a.batch), kWarps * 32, 0, p.cluster, false, stream};
+    return bf16 ? launch<attention_token_kernel<DK, DV, NT, true>>(at, p) : launch<attention_token_kernel<DK, DV, NT, false>>(at, p);
 }
 
 template <int NT>
@@ -253,10 +252,12 @@ int token_splits(const AttentionParams& a, uint32_t* cluster, uint32_t* clusters
     uint32_t sms;
     const int rc = sm_count(&sms);
     if (rc) return rc;
-    // Three CTAs fit a multiprocessor.  Parts of 64 keys at least (a step of every warp).
+    // Three CTAs fit a multiprocessor.  Parts of 64 keys at least (a step of every warp).  Where they fill the multiprocessors, long ones are
+    // halved once more, so that sequences of different lengths keep them all at work (32 sequences of up to 8192 keys: 126 us, 116 us
+    // with four parts instead of two; with parts of 512 keys it does not pay).
     const uint64_t heads = (uint64_t)a.batch * (a.q_heads / a.group), room = 3ull * sms, most = ceil_div(a.seq_kv, kWarps * kStep);
     uint64_t parts = 1;
-    while (parts < 8 && parts * heads < room && 2 * parts <= most) parts *= 2;
+    while (parts < 8 && 2 * parts <= most && (parts * heads < room || (parts * heads < 2 * room && a.seq_kv >= 2048 * parts))) parts *= 2;
     *cluster = (uint32_t)parts;
     // Few heads with very many keys: more clusters, of at least 16 steps a CTA, which pay for the launch that joins them.
     uint64_t more = 1;

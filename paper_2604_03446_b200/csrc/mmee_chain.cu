@@ -44,16 +44,16 @@ int tile_map(CUtensorMap* map, Values type, const void* base, uint32_t rank, con
 }
 
 int sm_count(uint32_t* out) {
+    static std::atomic<uint32_t> known[64];            // (asking takes longer than a launch's other preparations)
     int device = 0, n = 0;
     cudaError_t e = cudaGetDevice(&device);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device);
+    if (e != cudaSuccess) return cuda_status(e);
+    if (device < 64 && (*out = known[device].load(std::memory_order_relaxed))) return MMEE_OK;
+    e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device);
     if (e != cudaSuccess) return cuda_status(e);
     *out = (uint32_t)n;
+    if (device < 64) known[device].store(*out, std::memory_order_relaxed);
     return MMEE_OK;
-}
-
-int allow_smem(const void* kernel, uint32_t bytes) {
-    return cuda_status(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
 }
 
 }  // namespace mmee

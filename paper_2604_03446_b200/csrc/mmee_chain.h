@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/mmee.h"
 
 namespace mmee {
@@ -22,8 +24,52 @@ inline int tile_map(CUtensorMap* map, bool bf16, const void* base, uint32_t rank
 // Streaming multiprocessors of the current device.
 int sm_count(uint32_t* out);
 
-// Lets a kernel use that much dynamic shared memory on the current device.
-int allow_smem(const void* kernel, uint32_t bytes);
+// A launch of KERNEL with up to 227 KB of dynamic shared memory; `cluster` CTAs to a cluster; `early`: it may start before the kernel
+// before it in the stream has ended, and waits for it itself.
+struct LaunchAt {
+    dim3 grid;
+    uint32_t block, smem, cluster;
+    bool early;
+    cudaStream_t stream;
+};
+
+template <auto KERNEL, typename... Args>
+int launch(const LaunchAt& at, const Args&... args) {
+    // Devices on which the kernel may use its shared memory: asked for once, and again where the device has been reset since.
+    static std::atomic<uint64_t> allowed{0};
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return cuda_status(e);
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    cudaLaunchAttribute attr[2];
+    cudaLaunchConfig_t c{};
+    c.gridDim = at.grid;
+    c.blockDim = dim3(at.block);
+    c.dynamicSmemBytes = at.smem;
+    c.stream = at.stream;
+    c.attrs = attr;
+    if (at.cluster > 1) {
+        attr[c.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        attr[c.numAttrs].val.clusterDim.x = at.cluster;
+        attr[c.numAttrs].val.clusterDim.y = attr[c.numAttrs].val.clusterDim.z = 1;
+        ++c.numAttrs;
+    }
+    if (at.early) {
+        attr[c.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[c.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+        ++c.numAttrs;
+    }
+    for (bool ask = at.smem > 48 * 1024 && !(allowed.load(std::memory_order_relaxed) & bit);; ask = true) {
+        if (ask) {
+            e = cudaFuncSetAttribute((const void*)KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)at.smem);
+            if (e != cudaSuccess) return cuda_status(e);
+            allowed.fetch_or(bit, std::memory_order_relaxed);
+        }
+        e = cudaLaunchKernelEx(&c, KERNEL, args...);
+        if (e != cudaErrorInvalidValue || ask || at.smem <= 48 * 1024) return cuda_status(e);
+        cudaGetLastError();
+    }
+}
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 constexpr uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }

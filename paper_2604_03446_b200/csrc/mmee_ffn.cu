@@ -418,21 +418,9 @@ int launch_products(Products& ps, Operand* (&ops)[kMostProducts][4], uint32_t sm
         if (!rc && p.gate) rc = tile_map(&ps.gate, Values::f32, p.gate, 2, result, &n, 32);
         if (!rc && p.gate) rc = tile_map(&ps.up, Values::f32, p.up, 2, result, &n, 32);
     }
-    const auto kernel = product_kernel<EPI, PAIR, TN, BF16>;
-    if (!rc) rc = allow_smem((const void*)kernel, Shape::smem);
     if (rc) return rc;
-    cudaLaunchConfig_t c{};
-    c.gridDim = dim3(PAIR ? 2 * min(sms / 2, end) : min(sms, end));
-    c.blockDim = dim3(192);
-    c.dynamicSmemBytes = Shape::smem;
-    c.stream = stream;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 2;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    c.attrs = &attr;
-    c.numAttrs = PAIR ? 1 : 0;
-    return cuda_status(cudaLaunchKernelEx(&c, kernel, ps));
+    const LaunchAt at{dim3(PAIR ? 2 * min(sms / 2, end) : min(sms, end)), 192, Shape::smem, PAIR ? 2u : 1u, false, stream};
+    return launch<product_kernel<EPI, PAIR, TN, BF16>>(at, ps);
 }
 
 // Tiles of 256 x 256 by pairs of CTAs where there are enough of them; smaller ones where that would leave multiprocessors idle.

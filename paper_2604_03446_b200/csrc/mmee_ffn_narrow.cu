@@ -209,27 +209,14 @@ int launch_narrow(const FfnTokens& p, cudaStream_t stream) {
     int rc = GATE ? matrix_map(&w0, BF16, p.w_gate, rows, depth, p.w_gate_stride, kRowsW) : matrix_map(&w0, BF16, p.w_down, rows, depth, p.w_down_stride, kRowsW);
     if (!rc && GATE) rc = matrix_map(&w1, BF16, p.w_up, rows, depth, p.w_up_stride, kRowsW);
     if (!rc) rc = GATE ? matrix_map(&x, BF16, p.x, p.tokens, depth, p.x_stride, z.cols) : matrix_map(&x, BF16, p.hidden, p.tokens, depth, depth, z.cols);
-    if (!rc) rc = allow_smem((const void*)ffn_narrow_kernel<GATE, BF16>, kNarrowSmem);
     uint32_t sms;
     if (!rc) rc = sm_count(&sms);
     if (rc) return rc;
     // Parts of the reduction: as many as fill the multiprocessors twice, of two steps at least.
     const uint32_t tiles = (uint32_t)ceil_div(rows, kRowsW), most = (uint32_t)ceil_div(depth, 128);
     const uint32_t parts = max(1u, min(min(8u, 2 * sms / tiles), most));
-    cudaLaunchConfig_t c{};
-    c.gridDim = dim3(tiles * parts);
-    c.blockDim = dim3(192);
-    c.dynamicSmemBytes = kNarrowSmem;
-    c.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = parts;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    c.attrs = attr;
-    c.numAttrs = GATE ? 1 : 2;
-    return cuda_status(cudaLaunchKernelEx(&c, ffn_narrow_kernel<GATE, BF16>, w0, GATE ? w1 : w0, x, p, z));
+    const LaunchAt at{dim3(tiles * parts), 192, kNarrowSmem, parts, !GATE, stream};
+    return launch<ffn_narrow_kernel<GATE, BF16>>(at, w0, GATE ? w1 : w0, x, p, z);
 }
 
 }  // namespace

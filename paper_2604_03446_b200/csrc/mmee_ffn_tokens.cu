@@ -131,29 +131,21 @@ __global__ void __launch_bounds__(kMostWarps * 32, 2) ffn_tokens_kernel(const Ff
 }
 
 template <bool BF16>
-int launch(const FfnTokens& p, cudaStream_t stream) {
+int launch_both(const FfnTokens& p, cudaStream_t stream) {
     // As many warps to a CTA as there are turns, eight at most.
     auto threads = [](uint32_t depth, uint32_t turn) {
         uint32_t n = 1;
         while (n < kMostWarps && n * 2 * turn <= depth) n *= 2;
         return 32 * n;
     };
-    ffn_tokens_kernel<true, BF16><<<(uint32_t)ceil_div(p.d_ff, 16), threads(p.d_in, 64), 0, stream>>>(p);
-    cudaLaunchConfig_t c{};
-    c.gridDim = dim3((uint32_t)ceil_div(p.d_out, 16));
-    c.blockDim = dim3(threads(p.d_ff, 128));
-    c.stream = stream;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    c.attrs = &attr;
-    c.numAttrs = 1;
-    const cudaError_t e = cudaGetLastError();
-    return cuda_status(e != cudaSuccess ? e : cudaLaunchKernelEx(&c, ffn_tokens_kernel<false, BF16>, p));
+    const LaunchAt gate{dim3((uint32_t)ceil_div(p.d_ff, 16)), threads(p.d_in, 64), 0, 1, false, stream};
+    const LaunchAt down{dim3((uint32_t)ceil_div(p.d_out, 16)), threads(p.d_ff, 128), 0, 1, true, stream};
+    const int rc = launch<ffn_tokens_kernel<true, BF16>>(gate, p);
+    return rc ? rc : launch<ffn_tokens_kernel<false, BF16>>(down, p);
 }
 
 }  // namespace
 
-int ffn_tokens(const FfnTokens& p, bool bf16, cudaStream_t stream) { return bf16 ? launch<true>(p, stream) : launch<false>(p, stream); }
+int ffn_tokens(const FfnTokens& p, bool bf16, cudaStream_t stream) { return bf16 ? launch_both<true>(p, stream) : launch_both<false>(p, stream); }
 
 }  // namespace mmee
