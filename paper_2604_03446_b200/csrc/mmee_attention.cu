@@ -39,12 +39,14 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     __shared__ __align__(8) uint64_t bars[TILES * 5 + 4 * kRing + 1];
     __shared__ uint32_t tmem_base, gave_up;
 
-    const uint32_t b = blockIdx.z / p.splits, split = blockIdx.z % p.splits, head = blockIdx.y;
-    const uint32_t q0 = blockIdx.x * TILES * kTile;
+    // The query tile, and the part of its keys.
+    const bool cut_up = blockIdx.x >= p.whole;
+    const uint32_t past = blockIdx.x - p.whole, split = cut_up ? past % p.splits : 0, tile = cut_up ? p.whole + past / p.splits : blockIdx.x;
+    const uint32_t head = tile / p.tiles_q % p.q_heads, b = tile / p.tiles_q / p.q_heads, q0 = tile % p.tiles_q * (TILES * kTile);
     const uint32_t tiles = (p.seq_q - q0 <= kTile) ? 1 : TILES;
     const uint32_t keys = valid_keys(p.kv_len, b, p.seq_kv);
     const uint32_t t0 = split * p.tiles_per_split, t_all = (keys + kTile - 1) / kTile;
-    const uint32_t n = t0 < t_all ? min(p.tiles_per_split, t_all - t0) : 0;      // key tiles of this CTA
+    const uint32_t n = !cut_up ? t_all : t0 < t_all ? min(p.tiles_per_split, t_all - t0) : 0;     // key tiles of this CTA
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
 
     const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
@@ -273,14 +275,13 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         if (n && sound) sound = mbar_wait(o_full(t), 0, lost);
         tcgen05_fence_after();
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        const uint64_t at = ((uint64_t)b * p.q_heads + head) * p.seq_q + token;
-        const uint64_t rows = (uint64_t)p.batch * p.q_heads * p.seq_q;
+        const uint64_t part_at = ((uint64_t)split * (p.tiles - p.whole) + (tile - p.whole)) * p.tile_rows + t * kTile + row;    // (if cut up)
         if (sound && token < p.seq_q) {
             const float l2 = l == 0.f ? -INFINITY : m - kBias<BF16> + log2f(l);
-            if (p.splits > 1)
-                p.part_lse[split * rows + at] = l2;
+            if (cut_up)
+                p.part_lse[part_at] = l2;
             else if (p.lse)
-                p.lse[at] = l2 * kLn2;
+                p.lse[((uint64_t)b * p.q_heads + head) * p.seq_q + token] = l2 * kLn2;
         }
         if (sound) {
             const int64_t to = (int64_t)b * p.os.batch + (int64_t)token * p.os.token + (int64_t)head * p.os.head;
@@ -295,9 +296,9 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                     float v[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = l == 0.f ? 0.f : __uint_as_float(o[j]) * inv;
-                    if (p.splits > 1) {
+                    if (cut_up) {
                         if (l != 0.f) {
-                            float4* const q = reinterpret_cast<float4*>(p.part_o + (split * rows + at) * p.d_v + c);
+                            float4* const q = reinterpret_cast<float4*>(p.part_o + part_at * p.d_v + c);
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
                                 if (c + 4 * j < p.d_v) q[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
@@ -332,10 +333,12 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
 template <bool BF16>
 __global__ void __launch_bounds__(128) attention_join_kernel(const AttentionParams p) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const uint64_t rows = (uint64_t)p.batch * p.q_heads * p.seq_q;
-    const uint64_t at = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const uint64_t rows = (uint64_t)(p.tiles - p.whole) * p.tile_rows, at = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     const uint32_t lane = threadIdx.x & 31u;
     if (at >= rows) return;
+    const uint32_t tile = p.whole + (uint32_t)(at / p.tile_rows), token = tile % p.tiles_q * p.tile_rows + (uint32_t)(at % p.tile_rows);
+    const uint32_t head = tile / p.tiles_q % p.q_heads, b = tile / p.tiles_q / p.q_heads;
+    if (token >= p.seq_q) return;
     const float part = lane < p.splits ? p.part_lse[lane * rows + at] : -INFINITY;
     float top = part;
     for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
@@ -352,9 +355,7 @@ __global__ void __launch_bounds__(128) attention_join_kernel(const AttentionPara
         }
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const uint32_t token = (uint32_t)(at % p.seq_q), head = (uint32_t)(at / p.seq_q % p.q_heads);
-    const uint64_t b = at / ((uint64_t)p.seq_q * p.q_heads);
-    if (p.lse && lane == 0) p.lse[at] = sum == 0.f ? -INFINITY : (from + log2f(sum)) * kLn2;
+    if (p.lse && lane == 0) p.lse[((uint64_t)b * p.q_heads + head) * p.seq_q + token] = sum == 0.f ? -INFINITY : (from + log2f(sum)) * kLn2;
     if (4 * lane < p.d_v) {
         uint16_t* const to = static_cast<uint16_t*>(p.o) + (int64_t)b * p.os.batch + (int64_t)token * p.os.token + (int64_t)head * p.os.head;
         *reinterpret_cast<uint2*>(to + 4 * lane) = make_uint2(pack2<BF16>(v[0] * inv, v[1] * inv), pack2<BF16>(v[2] * inv, v[3] * inv));
@@ -370,27 +371,13 @@ int launch_forward(const Problem& x, cudaStream_t stream) {
     if (!rc) rc = view_map(&mk, BF16, x.p.batch, x.k);
     if (!rc) rc = view_map(&mv, BF16, x.p.batch, x.v);
     if (rc) return rc;
-    const LaunchAt at{dim3((uint32_t)ceil_div(x.p.seq_q, TILES * kTile), x.p.q_heads, x.p.batch * x.p.splits), forward_threads(TILES),
-                      ForwardShape<DK, DV>::smem(TILES), 1, false, stream};
+    const LaunchAt at{dim3(x.p.whole + (x.p.tiles - x.p.whole) * x.p.splits), forward_threads(TILES), ForwardShape<DK, DV>::smem(TILES), 1, false, stream};
     return launch<attention_kernel<DK, DV, TILES, BF16>>(at, mq, mk, mv, x.p);
-}
-
-// Two query tiles a CTA, or one, of which two share a multiprocessor if the widths allow it: the former where both take as many
-// turns of the multiprocessors, as its tiles share the loads of the keys.
-template <int DK, int DV>
-bool single_tiles(const AttentionParams& p, uint32_t sms) {
-    if (p.seq_q <= kTile) return true;
-    if (DK + DV > 128) return false;
-    const uint64_t heads = (uint64_t)p.q_heads * p.batch * p.splits;
-    return ceil_div(ceil_div(p.seq_q, kTile) * heads, 2 * sms) < ceil_div(ceil_div(p.seq_q, 2 * kTile) * heads, sms);
 }
 
 template <int DK, int DV>
 int forward_typed(const Problem& x, cudaStream_t stream) {
-    uint32_t sms;
-    const int rc = sm_count(&sms);
-    if (rc) return rc;
-    if (single_tiles<DK, DV>(x.p, sms)) return x.bf16 ? launch_forward<DK, DV, 1, true>(x, stream) : launch_forward<DK, DV, 1, false>(x, stream);
+    if (x.p.tile_rows == kTile) return x.bf16 ? launch_forward<DK, DV, 1, true>(x, stream) : launch_forward<DK, DV, 1, false>(x, stream);
     return x.bf16 ? launch_forward<DK, DV, 2, true>(x, stream) : launch_forward<DK, DV, 2, false>(x, stream);
 }
 
@@ -400,29 +387,45 @@ int forward(const Problem& x, cudaStream_t stream) {
              : v ? forward_typed<64, 128>(x, stream) : forward_typed<64, 64>(x, stream);
 }
 
-// Parts that the keys are cut into where the query tiles alone leave most of the multiprocessors without work: as many as fill
-// them once, of at least two tiles each.
-// Up to 16 query rows to a key head take the kernel for few rows (`cluster` > 0), in `splits` parts that are joined afterwards.
-int choose_splits(AttentionParams* p, uint32_t* cluster) {
+// How a call is cut up.  Up to 16 query rows to a key head take the kernel for few rows (`cluster` > 0).
+int plan(AttentionParams* p, uint32_t* cluster) {
     *cluster = 0;
-    if ((uint64_t)p->group * p->seq_q <= 16) return token_splits(*p, cluster, &p->splits);
+    const uint64_t heads = (uint64_t)p->q_heads * p->batch;
+    if ((uint64_t)p->group * p->seq_q <= 16) {
+        p->tile_rows = p->seq_q;
+        p->tiles_q = 1;
+        p->tiles = (uint32_t)heads;
+        return token_splits(*p, cluster, &p->splits);
+    }
     uint32_t sms;
     const int rc = sm_count(&sms);
     if (rc) return rc;
-    const uint64_t ctas = ceil_div(p->seq_q, p->seq_q <= kTile ? kTile : 2 * kTile) * p->q_heads * p->batch;
-    const uint32_t tiles = (uint32_t)ceil_div(p->seq_kv, kTile);
-    uint64_t splits = 2 * ctas > sms ? 1 : sms / ctas;
-    if (splits > tiles / 2) splits = tiles / 2;
-    if (splits > 16) splits = 16;                      // (batch * splits has to stay within the grid, and parts cost memory)
-    if (splits < 1) splits = 1;
-    p->tiles_per_split = (uint32_t)ceil_div(tiles, splits);
-    p->splits = (uint32_t)ceil_div(tiles, p->tiles_per_split);
+    // Two query tiles a CTA, which share the loads of the keys; or one, of which two fit a multiprocessor if the widths allow it, where
+    // that takes fewer turns of the multiprocessors.
+    const bool narrow = p->d_qk <= 64 && p->d_v <= 64;
+    const uint64_t ones = ceil_div(p->seq_q, kTile) * heads, twos = ceil_div(p->seq_q, 2 * kTile) * heads;
+    const bool single = p->seq_q <= kTile || (narrow && ceil_div(ones, 2 * sms) < ceil_div(twos, sms));
+    p->tile_rows = single ? kTile : 2 * kTile;
+    p->tiles_q = (uint32_t)ceil_div(p->seq_q, p->tile_rows);
+    if ((single ? ones : twos) >> 27) return MMEE_ERR_RANGE;
+    p->tiles = (uint32_t)(single ? ones : twos);
+    // Query tiles that would leave most of the multiprocessors without work have their keys cut into parts: all of them where they are
+    // few, of two tiles of keys at least; otherwise those of the last turn, if the time of eight tiles of keys is saved (parts
+    // cost a launch, and their sums' way through memory).
+    const uint32_t slots = single && narrow ? 2 * sms : sms, keys = (uint32_t)ceil_div(p->seq_kv, kTile), last = p->tiles % slots;
+    uint32_t splits = last ? min(slots / last, 16u) : 1;
+    if (p->tiles < slots)
+        splits = min(splits, keys / 2);
+    else if (keys - keys / splits < 8)
+        splits = 1;
+    p->whole = splits > 1 ? p->tiles - last : p->tiles;
+    p->tiles_per_split = splits > 1 ? (uint32_t)ceil_div(keys, splits) : keys;
+    p->splits = (uint32_t)ceil_div(keys, p->tiles_per_split);
     return MMEE_OK;
 }
 
-uint64_t parts_bytes(const AttentionParams& p) {
-    return p.splits > 1 ? round_up((uint64_t)p.splits * p.batch * p.q_heads * p.seq_q * 4, 16) * (p.d_v + 1) : 0;
-}
+uint64_t part_rows(const AttentionParams& p) { return p.splits > 1 ? (uint64_t)p.splits * (p.tiles - p.whole) * p.tile_rows : 0; }
+uint64_t parts_bytes(const AttentionParams& p) { return round_up(part_rows(p) * 4, 16) * (p.d_v + 1); }
 
 }  // namespace
 
@@ -444,11 +447,12 @@ extern "C" int mmee_attention_workspace(const mmee_workload_t* w, uint64_t* byte
     p.q_heads = w->q_heads;
     p.seq_q = w->seq_q;
     p.seq_kv = w->seq_kv;
+    p.d_qk = w->d_qk;
     p.d_v = w->d_v;
     if (!p.batch || w->q_heads < w->kv_heads || !p.seq_q || !p.seq_kv) return MMEE_ERR_ARG;
     p.group = w->q_heads / w->kv_heads;
     uint32_t cluster;
-    const int rc = choose_splits(&p, &cluster);
+    const int rc = plan(&p, &cluster);
     if (!rc) *bytes = parts_bytes(p);
     return rc;
 }
@@ -457,20 +461,18 @@ extern "C" int mmee_attention(const mmee_workload_t* workload, const mmee_attent
     Problem x;
     int rc = check(workload, a, &x);
     uint32_t cluster;
-    if (!rc) rc = choose_splits(&x.p, &cluster);
+    if (!rc) rc = plan(&x.p, &cluster);
     if (rc) return rc;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (x.p.splits > 1) {
+    const uint64_t rows = part_rows(x.p);
+    if (rows) {
         if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < parts_bytes(x.p)) return MMEE_ERR_ARG;
-        const uint64_t rows = (uint64_t)x.p.splits * x.p.batch * x.p.q_heads * x.p.seq_q;
         x.p.part_o = static_cast<float*>(a->workspace);
         x.p.part_lse = x.p.part_o + rows * x.p.d_v;
     }
     if ((rc = cluster ? attention_tokens(x, cluster, stream) : forward(x, stream))) return rc;
-    if (x.p.splits > 1) {
-        const uint64_t rows = (uint64_t)x.p.batch * x.p.q_heads * x.p.seq_q;
-        const uint32_t grid = (uint32_t)ceil_div(rows, 4);
-        const LaunchAt at{dim3(grid), 128, 0, 1, true, stream};
+    if (rows) {
+        const LaunchAt at{dim3((uint32_t)ceil_div(rows / x.p.splits, 4)), 128, 0, 1, true, stream};
         rc = x.bf16 ? launch<attention_join_kernel<true>>(at, x.p) : launch<attention_join_kernel<false>>(at, x.p);
     }
     return rc;

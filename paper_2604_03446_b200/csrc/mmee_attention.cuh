@@ -25,13 +25,15 @@ struct Strides {
 
 struct AttentionParams {
     uint32_t batch, q_heads, group, seq_q, seq_kv, d_qk, d_v;
-    uint32_t splits, tiles_per_split;  // parts that the keys are cut into, tiles of each
+    // Query tiles (blocks of `tile_rows` rows of a head, `tiles_q` of them, `tiles` in all) from `whole` on have their keys cut into
+    // `splits` parts of `tiles_per_split` tiles of keys, which are joined afterwards.
+    uint32_t tile_rows, tiles_q, tiles, whole, splits, tiles_per_split;
     float scale;
     const int32_t* kv_len;
     void* o;
     Strides os;
     float* lse;                        // [batch][q_heads][seq_q]
-    float *part_o, *part_lse;          // splits > 1: [split][batch][q_heads][seq_q] rows of d_v; log2 of the sums
+    float *part_o, *part_lse;          // [split][tiles - whole][tile_rows] rows of d_v; log2 of the sums
 };
 
 __device__ __forceinline__ uint32_t valid_keys(const int32_t* kv_len, uint32_t b, uint32_t seq_kv) {
@@ -154,8 +156,6 @@ inline int check(const mmee_workload_t* w, const mmee_attention_t* a, Problem* o
     p.seq_kv = w->seq_kv;
     p.d_qk = w->d_qk;
     p.d_v = w->d_v;
-    p.splits = 1;
-    p.tiles_per_split = (uint32_t)ceil_div(w->seq_kv, kTile);
     p.scale = a->scale;
     p.kv_len = a->kv_len;
     p.o = a->o;

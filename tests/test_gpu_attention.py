@@ -20,7 +20,8 @@ SIZES = [
     (2, 8, 1, 2, 777, 72, 40), (1, 16, 1, 1, 1000, 128, 64), (1, 2, 2, 16, 65, 40, 128), (1, 1, 1, 8, 5000, 128, 128),
     (1, 4, 4, 17, 128, 64, 64), (2, 4, 2, 64, 129, 64, 128), (1, 2, 1, 100, 127, 128, 64), (1, 1, 1, 127, 1, 96, 96),
     (3, 5, 1, 77, 1501, 72, 40), (1, 3, 3, 128, 128, 128, 128), (2, 2, 2, 129, 255, 64, 64), (1, 2, 2, 255, 256, 128, 128),
-    (1, 4, 1, 256, 257, 120, 8), (2, 4, 2, 300, 640, 64, 64), (1, 2, 1, 513, 1025, 128, 128), (1, 1, 1, 200, 9000, 64, 64),
+    (1, 4, 1, 256, 257, 120, 8), (2, 4, 2, 300, 640, 64, 64), (1, 2, 1, 513, 1025, 128, 128), (1, 1, 1, 200, 9000, 64, 64), (5, 16, 4, 260, 2700, 128, 64),
+    (1, 31, 31, 700, 1300, 64, 64),
 ]
 
 
