@@ -492,6 +492,8 @@ typedef struct {
     float   *kept;                           /* out, may be NULL: gate, then up, tokens x L each, for the backward
                                                 pass (there: in)                                  */
     void    *y;                              /* out: tokens x J, contiguous (backward: not used)  */
+    void    *workspace;                      /* DEVICE, mmee_gated_ffn_workspace bytes (0: may be NULL), for this call alone until it ends */
+    uint64_t workspace_bytes;
 } mmee_gated_ffn_t;
 int mmee_gated_ffn(const mmee_workload_t* workload, const mmee_gated_ffn_t* f, void* cuda_stream);
 
@@ -504,12 +506,11 @@ typedef struct {
     const void *d_y;                         /* tokens x J                                        */
     int64_t  d_y_stride;
     void    *d_x, *d_w_gate, *d_w_up, *d_w_down;   /* out: shaped as x and the weights, contiguous */
-    void    *workspace;                      /* DEVICE, mmee_gated_ffn_workspace bytes, for this call alone until it ends */
-    uint64_t workspace_bytes;
 } mmee_gated_ffn_grad_t;
 int mmee_gated_ffn_backward(const mmee_workload_t* workload, const mmee_gated_ffn_t* f, const mmee_gated_ffn_grad_t* g,
                             void* cuda_stream);
-int mmee_gated_ffn_workspace(const mmee_workload_t* workload, uint64_t* bytes);
+/* backward: 1 for the workspace of mmee_gated_ffn_backward, 0 for that of mmee_gated_ffn */
+int mmee_gated_ffn_workspace(const mmee_workload_t* workload, uint32_t backward, uint64_t* bytes);
 
 /*
  * mmee_chain_status -- MMEE_OK, or MMEE_ERR_TIMEOUT once after a wait inside one of the chains' kernels ran out

@@ -92,12 +92,13 @@ class GatedFfn(C.Structure):
     _fields_ = [("dtype", C.c_uint32), ("activation", C.c_uint32),
                 ("x", C.c_void_p), ("w_gate", C.c_void_p), ("w_up", C.c_void_p), ("w_down", C.c_void_p),
                 ("x_stride", C.c_int64), ("w_gate_stride", C.c_int64), ("w_up_stride", C.c_int64),
-                ("w_down_stride", C.c_int64), ("hidden", C.c_void_p), ("kept", C.c_void_p), ("y", C.c_void_p)]
+                ("w_down_stride", C.c_int64), ("hidden", C.c_void_p), ("kept", C.c_void_p), ("y", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
 
 
 class GatedFfnGrad(C.Structure):
     _fields_ = [("d_y", C.c_void_p), ("d_y_stride", C.c_int64), ("d_x", C.c_void_p), ("d_w_gate", C.c_void_p),
-                ("d_w_up", C.c_void_p), ("d_w_down", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+                ("d_w_up", C.c_void_p), ("d_w_down", C.c_void_p)]
 
 
 RESULT_BYTES = C.sizeof(Result)
@@ -164,7 +165,7 @@ def library():
     L.mmee_alu_peak.argtypes = [C.POINTER(C.c_double)]
     L.mmee_gated_ffn.argtypes = [C.POINTER(Workload), C.POINTER(GatedFfn), C.c_void_p]
     L.mmee_gated_ffn_backward.argtypes = [C.POINTER(Workload), C.POINTER(GatedFfn), C.POINTER(GatedFfnGrad), C.c_void_p]
-    L.mmee_gated_ffn_workspace.argtypes = [C.POINTER(Workload), C.POINTER(C.c_uint64)]
+    L.mmee_gated_ffn_workspace.argtypes = [C.POINTER(Workload), C.c_uint32, C.POINTER(C.c_uint64)]
     L.mmee_attention.argtypes = [C.POINTER(Workload), C.POINTER(Attention), C.c_void_p]
     L.mmee_attention_workspace.argtypes = [C.POINTER(Workload), C.POINTER(C.c_uint64)]
     L.mmee_attention_backward.argtypes = [C.POINTER(Workload), C.POINTER(Attention), C.POINTER(AttentionGrad), C.c_void_p]
@@ -424,7 +425,7 @@ def _there(t, stream):
 # The call structs as bytes, in the layouts of Workload, Attention, AttentionGrad, GatedFfn and GatedFfnGrad: filling a
 # ctypes struct field by field takes several times as long (the calls below are made once per layer and token).
 _WORKLOAD, _ATTENTION, _ATTENTION_GRAD = struct.Struct("=8I").pack, struct.Struct("=If4Q12q4Q").pack, struct.Struct("=4Q12q2Q").pack
-_FFN, _FFN_GRAD = struct.Struct("=2I4Q4q3Q").pack, struct.Struct("=Qq6Q").pack
+_FFN, _FFN_GRAD = struct.Struct("=2I4Q4q5Q").pack, struct.Struct("=Qq4Q").pack
 
 
 class _ChainCalls:
@@ -438,7 +439,7 @@ class _ChainCalls:
             setattr(self, name, f)
         for name in ("attention_workspace", "attention_backward_workspace", "gated_ffn_workspace"):
             f = L["mmee_" + name]
-            f.argtypes = [C.c_char_p, C.c_void_p]
+            f.argtypes = [C.c_char_p] + [C.c_uint32] * (name == "gated_ffn_workspace") + [C.c_void_p]
             setattr(self, name, f)
 
 
@@ -452,10 +453,10 @@ def _chain():
     return _chain_calls
 
 
-def _space(ask, workload, like, where):
+def _space(ask, like, where, *args):
     """Workspace for one call (None: it needs none) and its size."""
     need = C.c_uint64()
-    code = ask(workload, C.addressof(need))
+    code = ask(*args, C.addressof(need))
     if code:
         _check(code, where)
     return (_torch.empty(need.value, dtype=_torch.uint8, device=like.device) if need.value else None), need.value
@@ -486,7 +487,7 @@ def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
     batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v = _attention_sizes(where, q, k, v, kv_len)
     calls = _chain()
     w = _WORKLOAD(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v, 2)
-    space, need = _space(calls.attention_workspace, w, q, where)
+    space, need = _space(calls.attention_workspace, q, where, w)
     o = q.new_empty((batch, seq_q, q_heads, d_v))
     lse = _torch.empty((batch, q_heads, seq_q), dtype=_torch.float32, device=q.device)
     a = _ATTENTION(code, (d_qk or 1) ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
@@ -514,7 +515,7 @@ def mmee_attention_backward(d_o, q, k, v, o, lse, kv_len=None, scale=None, strea
         _refuse(where, "lse is what the forward call for these tensors returned")
     calls = _chain()
     w = _WORKLOAD(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v, 2)
-    space, need = _space(calls.attention_backward_workspace, w, q, where)
+    space, need = _space(calls.attention_backward_workspace, q, where, w)
     d_q, d_k, d_v_ = q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(v.shape)
     a = _ATTENTION(code, (d_qk or 1) ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
                    *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], lse.data_ptr(),
@@ -548,8 +549,9 @@ def mmee_gated_ffn(x, w_gate, w_up, w_down, activation: int = ACT_SILU, save: bo
     w = _WORKLOAD(1, 1, 1, tokens, d_ff, d_in, d_out, 2)
     hidden, y = x.new_empty((tokens, d_ff)), x.new_empty((tokens, d_out))
     kept = _torch.empty((2, tokens, d_ff), dtype=_torch.float32, device=x.device) if save else None
+    space, need = _space(calls.gated_ffn_workspace, x, where, w, 0)
     f = _FFN(code, activation, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), x.stride(0), w_gate.stride(0),
-             w_up.stride(0), w_down.stride(0), hidden.data_ptr(), kept.data_ptr() if save else 0, y.data_ptr())
+             w_up.stride(0), w_down.stride(0), hidden.data_ptr(), kept.data_ptr() if save else 0, y.data_ptr(), space.data_ptr() if need else 0, need)
     code = calls.gated_ffn(w, f, _current_stream())
     if code:
         _check(code, where)
@@ -575,11 +577,12 @@ def mmee_gated_ffn_backward(d_y, x, w_gate, w_up, w_down, saved, activation: int
         _refuse(where, "saved is not what the forward call for these tensors returned")
     calls = _chain()
     w = _WORKLOAD(1, 1, 1, tokens, d_ff, d_in, d_out, 2)
-    space, need = _space(calls.gated_ffn_workspace, w, x, where)
+    space, need = _space(calls.gated_ffn_workspace, x, where, w, 1)
     grads = tuple([x.new_empty(t.shape) for t in (x, w_gate, w_up, w_down)])
     f = _FFN(code, activation, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), x.stride(0), w_gate.stride(0),
-             w_up.stride(0), w_down.stride(0), hidden.data_ptr(), kept.data_ptr(), 0)
-    g = _FFN_GRAD(d_y.data_ptr(), d_y.stride(0), *[t.data_ptr() for t in grads], space.data_ptr() if need else 0, need)
+             w_up.stride(0), w_down.stride(0), hidden.data_ptr(), kept.data_ptr(), 0,
+             space.data_ptr() if need else 0, need)
+    g = _FFN_GRAD(d_y.data_ptr(), d_y.stride(0), *[t.data_ptr() for t in grads])
     code = calls.gated_ffn_backward(w, f, g, _current_stream())
     if code:
         _check(code, where)

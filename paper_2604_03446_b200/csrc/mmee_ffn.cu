@@ -24,17 +24,19 @@ struct Product {
     uint32_t m, n;                     // results: rows, columns (kGate: columns of h)
     uint32_t chunks0, chunks1;         // steps of 64 along the reduction, first and second pair of operands
     uint32_t tiles_m, tiles_n, end;    // `end`: tiles of the launch up to here
+    uint32_t splits, part_chunks;      // kPlain: parts of the reduction, steps of each; parts are added up afterwards
     uint32_t a_mn, b_mn;               // the operand lies with the reduction along its columns
     uint32_t act;
     void *out, *out2;                  // kPlain: the product; kGate: h; kGrad: dg, du
     int64_t out_stride;                // elements from row to row of out and out2
+    float* parts;                      // splits > 1: [splits][m][n]
     float *gate, *up;                  // kGate: where to keep them, or null; kGrad: what was kept.  Rows of n
 };
 
 constexpr uint32_t kMostProducts = 4;
 struct Products {
     CUtensorMap a0[kMostProducts], b0[kMostProducts], a1[kMostProducts], b1[kMostProducts];
-    CUtensorMap out[kMostProducts];
+    CUtensorMap out[kMostProducts];    // the result, or its parts
     CUtensorMap out2, gate, up;        // kGate, kGrad: of the only product
     Product of[kMostProducts];
     uint32_t count;
@@ -57,8 +59,10 @@ struct TileShape {
 constexpr uint32_t kGroupRows = 2048;  // result rows that are gone through together, so that their operands stay in L2
 
 template <uint32_t TM>
-__device__ __forceinline__ void tile_of(const Product& p, uint32_t i, uint32_t* tm, uint32_t* tn) {
+__device__ __forceinline__ void tile_of(const Product& p, uint32_t i, uint32_t* tm, uint32_t* tn, uint32_t* split) {
     constexpr uint32_t kGroup = kGroupRows / TM;
+    *split = i / (p.tiles_m * p.tiles_n);
+    i -= *split * (p.tiles_m * p.tiles_n);
     const uint32_t per = kGroup * p.tiles_n, g = i / per, first = g * kGroup;
     const uint32_t rows = min(kGroup, p.tiles_m - first), r = i - g * per;
     *tm = first + r % rows;
@@ -113,6 +117,7 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
     tcgen05_fence_after();
     const uint32_t tmem = tmem_base;
     volatile uint32_t* const lost = &gave_up;
+    asm volatile("griddepcontrol.launch_dependents;");
     const uint32_t n_tiles = ps.of[ps.count - 1].end;
     // The product that tile i is part of, and the tile's number there.
     auto product_of = [&](uint32_t i, uint32_t* at) {
@@ -131,15 +136,17 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
 
     if (warp == 4) {                                   // operands
         if (elect_one()) {
+            asm volatile("griddepcontrol.wait;" ::: "memory");         // (operands may come from the kernel before)
             uint32_t it = 0;
             bool sound = true;
             for (uint32_t i = worker; i < n_tiles && sound; i += workers) {
-                uint32_t at, tm, tn;
+                uint32_t at, tm, tn, split;
                 const uint32_t k = product_of(i, &at);
                 const Product& p = ps.of[k];
-                tile_of<Shape::kM>(p, at, &tm, &tn);
+                tile_of<Shape::kM>(p, at, &tm, &tn, &split);
                 const int32_t m0 = (int32_t)(tm * Shape::kM + rank * 128), n0 = (int32_t)(tn * kCols + (EPI == kGate ? 0 : rank * Shape::kRowsB));
-                for (uint32_t c = 0; c < p.chunks0 + p.chunks1; ++c, ++it) {
+                const uint32_t end = min((split + 1) * p.part_chunks, p.chunks0 + p.chunks1);
+                for (uint32_t c = split * p.part_chunks; c < end; ++c, ++it) {
                     const uint32_t s = it % kStages;
                     if (!mbar_wait(empty(s), ((it / kStages) & 1) ^ 1, lost)) {
                         sound = false;
@@ -186,7 +193,8 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
             const uint32_t b = n & 1;
             uint32_t at;
             const Product& p = ps.of[product_of(i, &at)];
-            const uint32_t chunks = p.chunks0 + p.chunks1, desc = mma_desc(BF16, Shape::kM, TN, p.a_mn, p.b_mn);
+            const uint32_t split = at / (p.tiles_m * p.tiles_n), chunks = min(p.part_chunks, p.chunks0 + p.chunks1 - split * p.part_chunks);
+            const uint32_t desc = mma_desc(BF16, Shape::kM, TN, p.a_mn, p.b_mn);
             const uint64_t step_a = p.a_mn ? kStepMN : kStepK, step_b = p.b_mn ? kStepMN : kStepK;
             if (!mbar_wait(acc_empty(b), ((n >> 1) & 1) ^ 1, lost)) break;
             tcgen05_fence_after();
@@ -228,10 +236,10 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
         };
         for (uint32_t i = worker; i < n_tiles; i += workers, ++n) {
             const uint32_t b = n & 1;
-            uint32_t at, tm, tn;
+            uint32_t at, tm, tn, split;
             const uint32_t k = product_of(i, &at);
             const Product& p = ps.of[k];
-            tile_of<Shape::kM>(p, at, &tm, &tn);
+            tile_of<Shape::kM>(p, at, &tm, &tn, &split);
             const uint32_t row0 = tm * Shape::kM + rank * 128 + warp * 32, col0 = tn * kCols;
             const uint32_t cols = row0 < p.m ? min(kCols, p.n - col0) : 0;     // of this warp's rows, inside
             auto ask_kept = [&](uint32_t c, uint32_t piece) {          // gate and up of 32 columns
@@ -264,7 +272,21 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
                     if (EPI == kGate) tmem_load32(acc + TN / 2 + d, y);
                     tmem_loaded32(x);
                     if (EPI == kGate) tmem_loaded32(y);
-                    if (EPI == kPlain) {
+                    if (EPI == kPlain && p.splits > 1) {
+                        if (d < cols) {                // a part, in 32 bits
+                            const uint32_t to = part(stores & 1);
+                            if (lane == 0) tma_store_read<1>();
+                            __syncwarp();
+#pragma unroll
+                            for (uint32_t j = 0; j < 8; ++j) store_shared16(swizzled(to, lane, j), x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+                            ready();
+                            if (lane == 0) {
+                                tma_store_3d(&ps.out[k], to, (int32_t)(col0 + d), (int32_t)row0, (int32_t)split);
+                                tma_store_commit();
+                            }
+                            ++stores;
+                        }
+                    } else if (EPI == kPlain) {
 #pragma unroll
                         for (int j = 0; j < 16; ++j) o[16 * half + j] = pack2<BF16>(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
                     } else if (EPI == kGate) {
@@ -319,7 +341,7 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
                         ++kept;
                     }
                 }
-                if (c >= cols) continue;               // (the same for the whole warp)
+                if (c >= cols || (EPI == kPlain && p.splits > 1)) continue;        // (the same for the whole warp)
                 const uint32_t to = EPI == kGrad ? part(0) : part(stores & 1);
                 if (lane == 0) {
                     if (EPI == kGrad)
@@ -393,8 +415,49 @@ void add_product(Products* ps, Operand* (&ops)[kMostProducts][4], Product p, Ope
     ps->of[ps->count++] = p;
 }
 
+// Adds the parts of a product up, in order: eight values of a row to a thread.
+template <bool BF16>
+__global__ void __launch_bounds__(256) join_parts_kernel(const float* parts, uint32_t splits, uint32_t m, uint32_t n, void* out, int64_t out_stride) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    const uint64_t size = (uint64_t)m * n, at = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (at >= size) return;
+    float4 sum[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 4
+    for (uint32_t s = 0; s < splits; ++s) {
+        const float4* const from = reinterpret_cast<const float4*>(parts + s * size + at);
+        const float4 x = __ldcg(from), y = __ldcg(from + 1);
+        sum[0].x += x.x, sum[0].y += x.y, sum[0].z += x.z, sum[0].w += x.w;
+        sum[1].x += y.x, sum[1].y += y.y, sum[1].z += y.z, sum[1].w += y.w;
+    }
+    uint16_t* const to = static_cast<uint16_t*>(out) + (int64_t)(at / n) * out_stride + at % n;
+    *reinterpret_cast<uint4*>(to) = make_uint4(pack2<BF16>(sum[0].x, sum[0].y), pack2<BF16>(sum[0].z, sum[0].w), pack2<BF16>(sum[1].x, sum[1].y),
+                                               pack2<BF16>(sum[1].z, sum[1].w));
+}
+
+// Cuts the reductions of products of few tiles into parts, so that no pair of CTAs has much more to do than its share of the launch; parts
+// of eight steps at least.  Returns the values of all parts.
+// 512 tokens, 1024-4096-1024: the down product is 8 tiles of 64 steps each, and took 24 us on 8 of 74 pairs.
+uint64_t cut_up(Products* ps, uint32_t sms) {
+    const uint32_t pairs = sms / 2;
+    uint64_t all = 0, values = 0;
+    for (uint32_t i = 0; i < ps->count; ++i) {
+        const Product& p = ps->of[i];
+        all += ceil_div(p.m, 256) * ceil_div(p.n, 256) * (p.chunks0 + p.chunks1);
+    }
+    const uint32_t share = (uint32_t)max(ceil_div(all, pairs), (uint64_t)8);
+    for (uint32_t i = 0; i < ps->count; ++i) {
+        Product& p = ps->of[i];
+        const uint32_t chunks = p.chunks0 + p.chunks1, splits = min((uint32_t)ceil_div(chunks, share), 8u);
+        p.part_chunks = (uint32_t)ceil_div(chunks, splits);
+        p.splits = (uint32_t)ceil_div(chunks, p.part_chunks);
+        if (p.splits > 1) values += (uint64_t)p.splits * p.m * p.n;
+    }
+    return values;
+}
+
 template <int EPI, bool PAIR, int TN, bool BF16>
-int launch_products(Products& ps, Operand* (&ops)[kMostProducts][4], uint32_t sms, cudaStream_t stream) {
+int launch_products(Products& ps, Operand* (&ops)[kMostProducts][4], uint32_t sms, bool early, float* parts, cudaStream_t stream) {
     using Shape = TileShape<EPI, PAIR, TN>;
     constexpr uint32_t kRowsX = EPI == kGate && !PAIR ? TN / 2 : Shape::kRowsB;
     uint32_t end = 0;
@@ -403,7 +466,7 @@ int launch_products(Products& ps, Operand* (&ops)[kMostProducts][4], uint32_t sm
         Product& p = ps.of[i];
         p.tiles_m = (uint32_t)ceil_div(p.m, Shape::kM);
         p.tiles_n = (uint32_t)ceil_div(p.n, EPI == kGate ? TN / 2 : TN);
-        p.end = end += p.tiles_m * p.tiles_n;
+        p.end = end += p.tiles_m * p.tiles_n * p.splits;
         CUtensorMap* const maps[4] = {&ps.a0[i], &ps.b0[i], &ps.a1[i], &ps.b1[i]};
         for (int k = 0; k < 4 && !rc; ++k) {
             const Operand* const o = ops[i][k];
@@ -411,33 +474,49 @@ int launch_products(Products& ps, Operand* (&ops)[kMostProducts][4], uint32_t sm
             const uint64_t extent[2] = {o->cols, o->rows};
             rc = tile_map(maps[k], BF16, o->base, 2, extent, &o->stride, o->mn ? 64 : k % 2 ? min(128u, kRowsX) : 128);
         }
-        const uint64_t result[2] = {p.n, p.m};
-        if (!rc) rc = tile_map(&ps.out[i], BF16, p.out, 2, result, &p.out_stride, 32);
+        const uint64_t result[3] = {p.n, p.m, p.splits};
+        const int64_t packed[2] = {p.n, (int64_t)p.m * p.n};
+        if (p.splits > 1) {
+            p.parts = parts;
+            parts += (uint64_t)p.splits * p.m * p.n;
+        }
+        if (!rc) rc = p.splits > 1 ? tile_map(&ps.out[i], Values::f32, p.parts, 3, result, packed, 32) : tile_map(&ps.out[i], BF16, p.out, 2, result, &p.out_stride, 32);
         if (!rc && EPI == kGrad) rc = tile_map(&ps.out2, BF16, p.out2, 2, result, &p.out_stride, 32);
-        const int64_t n = p.n;
-        if (!rc && p.gate) rc = tile_map(&ps.gate, Values::f32, p.gate, 2, result, &n, 32);
-        if (!rc && p.gate) rc = tile_map(&ps.up, Values::f32, p.up, 2, result, &n, 32);
+        if (!rc && p.gate) rc = tile_map(&ps.gate, Values::f32, p.gate, 2, result, packed, 32);
+        if (!rc && p.gate) rc = tile_map(&ps.up, Values::f32, p.up, 2, result, packed, 32);
     }
     if (rc) return rc;
-    const LaunchAt at{dim3(PAIR ? 2 * min(sms / 2, end) : min(sms, end)), 192, Shape::smem, PAIR ? 2u : 1u, false, stream};
-    return launch<product_kernel<EPI, PAIR, TN, BF16>>(at, ps);
+    const LaunchAt at{dim3(PAIR ? 2 * min(sms / 2, end) : min(sms, end)), 192, Shape::smem, PAIR ? 2u : 1u, early, stream};
+    rc = launch<product_kernel<EPI, PAIR, TN, BF16>>(at, ps);
+    for (uint32_t i = 0; i < ps.count && !rc; ++i) {
+        const Product& p = ps.of[i];
+        if (p.splits == 1) continue;
+        const LaunchAt join{dim3((uint32_t)ceil_div((uint64_t)p.m * p.n, 8 * 256)), 256, 0, 1, true, stream};
+        rc = launch<join_parts_kernel<BF16>>(join, (const float*)p.parts, p.splits, p.m, p.n, p.out, p.out_stride);
+    }
+    return rc;
 }
 
-// Tiles of 256 x 256 by pairs of CTAs where there are enough of them; smaller ones where that would leave multiprocessors idle.
+// Tiles of 256 x 256 by pairs of CTAs.  The kernels with work at the end of a tile take tiles of 128 x 128 by single CTAs where the large ones
+// would leave multiprocessors idle (us, large and small: gate of 512 x 4096 x 1024, 64 large tiles, 15 and 18; gradient, 32 tiles, 22 and 17;
+// gradient of 2048 x 4096 x 1024, 128 tiles, 39 and 43).  `early`: the kernel before it in the stream is one of this call.
+// parts: room for what cut_up says.
 template <int EPI>
-int products(bool bf16, Products& ps, Operand* (&ops)[kMostProducts][4], cudaStream_t stream) {
+int products(bool bf16, Products& ps, Operand* (&ops)[kMostProducts][4], bool early, float* parts, cudaStream_t stream) {
     uint32_t sms;
     const int rc = sm_count(&sms);
     if (rc) return rc;
-    uint64_t large = 0, middle = 0;
-    for (uint32_t i = 0; i < ps.count; ++i) {
-        const uint64_t n = EPI == kGate ? 2ull * ps.of[i].n : ps.of[i].n;
-        large += ceil_div(ps.of[i].m, 256) * ceil_div(n, 256);
-        middle += ceil_div(ps.of[i].m, 128) * ceil_div(n, 256);
+    if constexpr (EPI == kPlain) {
+        cut_up(&ps, sms);
+    } else {
+        Product& p = ps.of[0];
+        p.splits = 1;
+        p.part_chunks = p.chunks0 + p.chunks1;
+        const uint64_t large = ceil_div(p.m, 256) * ceil_div(p.n, EPI == kGate ? 128 : 256);
+        if (large < (EPI == kGate ? sms / 4 : sms / 2))
+            return bf16 ? launch_products<EPI, false, 128, true>(ps, ops, sms, early, parts, stream) : launch_products<EPI, false, 128, false>(ps, ops, sms, early, parts, stream);
     }
-    if (large >= sms / 2) return bf16 ? launch_products<EPI, true, 256, true>(ps, ops, sms, stream) : launch_products<EPI, true, 256, false>(ps, ops, sms, stream);
-    (void)middle;
-    return bf16 ? launch_products<EPI, false, 128, true>(ps, ops, sms, stream) : launch_products<EPI, false, 128, false>(ps, ops, sms, stream);
+    return bf16 ? launch_products<EPI, true, 256, true>(ps, ops, sms, early, parts, stream) : launch_products<EPI, true, 256, false>(ps, ops, sms, early, parts, stream);
 }
 
 Product plain(uint32_t m, uint32_t n, void* out) {
@@ -473,6 +552,77 @@ int check(const mmee_workload_t* w, const mmee_gated_ffn_t* f, Sizes* s) {
     return MMEE_OK;
 }
 
+// The products of one launch with their operands.
+struct Plan {
+    Products ps;
+    Operand* ops[kMostProducts][4];
+    Operand held[10];
+};
+
+void plan_forward(const Sizes& s, const mmee_gated_ffn_t& f, Plan* gate, Plan* down) {
+    Operand* const g = gate->held;
+    g[0] = {f.x, s.tokens, s.d_in, f.x_stride, false};
+    g[1] = {f.w_gate, s.d_ff, s.d_in, f.w_gate_stride, false};
+    g[2] = {f.w_up, s.d_ff, s.d_in, f.w_up_stride, false};
+    Product p = plain(s.tokens, s.d_ff, f.hidden);
+    p.act = f.activation;
+    p.gate = f.kept;
+    p.up = f.kept ? f.kept + (uint64_t)s.tokens * s.d_ff : nullptr;
+    gate->ps.count = 0;
+    add_product(&gate->ps, gate->ops, p, &g[0], &g[1], nullptr, &g[2]);
+    Operand* const d = down->held;
+    d[0] = {f.hidden, s.tokens, s.d_ff, s.d_ff, false};
+    d[1] = {f.w_down, s.d_out, s.d_ff, f.w_down_stride, false};
+    down->ps.count = 0;
+    add_product(&down->ps, down->ops, plain(s.tokens, s.d_out, f.y), &d[0], &d[1], nullptr, nullptr);
+}
+
+void plan_backward(const Sizes& s, const mmee_gated_ffn_t& f, const mmee_gated_ffn_grad_t& g, Plan* grad, Plan* rest) {
+    const uint64_t inner = (uint64_t)s.tokens * s.d_ff;            // (a multiple of eight)
+    uint16_t* const dg = static_cast<uint16_t*>(f.workspace);
+    uint16_t* const du = dg ? dg + inner : nullptr;
+    Operand* const o = grad->held;
+    o[0] = {g.d_y, s.tokens, s.d_out, g.d_y_stride, false};
+    o[1] = {f.w_down, s.d_out, s.d_ff, f.w_down_stride, true};
+    Product p = plain(s.tokens, s.d_ff, dg);
+    p.out2 = du;
+    p.act = f.activation;
+    p.gate = f.kept;
+    p.up = f.kept ? f.kept + inner : nullptr;
+    grad->ps.count = 0;
+    add_product(&grad->ps, grad->ops, p, &o[0], &o[1], nullptr, nullptr);
+    // The other four products depend on nothing but these, and are one launch: the one with the longest reduction first.
+    Operand* const r = rest->held;
+    r[0] = {dg, s.tokens, s.d_ff, s.d_ff, false};
+    r[1] = {du, s.tokens, s.d_ff, s.d_ff, false};
+    r[2] = {f.w_gate, s.d_ff, s.d_in, f.w_gate_stride, true};
+    r[3] = {f.w_up, s.d_ff, s.d_in, f.w_up_stride, true};
+    r[4] = {dg, s.tokens, s.d_ff, s.d_ff, true};
+    r[5] = {du, s.tokens, s.d_ff, s.d_ff, true};
+    r[6] = {f.x, s.tokens, s.d_in, f.x_stride, true};
+    r[7] = {f.hidden, s.tokens, s.d_ff, s.d_ff, true};
+    r[8] = {g.d_y, s.tokens, s.d_out, g.d_y_stride, true};
+    rest->ps.count = 0;
+    add_product(&rest->ps, rest->ops, plain(s.tokens, s.d_in, g.d_x), &r[0], &r[2], &r[1], &r[3]);
+    add_product(&rest->ps, rest->ops, plain(s.d_ff, s.d_in, g.d_w_gate), &r[4], &r[6], nullptr, nullptr);
+    add_product(&rest->ps, rest->ops, plain(s.d_ff, s.d_in, g.d_w_up), &r[5], &r[6], nullptr, nullptr);
+    add_product(&rest->ps, rest->ops, plain(s.d_out, s.d_ff, g.d_w_down), &r[8], &r[7], nullptr, nullptr);
+}
+
+// Workspace of a call: `fixed` bytes and the parts of the plan's products.
+int space_of(Plan* plan, uint64_t fixed, uint64_t* bytes) {
+    uint32_t sms;
+    const int rc = sm_count(&sms);
+    if (!rc) *bytes = fixed + 4 * cut_up(&plan->ps, sms);
+    return rc;
+}
+
+int check_space(const void* space, uint64_t bytes, Plan* plan, uint64_t fixed) {
+    uint64_t need = 0;
+    const int rc = space_of(plan, fixed, &need);
+    return rc ? rc : need && (!space || !aligned16(space) || bytes < need) ? MMEE_ERR_ARG : MMEE_OK;
+}
+
 }  // namespace
 
 int ffn_gave_up(uint32_t* word) {
@@ -499,25 +649,11 @@ extern "C" int mmee_gated_ffn(const mmee_workload_t* workload, const mmee_gated_
         const uint64_t bytes = 2ull * s.d_ff * (2ull * s.d_in + s.d_out);
         return s.tokens <= kFew && bytes < kFewBytes ? ffn_tokens(few, bf16, stream) : ffn_narrow(few, bf16, stream);
     }
-    Operand x{f->x, s.tokens, s.d_in, f->x_stride, false}, wg{f->w_gate, s.d_ff, s.d_in, f->w_gate_stride, false};
-    Operand wu{f->w_up, s.d_ff, s.d_in, f->w_up_stride, false}, wd{f->w_down, s.d_out, s.d_ff, f->w_down_stride, false};
-    Operand h{f->hidden, s.tokens, s.d_ff, s.d_ff, false};
-    Operand* ops[kMostProducts][4];
-    Products ps;
-    Product p{};
-    p.m = s.tokens;
-    p.n = s.d_ff;
-    p.act = f->activation;
-    p.out = f->hidden;
-    p.out_stride = s.d_ff;
-    p.gate = f->kept;
-    p.up = f->kept ? f->kept + (uint64_t)s.tokens * s.d_ff : nullptr;
-    ps.count = 0;
-    add_product(&ps, ops, p, &x, &wg, nullptr, &wu);
-    if ((rc = products<kGate>(bf16, ps, ops, stream))) return rc;
-    ps.count = 0;
-    add_product(&ps, ops, plain(s.tokens, s.d_out, f->y), &h, &wd, nullptr, nullptr);
-    return products<kPlain>(bf16, ps, ops, stream);
+    Plan gate, down;
+    plan_forward(s, *f, &gate, &down);
+    if ((rc = check_space(f->workspace, f->workspace_bytes, &down, 0))) return rc;
+    if ((rc = products<kGate>(bf16, gate.ps, gate.ops, false, nullptr, stream))) return rc;
+    return products<kPlain>(bf16, down.ps, down.ops, true, static_cast<float*>(f->workspace), stream);
 }
 
 extern "C" int mmee_gated_ffn_backward(const mmee_workload_t* workload, const mmee_gated_ffn_t* f, const mmee_gated_ffn_grad_t* g,
@@ -530,43 +666,26 @@ extern "C" int mmee_gated_ffn_backward(const mmee_workload_t* workload, const mm
     void* outs[4] = {g->d_x, g->d_w_gate, g->d_w_up, g->d_w_down};
     for (void* o : outs)
         if (!o || !aligned16(o)) return MMEE_ERR_ARG;
-    const uint64_t inner = (uint64_t)s.tokens * s.d_ff;
-    if (!g->workspace || !aligned16(g->workspace) || g->workspace_bytes < 4 * inner) return MMEE_ERR_ARG;
+    Plan grad, rest;
+    plan_backward(s, *f, *g, &grad, &rest);
+    const uint64_t inner = 4 * (uint64_t)s.tokens * s.d_ff;        // bytes of dg and du
+    if ((rc = check_space(f->workspace, f->workspace_bytes, &rest, inner))) return rc;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool bf16 = f->dtype == MMEE_BF16;
-    uint16_t* const dg = static_cast<uint16_t*>(g->workspace);
-    uint16_t* const du = dg + inner;                   // (inner is a multiple of eight)
-    Operand wd{f->w_down, s.d_out, s.d_ff, f->w_down_stride, true}, dy{g->d_y, s.tokens, s.d_out, g->d_y_stride, false};
-    Operand* ops[kMostProducts][4];
-    Products ps;
-    Product p{};
-    p.m = s.tokens;
-    p.n = s.d_ff;
-    p.act = f->activation;
-    p.out = dg;
-    p.out2 = du;
-    p.out_stride = s.d_ff;
-    p.gate = f->kept;
-    p.up = f->kept + inner;
-    ps.count = 0;
-    add_product(&ps, ops, p, &dy, &wd, nullptr, nullptr);
-    if ((rc = products<kGrad>(bf16, ps, ops, stream))) return rc;
-    // The other four products depend on nothing but these, and are one launch: the one with the longest reduction first.
-    Operand dg_x{dg, s.tokens, s.d_ff, s.d_ff, false}, du_x{du, s.tokens, s.d_ff, s.d_ff, false};
-    Operand wg{f->w_gate, s.d_ff, s.d_in, f->w_gate_stride, true}, wu{f->w_up, s.d_ff, s.d_in, f->w_up_stride, true};
-    Operand dg_w{dg, s.tokens, s.d_ff, s.d_ff, true}, du_w{du, s.tokens, s.d_ff, s.d_ff, true};
-    Operand x{f->x, s.tokens, s.d_in, f->x_stride, true}, h{f->hidden, s.tokens, s.d_ff, s.d_ff, true};
-    dy.mn = true;
-    ps.count = 0;
-    add_product(&ps, ops, plain(s.tokens, s.d_in, g->d_x), &dg_x, &wg, &du_x, &wu);
-    add_product(&ps, ops, plain(s.d_ff, s.d_in, g->d_w_gate), &dg_w, &x, nullptr, nullptr);
-    add_product(&ps, ops, plain(s.d_ff, s.d_in, g->d_w_up), &du_w, &x, nullptr, nullptr);
-    add_product(&ps, ops, plain(s.d_out, s.d_ff, g->d_w_down), &dy, &h, nullptr, nullptr);
-    return products<kPlain>(bf16, ps, ops, stream);
+    if ((rc = products<kGrad>(bf16, grad.ps, grad.ops, false, nullptr, stream))) return rc;
+    return products<kPlain>(bf16, rest.ps, rest.ops, true, reinterpret_cast<float*>(static_cast<char*>(f->workspace) + inner), stream);
 }
 
-extern "C" int mmee_gated_ffn_workspace(const mmee_workload_t* w, uint64_t* bytes) {
-    if (!w || !bytes) return MMEE_ERR_ARG;
-    *bytes = 4 * (uint64_t)w->seq_q * w->seq_kv;
-    return MMEE_OK;
+extern "C" int mmee_gated_ffn_workspace(const mmee_workload_t* w, uint32_t backward, uint64_t* bytes) {
+    if (!w || !bytes || backward > 1) return MMEE_ERR_ARG;
+    const Sizes s{w->seq_q, w->d_qk, w->seq_kv, w->d_v};
+    if (!s.tokens || !s.d_in || !s.d_ff || !s.d_out) return MMEE_ERR_ARG;
+    *bytes = 0;
+    if (!backward && s.tokens <= kNarrow) return MMEE_OK;
+    Plan first, rest;
+    if (backward)
+        plan_backward(s, mmee_gated_ffn_t{}, mmee_gated_ffn_grad_t{}, &first, &rest);
+    else
+        plan_forward(s, mmee_gated_ffn_t{}, &first, &rest);
+    return space_of(&rest, backward ? 4 * (uint64_t)s.tokens * s.d_ff : 0, bytes);
 }

@@ -4,6 +4,7 @@ Bounds: a value rounded to the operands' type is off by at most u = eps / 2 of i
 |dy| <= u (|hidden| |Wd|^T + |y|); the gradients of gate and up are rounded once before they enter a product, whose result is
 rounded once.  32-bit sums of n products are off by at most n 2^-23 of the sum of their sizes (2^-23, not 2^-24: the tensor
 cores may cut off instead of rounding), and the activations, from approximate exponentials, by 2^-18 of their size."""
+import ctypes as C
 import math
 
 import pytest
@@ -19,7 +20,7 @@ ACT32 = 2.0 ** -18
 SIZES = [                                  # tokens, in, inner, out
     (1, 64, 64, 64), (1, 8, 8, 8), (8, 4096, 8192, 4096), (2, 16, 8, 24), (5, 72, 136, 40), (8, 256, 512, 256), (9, 264, 520, 8), (16, 1024, 2048, 512),
     (17, 64, 384, 64), (33, 200, 264, 712), (64, 512, 128, 1032), (127, 136, 248, 72), (128, 64, 256, 128), (129, 192, 384, 264),
-    (300, 328, 1000, 520), (777, 1000, 2728, 712), (768, 64, 384, 64), (2048, 256, 1024, 512), (1500, 520, 4100 - 4, 1000), (4100, 264, 2056, 136),
+    (300, 328, 1000, 520), (777, 1000, 2728, 712), (768, 64, 384, 64), (2048, 256, 1024, 512), (1500, 520, 4100 - 4, 1000), (4100, 264, 2056, 136), (200, 2048, 4104, 520), (512, 1024, 4096, 1024),
 ]
 
 
@@ -215,8 +216,8 @@ class _Case:
         self.b = b
         self.w = b.Workload(batch=1, q_heads=1, kv_heads=1, seq_q=4, seq_kv=64, d_qk=32, d_v=16, word_bytes=2)
         self.f = b.GatedFfn(dtype=b.BF16, activation=0, x=4096, w_gate=4096, w_up=4096, w_down=4096, x_stride=32, w_gate_stride=32,
-                            w_up_stride=32, w_down_stride=64, hidden=4096, kept=4096, y=4096)
-        self.g = b.GatedFfnGrad(4096, 16, 4096, 4096, 4096, 4096, 4096, 4 * 4 * 64)
+                            w_up_stride=32, w_down_stride=64, hidden=4096, kept=4096, y=4096, workspace=4096, workspace_bytes=4 * 4 * 64)
+        self.g = b.GatedFfnGrad(4096, 16, 4096, 4096, 4096, 4096)
 
 
 BAD = [("w", "batch", 2), ("w", "q_heads", 2), ("w", "kv_heads", 2), ("w", "seq_q", 0), ("w", "seq_kv", 0), ("w", "d_qk", 0),
@@ -236,11 +237,10 @@ def test_bad_arguments_are_refused(where, field, value):
 
 
 @pytest.mark.parametrize("field,value", [("d_y", 0), ("d_y", 4100), ("d_y_stride", 8), ("d_y_stride", 20), ("d_x", 0), ("d_w_gate", 0),
-                                         ("d_w_up", 4100), ("d_w_down", 0), ("workspace", 0), ("workspace", 4104),
-                                         ("workspace_bytes", 4 * 4 * 64 - 1)])
+                                         ("d_w_up", 4100), ("d_w_down", 0), ("kept", 0), ("kept", 4100)])
 def test_bad_gradient_arguments_are_refused(field, value):
     c = _Case()
-    setattr(c.g, field, value)
+    setattr(c.f if field == "kept" else c.g, field, value)
     assert mm.library().mmee_gated_ffn_backward(c.w, c.f, c.g, None) == mm.ERR_ARG
 
 
@@ -248,7 +248,7 @@ def test_null_and_missing_arguments_are_refused():
     c, lib = _Case(), mm.library()
     assert lib.mmee_gated_ffn(None, c.f, None) == mm.ERR_ARG and lib.mmee_gated_ffn(c.w, None, None) == mm.ERR_ARG
     assert lib.mmee_gated_ffn_backward(c.w, c.f, None, None) == mm.ERR_ARG
-    assert lib.mmee_gated_ffn_workspace(None, None) == mm.ERR_ARG
+    assert lib.mmee_gated_ffn_workspace(None, 0, None) == mm.ERR_ARG
     c.f.y = None
     assert lib.mmee_gated_ffn(c.w, c.f, None) == mm.ERR_ARG
     c.f.kept = None
@@ -264,6 +264,24 @@ def test_tensors_that_do_not_fit_are_refused():
         with pytest.raises(mm.MmeeError) as e:
             mm.mmee_gated_ffn(*bad)
         assert e.value.code == mm.ERR_ARG
+
+
+@gpu
+def test_a_workspace_that_is_missing_short_or_unaligned_is_refused():
+    """(The sizes of workspaces go by the device, so that the check comes after one.)"""
+    lib, need = mm.library(), C.c_uint64()
+    c = _Case()
+    for tokens in (4, 300):
+        c.w.seq_q = tokens
+        for backward in (0, 1):
+            assert lib.mmee_gated_ffn_workspace(c.w, backward, need) == mm.OK
+            if not need.value:
+                continue
+            for at, size in ((0, need.value), (4104, need.value), (4096, need.value - 1)):
+                c.f.workspace, c.f.workspace_bytes = at, size
+                code = lib.mmee_gated_ffn_backward(c.w, c.f, c.g, None) if backward else lib.mmee_gated_ffn(c.w, c.f, None)
+                assert code == mm.ERR_ARG
+    assert lib.mmee_gated_ffn_workspace(c.w, 2, need) == mm.ERR_ARG
 
 
 @gpu
