@@ -452,6 +452,8 @@ typedef struct {
     void    *o;                              /* out (backward: in)                                */
     int64_t  q_stride[3], k_stride[3], v_stride[3], o_stride[3];   /* elements: batch, token, head */
     float   *lse;                            /* out, may be NULL (backward: in): [batch][q_heads][seq_q], contiguous */
+    void    *o_rest;                         /* out, may be NULL (backward: in, may be NULL): [batch][token][q head][d_v], contiguous:
+                                                what the rounding of o took off; with it the backward pass sees o exactly enough */
     const int32_t *kv_len;                   /* DEVICE, one per sequence, clamped to 0..seq_kv; NULL: all keys */
     void    *workspace;                      /* DEVICE, mmee_attention_workspace bytes (0: may be NULL), for this call alone until it ends */
     uint64_t workspace_bytes;

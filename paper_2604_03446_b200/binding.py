@@ -78,7 +78,7 @@ class LaunchStats(C.Structure):
 class Attention(C.Structure):
     _fields_ = [("dtype", C.c_uint32), ("scale", C.c_float), ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
                 ("o", C.c_void_p), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
-                ("o_stride", C.c_int64 * 3), ("lse", C.c_void_p), ("kv_len", C.c_void_p), ("workspace", C.c_void_p),
+                ("o_stride", C.c_int64 * 3), ("lse", C.c_void_p), ("o_rest", C.c_void_p), ("kv_len", C.c_void_p), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_uint64)]
 
 
@@ -424,7 +424,7 @@ def _there(t, stream):
 
 # The call structs as bytes, in the layouts of Workload, Attention, AttentionGrad, GatedFfn and GatedFfnGrad: filling a
 # ctypes struct field by field takes several times as long (the calls below are made once per layer and token).
-_WORKLOAD, _ATTENTION, _ATTENTION_GRAD = struct.Struct("=8I").pack, struct.Struct("=If4Q12q4Q").pack, struct.Struct("=4Q12q2Q").pack
+_WORKLOAD, _ATTENTION, _ATTENTION_GRAD = struct.Struct("=8I").pack, struct.Struct("=If4Q12q5Q").pack, struct.Struct("=4Q12q2Q").pack
 _FFN, _FFN_GRAD = struct.Struct("=2I4Q4q5Q").pack, struct.Struct("=Qq4Q").pack
 
 
@@ -476,9 +476,10 @@ def _attention_sizes(where, q, k, v, kv_len):
 
 
 def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
-    """softmax(scale q k^T) v over each sequence's first kv_len keys: (o, lse).  q: (batch, tokens, q_heads, d_qk), k: (batch, keys,
+    """softmax(scale q k^T) v over each sequence's first kv_len keys: (o, saved).  q: (batch, tokens, q_heads, d_qk), k: (batch, keys,
     kv_heads, d_qk), v: (batch, keys, kv_heads, d_v), bfloat16 or float16; kv_len: int32 tensor with an entry per sequence, None: all keys;
-    scale: d_qk ** -0.5 unless given.  lse: float32 (batch, q_heads, tokens).  Asynchronous."""
+    scale: d_qk ** -0.5 unless given.  saved: what mmee_attention_backward needs; attention_lse(saved, o) is the part of it that is
+    of use elsewhere.  Asynchronous."""
     where = "mmee_attention"
     code = _chain_code(where, 4, q, k, v)
     if stream is not None or _current_device() != q.get_device():
@@ -489,36 +490,48 @@ def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
     w = _WORKLOAD(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v, 2)
     space, need = _space(calls.attention_workspace, q, where, w)
     o = q.new_empty((batch, seq_q, q_heads, d_v))
-    lse = _torch.empty((batch, q_heads, seq_q), dtype=_torch.float32, device=q.device)
+    rows = batch * seq_q * q_heads
+    ahead = (rows + 3) // 4 * 4                        # (what follows the rows' sums starts on sixteen bytes)
+    saved = _torch.empty(ahead + rows * d_v // 2, dtype=_torch.float32, device=q.device)
+    at = saved.data_ptr()
     a = _ATTENTION(code, (d_qk or 1) ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
-                   *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], lse.data_ptr(),
+                   *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], at, at + 4 * ahead,
                    0 if kv_len is None else kv_len.data_ptr(), space.data_ptr() if need else 0, need)
     code = calls.attention(w, a, _current_stream())
     if code:
         _check(code, where)
-    return o, lse
+    return o, saved
 
 
-def mmee_attention_backward(d_o, q, k, v, o, lse, kv_len=None, scale=None, stream=None):
-    """The gradients (d_q, d_k, d_v) of mmee_attention for a gradient d_o of o; o and lse are what the forward call with the same
+def attention_lse(saved, o):
+    """log sum exp(scale q k^T) of every row, float32 (batch, q_heads, tokens), out of what mmee_attention returned beside o."""
+    batch, seq_q, q_heads, _ = o.shape
+    return saved[:batch * q_heads * seq_q].view(batch, q_heads, seq_q)
+
+
+def mmee_attention_backward(d_o, q, k, v, o, saved, kv_len=None, scale=None, stream=None):
+    """The gradients (d_q, d_k, d_v) of mmee_attention for a gradient d_o of o; o and saved are what the forward call with the same
     tensors returned.  Keys behind a sequence's end get zeros.  Asynchronous."""
     where = "mmee_attention_backward"
     code = _chain_code(where, 4, q, k, v, o, d_o)
     if stream is not None or _current_device() != q.get_device():
         with _there(q, stream):
-            return mmee_attention_backward(d_o, q, k, v, o, lse, kv_len, scale)
+            return mmee_attention_backward(d_o, q, k, v, o, saved, kv_len, scale)
     batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v = _attention_sizes(where, q, k, v, kv_len)
     if o.shape != (batch, seq_q, q_heads, d_v) or d_o.shape != o.shape:
         _refuse(where, "o and d_o are (batch, tokens, q_heads, d_v)")
-    if not (isinstance(lse, _torch.Tensor) and lse.shape == (batch, q_heads, seq_q) and lse.dtype is _torch.float32 and
-            lse.get_device() == q.get_device() and lse.is_contiguous()):
-        _refuse(where, "lse is what the forward call for these tensors returned")
+    rows = batch * seq_q * q_heads
+    ahead = (rows + 3) // 4 * 4
+    if not (isinstance(saved, _torch.Tensor) and saved.shape == (ahead + rows * d_v // 2,) and saved.dtype is _torch.float32 and
+            saved.get_device() == q.get_device() and saved.is_contiguous()):
+        _refuse(where, "saved is what the forward call for these tensors returned")
+    at = saved.data_ptr()
     calls = _chain()
     w = _WORKLOAD(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v, 2)
     space, need = _space(calls.attention_backward_workspace, q, where, w)
     d_q, d_k, d_v_ = q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(v.shape)
     a = _ATTENTION(code, (d_qk or 1) ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
-                   *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], lse.data_ptr(),
+                   *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], at, at + 4 * ahead,
                    0 if kv_len is None else kv_len.data_ptr(), 0, 0)
     g = _ATTENTION_GRAD(d_o.data_ptr(), d_q.data_ptr(), d_k.data_ptr(), d_v_.data_ptr(), *d_o.stride()[:3], *d_q.stride()[:3],
                         *d_k.stride()[:3], *d_v_.stride()[:3], space.data_ptr(), need)

@@ -305,6 +305,7 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                         }
                     } else {
                         write_row<BF16>(p.o, to, v, c, p.d_v);
+                        if (p.rest) write_row<BF16, true>(p.rest, rest_at(p, b, token, head), v, c, p.d_v);
                     }
                 }
                 __syncwarp();
@@ -358,7 +359,12 @@ __global__ void __launch_bounds__(128) attention_join_kernel(const AttentionPara
     if (p.lse && lane == 0) p.lse[((uint64_t)b * p.q_heads + head) * p.seq_q + token] = sum == 0.f ? -INFINITY : (from + log2f(sum)) * kLn2;
     if (4 * lane < p.d_v) {
         uint16_t* const to = static_cast<uint16_t*>(p.o) + (int64_t)b * p.os.batch + (int64_t)token * p.os.token + (int64_t)head * p.os.head;
-        *reinterpret_cast<uint2*>(to + 4 * lane) = make_uint2(pack2<BF16>(v[0] * inv, v[1] * inv), pack2<BF16>(v[2] * inv, v[3] * inv));
+        for (float& x : v) x *= inv;
+        const uint2 w = make_uint2(pack2<BF16>(v[0], v[1]), pack2<BF16>(v[2], v[3]));
+        *reinterpret_cast<uint2*>(to + 4 * lane) = w;
+        if (p.rest)
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.rest) + rest_at(p, b, token, head) + 4 * lane) =
+                make_uint2(rest2<BF16>(v[0], v[1], w.x), rest2<BF16>(v[2], v[3], w.y));
     }
 }
 

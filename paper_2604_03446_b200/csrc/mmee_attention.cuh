@@ -32,7 +32,8 @@ struct AttentionParams {
     const int32_t* kv_len;
     void* o;
     Strides os;
-    float* lse;                        // [batch][q_heads][seq_q]
+    float* lse;                        // [batch][q_heads][seq_q], or null
+    void* rest;                        // [batch][seq_q][q_heads][d_v]: what the rounding of o took off, or null
     float *part_o, *part_lse;          // [split][tiles - whole][tile_rows] rows of d_v; log2 of the sums
 };
 
@@ -89,15 +90,33 @@ __device__ __forceinline__ void turned_product(uint32_t to, uint32_t a, uint32_t
     }
 }
 
-// Writes 8 * n values of a row.
+// What a rounding to two 16-bit values took off, rounded to 16 bits itself.
 template <bool BF16>
+__device__ __forceinline__ uint32_t rest2(float lo, float hi, uint32_t rounded) {
+    const float2 r = unpack2<BF16>(rounded);
+    return pack2<BF16>(lo - r.x, hi - r.y);
+}
+
+// Writes 8 * n values of a row; REST: what that rounds off, instead.
+template <bool BF16, bool REST = false>
 __device__ __forceinline__ void write_row(void* to, int64_t at, const float* v, uint32_t from, uint32_t cols) {
     uint4* const p = reinterpret_cast<uint4*>(static_cast<uint16_t*>(to) + at + from);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        if (from + 8 * j < cols)
-            p[j] = make_uint4(pack2<BF16>(v[8 * j], v[8 * j + 1]), pack2<BF16>(v[8 * j + 2], v[8 * j + 3]),
-                              pack2<BF16>(v[8 * j + 4], v[8 * j + 5]), pack2<BF16>(v[8 * j + 6], v[8 * j + 7]));
+        if (from + 8 * j < cols) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float lo = v[8 * j + 2 * e], hi = v[8 * j + 2 * e + 1];
+                w[e] = pack2<BF16>(lo, hi);
+                if (REST) w[e] = rest2<BF16>(lo, hi, w[e]);
+            }
+            p[j] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+}
+
+__device__ __forceinline__ int64_t rest_at(const AttentionParams& p, uint32_t b, uint32_t token, uint32_t head) {
+    return (((int64_t)b * p.seq_q + token) * p.q_heads + head) * p.d_v;
 }
 
 // --- host -----------------------------------------------------------------------------------------------------------
@@ -161,6 +180,8 @@ inline int check(const mmee_workload_t* w, const mmee_attention_t* a, Problem* o
     p.o = a->o;
     p.os = out->o.s;
     p.lse = a->lse;
+    p.rest = a->o_rest;
+    if (p.rest && !aligned16(p.rest)) return MMEE_ERR_ARG;
     out->bf16 = a->dtype == MMEE_BF16;
     return MMEE_OK;
 }

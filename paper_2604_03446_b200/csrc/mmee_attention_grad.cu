@@ -41,7 +41,8 @@ __device__ __forceinline__ int ds_shift(const GradParams& p) {
     return max(-100, min(100, 14 - ilogbf(bound)));
 }
 
-// delta of every query row, half a warp to a row; in fp16 also the largest sizes in dO and in V's valid rows (their order
+// delta of every query row, half a warp to a row, from o and what its rounding took off (o alone would add four fifths of the error that
+// a rounding of dQ and dK is: 384 queries, 512 keys, fp16); in fp16 also the largest sizes in dO and in V's valid rows (their order
 // does not matter).  A block takes 64 tokens of a head.
 constexpr uint32_t kRowsOfBlock = 64;
 template <bool BF16>
@@ -51,29 +52,32 @@ __global__ void __launch_bounds__(256) grad_rows_kernel(const GradParams p) {
     const uint32_t lane = threadIdx.x & 15u, head = blockIdx.y, b = blockIdx.z, t0 = blockIdx.x * kRowsOfBlock + (threadIdx.x >> 4);
     const uint16_t* const d_o = static_cast<const uint16_t*>(p.d_o) + (int64_t)b * p.dos.batch + (int64_t)head * p.dos.head + 8 * lane;
     const uint16_t* const o = static_cast<const uint16_t*>(a.o) + (int64_t)b * a.os.batch + (int64_t)head * a.os.head + 8 * lane;
+    const uint16_t* const rest = static_cast<const uint16_t*>(a.rest) + rest_at(a, b, 0, head) + 8 * lane;
     const uint16_t* const v = static_cast<const uint16_t*>(p.v) + (int64_t)b * p.vs.batch + (int64_t)head * p.vs.head + 8 * lane;
     uint32_t keys = 0;
     if constexpr (!BF16) keys = head < p.kv_heads ? valid_keys(a.kv_len, b, a.seq_kv) : 0;
     const bool in = 8 * lane < a.d_v;
     float most[2] = {0.f, 0.f};
-    uint4 x[kRowsOfBlock / 16], y[kRowsOfBlock / 16], z[kRowsOfBlock / 16];
+    uint4 x[kRowsOfBlock / 16], y[kRowsOfBlock / 16], y2[kRowsOfBlock / 16], z[kRowsOfBlock / 16];
 #pragma unroll
     for (uint32_t i = 0; i < kRowsOfBlock / 16; ++i) {
         const uint32_t token = t0 + 16 * i;
         const uint4 none = make_uint4(0, 0, 0, 0);
         x[i] = in && token < a.seq_q ? *reinterpret_cast<const uint4*>(d_o + (int64_t)token * p.dos.token) : none;
         y[i] = in && token < a.seq_q ? *reinterpret_cast<const uint4*>(o + (int64_t)token * a.os.token) : none;
+        y2[i] = in && a.rest && token < a.seq_q ? *reinterpret_cast<const uint4*>(rest + (int64_t)token * a.q_heads * a.d_v) : none;
         if constexpr (!BF16) z[i] = in && token < keys ? *reinterpret_cast<const uint4*>(v + (int64_t)token * p.vs.token) : none;
     }
 #pragma unroll
     for (uint32_t i = 0; i < kRowsOfBlock / 16; ++i) {
         const uint32_t token = t0 + 16 * i;
         const uint32_t xs[4] = {x[i].x, x[i].y, x[i].z, x[i].w}, ys[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
+        const uint32_t rs[4] = {y2[i].x, y2[i].y, y2[i].z, y2[i].w};
         float sum = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float2 f = unpack2<BF16>(xs[j]), g = unpack2<BF16>(ys[j]);
-            sum += f.x * g.x + f.y * g.y;
+            const float2 f = unpack2<BF16>(xs[j]), g = unpack2<BF16>(ys[j]), r = unpack2<BF16>(rs[j]);
+            sum += f.x * (g.x + r.x) + f.y * (g.y + r.y);
             if (!BF16) most[0] = fmaxf(most[0], fmaxf(fabsf(f.x), fabsf(f.y)));
         }
         if (!BF16) {

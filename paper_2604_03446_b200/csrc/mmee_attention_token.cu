@@ -227,7 +227,12 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 3 : 2) attention_token_
         } else {
             if (d == 0 && a.lse) a.lse[at] = log * kLn2;
             uint16_t* const to = static_cast<uint16_t*>(a.o) + (int64_t)b * a.os.batch + (int64_t)token * a.os.token + (int64_t)h * a.os.head;
-            *reinterpret_cast<uint2*>(to + d) = make_uint2(pack2<BF16>(o.x * inv, o.y * inv), pack2<BF16>(o.z * inv, o.w * inv));
+            o.x *= inv, o.y *= inv, o.z *= inv, o.w *= inv;
+            const uint2 w = make_uint2(pack2<BF16>(o.x, o.y), pack2<BF16>(o.z, o.w));
+            *reinterpret_cast<uint2*>(to + d) = w;
+            if (a.rest)
+                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.rest) + rest_at(a, b, token, h) + d) =
+                    make_uint2(rest2<BF16>(o.x, o.y, w.x), rest2<BF16>(o.z, o.w, w.y));
         }
     }
     if (p.cluster > 1) cluster.sync();                 // shared memory stays until the others have read it

@@ -73,7 +73,8 @@ def formulas(q, k, v, kv_len, u, scale=None, do=None):
     delta = (D * O).sum(-1, keepdim=True)
     dS = P * (dP - delta) * ok
     edp = f(dv) * (D.abs() @ V.abs().transpose(-1, -2))
-    ed = (D.abs() * (eo + u * (O.abs() + eo))).sum(-1, keepdim=True) + f(dv) * (D.abs() * O.abs()).sum(-1, keepdim=True)
+    # (delta from o and the rest of its rounding, which is rounded itself: u^2, and 2^-25 in fp16)
+    ed = (D.abs() * (eo + u * u * (O.abs() + eo) + 2.0 ** -25)).sum(-1, keepdim=True) + f(dv) * (D.abs() * O.abs()).sum(-1, keepdim=True)
     relp = 2 * worst + 2.0 ** -19 + 2.0 ** -20 * (lse.nan_to_num(0, 0, 0).abs())     # here P = exp(S - lse)
     eds = P * (1 + relp) * (edp + ed + 2.0 ** -22 * (dP.abs() + delta.abs())) + relp * dS.abs()
     # Rounded once to the type; in fp16 what is below the smallest normal value of the scaled dS (2^-14 of at most 2^15) is off by
@@ -100,8 +101,13 @@ def inside(name, got, want):
     assert float(off.max()) <= 0, "%s: %.3g over the bound" % (name, float(off.max()))
 
 
+def forward(*args, **kw):
+    o, saved = mm.mmee_attention(*args, **kw)
+    return o, mm.attention_lse(saved, o)
+
+
 def check_forward(q, k, v, kv_len=None, scale=None):
-    o, lse = mm.mmee_attention(q, k, v, kv_len=kv_len, scale=scale)
+    o, lse = forward(q, k, v, kv_len=kv_len, scale=scale)
     want = formulas(q, k, v, kv_len, torch.finfo(q.dtype).eps / 2, scale)
     inside("o", o, want["o"])
     inside("lse", lse, want["lse"])
@@ -133,7 +139,7 @@ def test_lengths_and_what_lies_behind_them(size, dtype):
     for junk in (float("nan"), float("inf"), float("-inf")):
         k2, v2 = k.clone(), v.clone()
         k2[behind], v2[behind] = junk, junk
-        o2, lse2 = mm.mmee_attention(q, k2, v2, kv_len=n)
+        o2, lse2 = forward(q, k2, v2, kv_len=n)
         assert torch.equal(o, o2) and torch.equal(lse, lse2)
     empty = (n <= 0).nonzero()[:, 0]
     assert (o[empty] == 0).all() and (lse[empty] == -math.inf).all()
@@ -145,11 +151,11 @@ def test_layouts_with_strides(seq_q):
     """Heads before tokens, keys and values side by side, sequences in a larger buffer."""
     b, hq, hkv, m, d = 2, 4, 2, 333, 64
     q, k, v, _ = make((b, hq, hkv, seq_q, m, d, d), torch.bfloat16, seed=2)
-    want = mm.mmee_attention(q, k, v)
+    want = forward(q, k, v)
     q2 = q.permute(0, 2, 1, 3).contiguous().permute(0, 2, 1, 3)
     both = torch.full((b, m + 3, hkv, 2, d + 8), float("nan"), dtype=q.dtype, device="cuda")
     both[:, :m, :, 0, :d], both[:, :m, :, 1, 8:] = k, v
-    got = mm.mmee_attention(q2, both[:, :m, :, 0, :d], both[:, :m, :, 1, 8:])
+    got = forward(q2, both[:, :m, :, 0, :d], both[:, :m, :, 1, 8:])
     assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
 
 
@@ -175,14 +181,14 @@ def test_infinite_scores_of_valid_keys():
         k = torch.ones(1, 300, 1, 64, dtype=torch.bfloat16, device="cuda")
         v = torch.randn(1, 300, 1, 64, device="cuda").bfloat16()
         k[:, :150] = float("-inf")
-        o, lse = mm.mmee_attention(q, k, v)
+        o, lse = forward(q, k, v)
         inside("o", o, formulas(q, k[:, 150:], v[:, 150:], None, 2.0 ** -8)["o"])
         k[:] = float("-inf")
-        o, lse = mm.mmee_attention(q, k, v)
+        o, lse = forward(q, k, v)
         assert (o == 0).all() and (lse == -math.inf).all()
         k[:] = 1
         k[0, 77, 0, 3] = float("nan")
-        o, lse = mm.mmee_attention(q, k, v)
+        o, lse = forward(q, k, v)
         assert torch.isnan(o).all() and torch.isnan(lse).all()
 
 
@@ -207,9 +213,9 @@ def test_an_offset_beyond_32_bits():
 def test_same_bits_every_time_on_any_stream_and_replayed(size):
     q, k, v, _ = make(size, torch.bfloat16, seed=4)
     n = torch.tensor([2999, 700][:size[0]], dtype=torch.int32, device="cuda")
-    want = mm.mmee_attention(q, k, v, kv_len=n)
+    want = forward(q, k, v, kv_len=n)
     torch.cuda.synchronize()
-    got = [mm.mmee_attention(q, k, v, kv_len=n, stream=torch.cuda.Stream()) for _ in range(4)]
+    got = [forward(q, k, v, kv_len=n, stream=torch.cuda.Stream()) for _ in range(4)]
     torch.cuda.synchronize()
     for o, lse in got:
         assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
@@ -217,10 +223,10 @@ def test_same_bits_every_time_on_any_stream_and_replayed(size):
     for _ in range(2):
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
-            out = mm.mmee_attention(q, k, v, kv_len=n)
+            out = forward(q, k, v, kv_len=n)
         graphs.append((graph, out))
     n.copy_(torch.tensor([1234, 2999][:size[0]], dtype=torch.int32))   # read when it is replayed
-    want = mm.mmee_attention(q, k, v, kv_len=n)
+    want = forward(q, k, v, kv_len=n)
     for graph, out in graphs * 2:
         out[0].zero_()
         graph.replay()
@@ -232,12 +238,12 @@ def test_same_bits_every_time_on_any_stream_and_replayed(size):
 # --- gradients ------------------------------------------------------------------------------------------------------
 
 def check_backward(q, k, v, do, kv_len=None, scale=None):
-    o, lse = mm.mmee_attention(q, k, v, kv_len=kv_len, scale=scale)
-    grads = mm.mmee_attention_backward(do, q, k, v, o, lse, kv_len=kv_len, scale=scale)
+    o, saved = mm.mmee_attention(q, k, v, kv_len=kv_len, scale=scale)
+    grads = mm.mmee_attention_backward(do, q, k, v, o, saved, kv_len=kv_len, scale=scale)
     want = formulas(q, k, v, kv_len, torch.finfo(q.dtype).eps / 2, scale, do)
     for name, got in zip(("dq", "dk", "dv"), grads):
         inside(name, got, want[name])
-    return o, lse, grads
+    return o, saved, grads
 
 
 @gpu
@@ -255,13 +261,13 @@ def test_gradients_against_64_bits(size, dtype):
 def test_gradients_with_lengths_and_what_lies_behind_them(size, dtype):
     q, k, v, do = make(size, TYPES[dtype], seed=12)
     n = lengths(size[0], size[4], 0)
-    o, lse, grads = check_backward(q, k, v, do, n)
+    o, saved, grads = check_backward(q, k, v, do, n)
     behind = torch.arange(size[4], device="cuda") >= n[:, None]
     assert (grads[1][behind] == 0).all() and (grads[2][behind] == 0).all() and (grads[0][n <= 0] == 0).all()
     for junk in (float("nan"), float("inf"), 6e4):
         k2, v2 = k.clone(), v.clone()
         k2[behind], v2[behind] = junk, junk
-        for a, b in zip(grads, mm.mmee_attention_backward(do, q, k2, v2, o, lse, kv_len=n)):
+        for a, b in zip(grads, mm.mmee_attention_backward(do, q, k2, v2, o, saved, kv_len=n)):
             assert torch.equal(a, b)
 
 
@@ -347,7 +353,7 @@ class _Case:
 
 BAD = [("w", "batch", 0), ("w", "q_heads", 0), ("w", "kv_heads", 0), ("w", "kv_heads", 3), ("w", "seq_q", 0), ("w", "seq_kv", 0), ("w", "d_qk", 0),
        ("w", "d_v", 0), ("w", "d_qk", 60), ("w", "d_v", 4), ("w", "word_bytes", 1), ("a", "dtype", 2), ("a", "scale", 0.0), ("a", "scale", -1.0),
-       ("a", "scale", math.inf), ("a", "scale", math.nan), ("a", "q", 0), ("a", "k", 4104), ("a", "v", 0), ("a", "o", 0), ("a", "o", 4098),
+       ("a", "scale", math.inf), ("a", "scale", math.nan), ("a", "q", 0), ("a", "k", 4104), ("a", "v", 0), ("a", "o", 0), ("a", "o", 4098), ("a", "o_rest", 4104),
        ("a", "q_stride", (768, 0, 64)), ("a", "k_stride", (0, 128, 64)), ("a", "v_stride", (320, 64, 20)), ("a", "o_stride", (384, -128, 32))]
 
 
@@ -417,6 +423,6 @@ def test_shapes_that_do_not_fit_are_refused():
     with pytest.raises(mm.MmeeError):
         mm.mmee_attention(q, k, v, scale=-1.0)
     o, lse = mm.mmee_attention(q, k, v)
-    for bad in [(o[:, :2], o, lse), (o, o[..., :24], lse), (o, o, lse.half()), (o, o, lse[:1]), (o.bfloat16(), o, lse)]:
+    for bad in [(o[:, :2], o, lse), (o, o[..., :24], lse), (o, o, lse.half()), (o, o, lse[:-1]), (o, o, None), (o.bfloat16(), o, lse)]:
         with pytest.raises(mm.MmeeError):
             mm.mmee_attention_backward(bad[0], q, k, v, bad[1], bad[2])
