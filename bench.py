@@ -6,7 +6,10 @@ the device, in one kernel launch per search.  The default workload is the larges
 configuration: grouped-query attention (batch 4, 32 query heads on 8 KV heads, S = 8192, d = 128) on
 the cloud accelerator, latency-driven then energy-delay-product-driven, 3.39e9 mappings per search.
 
-    python bench.py [--gpus N] [--steps K] [--warmup W] [--impl ours|reference] [--workload NAME]
+    python bench.py [--gpus N] [--steps K] [--warmup W] [--impl ours|reference] [--workload NAME] [--run]
+
+--run also runs the workload's chains on this GPU (mmee_attention, or mmee_gated_ffn for the two-GEMM chains) and adds their
+times, next to the cycles of the best mapping that the search found, under "chains".
 
 Prints one JSON line.  With N > 1 (under torchrun) every rank runs an independent replica on its
 own GPU: the search is launched per workload and does not shard in this build.
@@ -171,6 +174,59 @@ def run_reference(args, rank):
         e2e=dict(value=value, unit=UNIT, h2d_bytes_per_step=0, d2h_bytes_per_step=0))))
 
 
+FFN_WORKLOADS = ("ffn", "beyond")      # two-GEMM chains; the others are attention
+
+
+def chain_inputs(workload, gated_ffn, gen):
+    """Tensors of a workload's chain, bfloat16, random: (q, k, v) or (x, w_gate, w_up, w_down)."""
+    import torch
+    w = workload
+
+    def normal(*shape, std=1.0):
+        return torch.empty(shape, dtype=torch.bfloat16, device="cuda").normal_(0.0, std, generator=gen)
+
+    if gated_ffn:
+        return (normal(w["seq_q"], w["d_qk"]), normal(w["seq_kv"], w["d_qk"], std=w["d_qk"] ** -0.5),
+                normal(w["seq_kv"], w["d_qk"], std=w["d_qk"] ** -0.5), normal(w["d_v"], w["seq_kv"], std=w["seq_kv"] ** -0.5))
+    return (normal(w["batch"], w["seq_q"], w["q_heads"], w["d_qk"]), normal(w["batch"], w["seq_kv"], w["kv_heads"], w["d_qk"]),
+            normal(w["batch"], w["seq_kv"], w["kv_heads"], w["d_v"]))
+
+
+def run_chains(name, jobs, bests, steps=10):
+    """The chains of a workload on this GPU: device time of a call, mean over `steps` after three warm-up calls, L2 flushed before
+    each.  A workload that several searches share runs once."""
+    import torch
+    import paper_2604_03446_b200 as mm
+    gated = name in FFN_WORKLOADS
+    call = mm.mmee_gated_ffn if gated else mm.mmee_attention
+    flush = torch.empty(256 * 1024 * 1024, dtype=torch.uint8, device="cuda")
+    out, seen = [], []
+    for (cfg, search), best in zip(jobs, bests):
+        w = cfg["workload"]
+        if w in seen:
+            continue
+        seen.append(w)
+        gen = torch.Generator(device="cuda").manual_seed(0)
+        inputs = chain_inputs(w, gated, gen)
+        ms = []
+        for i in range(3 + steps):
+            flush.fill_(1)
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            call(*inputs)
+            b.record()
+            torch.cuda.synchronize()
+            ms.append(a.elapsed_time(b))
+        # multiply-adds of the chain as it is searched; the gated block has a second projection
+        per_row = w["seq_kv"] * ((2 if gated else 1) * w["d_qk"] + w["d_v"])
+        flops = 2 * w["batch"] * w["q_heads"] * w["seq_q"] * per_row
+        mean = statistics.mean(ms[3:])
+        out.append(dict(problem=cfg["name"], call=call.__name__, ms=mean, tflops=flops / mean / 1e9,
+                        searched=OBJ_NAMES[search["objective"]], mapping_idx=best.idx, mapping_latency_cycles=best.latency_cycles))
+        del inputs
+    return out
+
+
 def run_reconfig(args):
     """EDP-driven search over the four array designs of the reconfigurable-array comparison: one search per
     logical shape through mmee_search_shapes, host wall clock per design."""
@@ -206,6 +262,7 @@ def main():
     ap.add_argument("--impl", default="ours", choices=["ours", "reference"])
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--workload", default="gqa", choices=sorted(WORKLOADS) + ["sweep", "ffn", "beyond", "reconfig"])
+    ap.add_argument("--run", action="store_true", help="run the workload's chains on this GPU as well")
     args = ap.parse_args()
     args.warmup = max(args.warmup, 3) if args.impl == "ours" else args.warmup
 
@@ -386,6 +443,8 @@ def main():
             kernels=per_kernel, roofline=roofline, row_pruning=pruning)
         if not args.no_cpu_baseline:
             line["cpu_baseline"] = cpu_baseline(*jobs[0])
+        if args.run:
+            line["chains"] = run_chains(args.workload, jobs, bests)
         print(json.dumps(line))
     if world > 1:
         dist.destroy_process_group()
