@@ -51,8 +51,8 @@ template <int EPI, bool PAIR, int TN>
 struct TileShape {
     static constexpr uint32_t kM = PAIR ? 256 : 128, kRowsB = PAIR ? TN / 2 : TN;      // rows of a tile; of B in a CTA
     static constexpr uint32_t kA = 128 * kRowBytes, kB = kRowsB * kRowBytes;
-    // A warp's places: kPlain two of the product; kGate two of h, gate and up each; kGrad one of dg and du each, two of gate and up.
-    static constexpr uint32_t kParts = EPI == kPlain ? 2 : 6, kStages = (226 * 1024 - 4 * kParts * kPart) / (kA + kB);
+    // A warp's places: two of results (kGate: gate and up, then h, or h by turns; kGrad: dg and du), for kGrad two of gate and up each.
+    static constexpr uint32_t kParts = EPI == kGrad ? 6 : 2, kStages = (226 * 1024 - 4 * kParts * kPart) / (kA + kB);
     static constexpr uint32_t smem = kStages * (kA + kB) + 4 * kParts * kPart + 1024;
 };
 
@@ -291,19 +291,18 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
                         for (int j = 0; j < 16; ++j) o[16 * half + j] = pack2<BF16>(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
                     } else if (EPI == kGate) {
                         if (p.gate && d < cols) {
-                            // (this half's places: the stores of the same half of the step before have been read)
-                            if (lane == 0) tma_store_read<1>();
+                            if (lane == 0) tma_store_read<0>();
                             __syncwarp();
 #pragma unroll
                             for (uint32_t j = 0; j < 8; ++j) {
-                                store_shared16(swizzled(part(2 + 2 * half), lane, j), x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
-                                store_shared16(swizzled(part(3 + 2 * half), lane, j), y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+                                store_shared16(swizzled(part(0), lane, j), x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+                                store_shared16(swizzled(part(1), lane, j), y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
                             }
                             ready();
                             if (lane == 0) {
-                                tma_store_2d(&ps.gate, part(2 + 2 * half), (int32_t)(col0 + d), (int32_t)row0);
-                                tma_store_2d(&ps.up, part(3 + 2 * half), (int32_t)(col0 + d), (int32_t)row0);
-                                if (half == 0) tma_store_commit();     // (the second half's go with h)
+                                tma_store_2d(&ps.gate, part(0), (int32_t)(col0 + d), (int32_t)row0);
+                                tma_store_2d(&ps.up, part(1), (int32_t)(col0 + d), (int32_t)row0);
+                                tma_store_commit();
                             }
                         }
                         with_act(p.act, [&](auto kind) {
@@ -344,7 +343,7 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
                 if (c >= cols || (EPI == kPlain && p.splits > 1)) continue;        // (the same for the whole warp)
                 const uint32_t to = EPI == kGrad ? part(0) : part(stores & 1);
                 if (lane == 0) {
-                    if (EPI == kGrad)
+                    if (EPI == kGrad || (EPI == kGate && p.gate))
                         tma_store_read<0>();
                     else
                         tma_store_read<1>();
