@@ -5,6 +5,13 @@
 // through shared memory by TMA in tiles of 128, S = Q K^T lands in tensor memory, a warpgroup per query tile (a thread per
 // row, so that no reduction crosses threads) turns it into P in place, which the next matrix instruction takes from there.
 // While one tile's scores are turned, the tensor cores work for the other.
+//
+// 32/8 heads, 4096 queries, 8192 keys, d 128, bf16: 505 us, 1090 TFLOP/s.  The tensor cores are at work 56 % of the time, the
+// exponentials' units as much.  What bounds it is a tile's way through a turn (scores read, maximum, 128 exponentials a thread,
+// written, P V, the next scores), which is longer than the other tile's products.  Measured on the way (narrow inputs, 459 us as it is):
+// exponentials on the multiply-add pipes for a quarter of the values 479; two warpgroups a tile, half a row to a thread, 490; blocks
+// of 64 keys with two places for scores 707 (more and smaller matrix instructions); a reference from the block before instead of a
+// maximum first 606.
 #include "mmee_attention.cuh"
 
 namespace mmee {
@@ -95,223 +102,223 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     if (warp >= kLoad) {
         if constexpr (TILES == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp == kLoad) {
-        if (elect_one() && n) {
-            const int32_t h = (int32_t)head, hk = (int32_t)(head / p.group), bb = (int32_t)b;
-            uint32_t k_sent = 0, v_sent = 0;
-            bool sound = true;
-            auto load_q = [&](uint32_t t) {
-                mbar_expect(q_full(t), Shape::kQ);
-                for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(q_tile(t) + j * kTile * kRowBytes, &mq, q_full(t), 64 * j, (int32_t)(q0 + t * kTile), h, bb);
+            if (elect_one() && n) {
+                const int32_t h = (int32_t)head, hk = (int32_t)(head / p.group), bb = (int32_t)b;
+                uint32_t k_sent = 0, v_sent = 0;
+                bool sound = true;
+                auto load_q = [&](uint32_t t) {
+                    mbar_expect(q_full(t), Shape::kQ);
+                    for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(q_tile(t) + j * kTile * kRowBytes, &mq, q_full(t), 64 * j, (int32_t)(q0 + t * kTile), h, bb);
+                };
+                load_q(0);
+                for (uint32_t i = 0; i < n; ++i) {
+                    const uint32_t s = i % kRing, turn = ((i / kRing) & 1) ^ 1;
+                    const int32_t row = (int32_t)((t0 + i) * kTile);
+                    if (!(sound = mbar_wait(k_empty(s), turn, lost))) break;
+                    mbar_expect(k_full(s), Shape::kQ);
+                    for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(k_tile(s) + j * kTile * kRowBytes, &mk, k_full(s), 64 * j, row, hk, bb);
+                    ++k_sent;
+                    if (i == 0)
+                        for (uint32_t t = 1; t < tiles; ++t) load_q(t);
+                    if (!(sound = mbar_wait(v_empty(s), turn, lost))) break;
+                    mbar_expect(v_full(s), Shape::kV);
+                    for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(v_tile(s) + j * kTile * kRowBytes, &mv, v_full(s), 64 * j, row, hk, bb);
+                    ++v_sent;
+                }
+                if (!sound) {                              // what is in flight lands before the CTA ends
+                    for (uint32_t t = 0; t < (k_sent ? tiles : 1); ++t) mbar_wait(q_full(t), 0, nullptr);
+                    for (uint32_t s = 0; s < kRing; ++s) {
+                        if (k_sent > s) mbar_wait(k_full(s), ((k_sent - 1 - s) / kRing) & 1, nullptr);
+                        if (v_sent > s) mbar_wait(v_full(s), ((v_sent - 1 - s) / kRing) & 1, nullptr);
+                    }
+                }
+            }
+            __syncwarp();
+        } else if (warp == kMma) {
+            constexpr uint32_t desc_s = mma_desc(BF16, kTile, kTile, false, false);
+            const uint32_t desc_o = mma_desc(BF16, kTile, (p.d_v + 15) / 16 * 16, false, true);
+            const uint32_t steps_s = (p.d_qk + 15) / 16;
+            auto scores = [&](uint32_t t, uint32_t s) {    // S_t = Q_t K^T
+                tile_product<DK>(s_col(t), q_tile(t), k_tile(s), desc_s, steps_s);
+                mma_commit(s_full(t));
             };
-            load_q(0);
-            for (uint32_t i = 0; i < n; ++i) {
-                const uint32_t s = i % kRing, turn = ((i / kRing) & 1) ^ 1;
-                const int32_t row = (int32_t)((t0 + i) * kTile);
-                if (!(sound = mbar_wait(k_empty(s), turn, lost))) break;
-                mbar_expect(k_full(s), Shape::kQ);
-                for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(k_tile(s) + j * kTile * kRowBytes, &mk, k_full(s), 64 * j, row, hk, bb);
-                ++k_sent;
-                if (i == 0)
-                    for (uint32_t t = 1; t < tiles; ++t) load_q(t);
-                if (!(sound = mbar_wait(v_empty(s), turn, lost))) break;
-                mbar_expect(v_full(s), Shape::kV);
-                for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(v_tile(s) + j * kTile * kRowBytes, &mv, v_full(s), 64 * j, row, hk, bb);
-                ++v_sent;
-            }
-            if (!sound) {                              // what is in flight lands before the CTA ends
-                for (uint32_t t = 0; t < (k_sent ? tiles : 1); ++t) mbar_wait(q_full(t), 0, nullptr);
-                for (uint32_t s = 0; s < kRing; ++s) {
-                    if (k_sent > s) mbar_wait(k_full(s), ((k_sent - 1 - s) / kRing) & 1, nullptr);
-                    if (v_sent > s) mbar_wait(v_full(s), ((v_sent - 1 - s) / kRing) & 1, nullptr);
-                }
-            }
-        }
-        __syncwarp();
-    } else if (warp == kMma) {
-        constexpr uint32_t desc_s = mma_desc(BF16, kTile, kTile, false, false);
-        const uint32_t desc_o = mma_desc(BF16, kTile, (p.d_v + 15) / 16 * 16, false, true);
-        const uint32_t steps_s = (p.d_qk + 15) / 16;
-        auto scores = [&](uint32_t t, uint32_t s) {    // S_t = Q_t K^T
-            tile_product<DK>(s_col(t), q_tile(t), k_tile(s), desc_s, steps_s);
-            mma_commit(s_full(t));
-        };
-        bool sound = n > 0;
-        if (sound) {
-            sound = mbar_wait(k_full(0), 0, lost);
-            for (uint32_t t = 0; t < tiles && sound; ++t) {
-                if (!(sound = mbar_wait(q_full(t), 0, lost))) break;
-                tcgen05_fence_after();
-                if (elect_one()) {
-                    scores(t, 0);
-                    if (t + 1 == tiles) mma_commit(k_empty(0));
-                }
-                __syncwarp();
-            }
-        }
-        for (uint32_t i = 0; i < n && sound; ++i) {
-            const uint32_t s = i % kRing, s1 = (i + 1) % kRing;
-            const uint32_t valid = min(kTile, keys - (t0 + i) * kTile), steps_o = (valid + 15) / 16;
-            if (!(sound = mbar_wait(v_full(s), (i / kRing) & 1, lost))) break;
-            if (valid % 16) zero_rows(v_tile(s), DV / 64, valid, steps_o * 16);
-            if (i + 1 < n && !(sound = mbar_wait(k_full(s1), ((i + 1) / kRing) & 1, lost))) break;
-            for (uint32_t t = 0; t < tiles; ++t) {
-                // P V in two halves of 64 keys, the first while the second is still scores.
-                for (uint32_t h = 0; h < 2 && sound; ++h) {
-                    if (!(sound = mbar_wait(p_full(t, h), i & 1, lost))) break;
+            bool sound = n > 0;
+            if (sound) {
+                sound = mbar_wait(k_full(0), 0, lost);
+                for (uint32_t t = 0; t < tiles && sound; ++t) {
+                    if (!(sound = mbar_wait(q_full(t), 0, lost))) break;
                     tcgen05_fence_after();
                     if (elect_one()) {
-                        turned_product<4, 32>(o_col(t), s_col(t) + 32 * h, v_tile(s) + h * 64 * kRowBytes, desc_o, max(steps_o, 4 * h) - 4 * h, i | h);
+                        scores(t, 0);
+                        if (t + 1 == tiles) mma_commit(k_empty(0));
                     }
                     __syncwarp();
                 }
-                if (!sound) break;
-                if (elect_one()) {
-                    if (t + 1 == tiles) mma_commit(v_empty(s));
-                    if (i + 1 < n) {
-                        scores(t, s1);
-                        if (t + 1 == tiles) mma_commit(k_empty(s1));
-                    } else {
-                        mma_commit(o_full(t));
+            }
+            for (uint32_t i = 0; i < n && sound; ++i) {
+                const uint32_t s = i % kRing, s1 = (i + 1) % kRing;
+                const uint32_t valid = min(kTile, keys - (t0 + i) * kTile), steps_o = (valid + 15) / 16;
+                if (!(sound = mbar_wait(v_full(s), (i / kRing) & 1, lost))) break;
+                if (valid % 16) zero_rows(v_tile(s), DV / 64, valid, steps_o * 16);
+                if (i + 1 < n && !(sound = mbar_wait(k_full(s1), ((i + 1) / kRing) & 1, lost))) break;
+                for (uint32_t t = 0; t < tiles; ++t) {
+                    // P V in two halves of 64 keys, the first while the second is still scores.
+                    for (uint32_t h = 0; h < 2 && sound; ++h) {
+                        if (!(sound = mbar_wait(p_full(t, h), i & 1, lost))) break;
+                        tcgen05_fence_after();
+                        if (elect_one()) {
+                            turned_product<4, 32>(o_col(t), s_col(t) + 32 * h, v_tile(s) + h * 64 * kRowBytes, desc_o, max(steps_o, 4 * h) - 4 * h, i | h);
+                        }
+                        __syncwarp();
                     }
+                    if (!sound) break;
+                    if (elect_one()) {
+                        if (t + 1 == tiles) mma_commit(v_empty(s));
+                        if (i + 1 < n) {
+                            scores(t, s1);
+                            if (t + 1 == tiles) mma_commit(k_empty(s1));
+                        } else {
+                            mma_commit(o_full(t));
+                        }
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
             }
         }
-    }
     } else {
         if constexpr (TILES == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         if (warp / 4 < tiles) {
-        const uint32_t t = warp / 4, row = (warp % 4) * 32 + lane, lanes = ((warp % 4) * 32) << 16;
-        const float sl2 = p.scale * kLog2e;
-        float m = -INFINITY, l = 0.f;                  // reference and sum, in powers of two
-        bool sound = true;
-        const uint32_t from_s = s_col(t) + lanes;
+            const uint32_t t = warp / 4, row = (warp % 4) * 32 + lane, lanes = ((warp % 4) * 32) << 16;
+            const float sl2 = p.scale * kLog2e;
+            float m = -INFINITY, l = 0.f;                  // reference and sum, in powers of two
+            bool sound = true;
+            const uint32_t from_s = s_col(t) + lanes;
 #pragma unroll 1
-        for (uint32_t i = 0; i < n; ++i) {
-            if (!(sound = mbar_wait(s_full(t), i & 1, lost))) break;
-            tcgen05_fence_after();
-            const int valid = (int)min(kTile, keys - (t0 + i) * kTile);
-            auto cut = [&](uint32_t* v, int from) {    // scores of keys behind the end
-                if (valid < from + 32) {
+            for (uint32_t i = 0; i < n; ++i) {
+                if (!(sound = mbar_wait(s_full(t), i & 1, lost))) break;
+                tcgen05_fence_after();
+                const int valid = (int)min(kTile, keys - (t0 + i) * kTile);
+                auto cut = [&](uint32_t* v, int from) {    // scores of keys behind the end
+                    if (valid < from + 32) {
 #pragma unroll
-                    for (int c = 0; c < 32; ++c)
-                        if (from + c >= valid) v[c] = 0xff800000u;
+                        for (int c = 0; c < 32; ++c)
+                            if (from + c >= valid) v[c] = 0xff800000u;
+                    }
+                };
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                auto take_most = [&](const uint32_t* v) {
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+                };
+                uint32_t x[kHeld], y[32];
+#pragma unroll
+                for (int c = 0; c < kHeld; c += 32) tmem_load32(from_s + c, x + c);
+#pragma unroll
+                for (int c = 0; c < kHeld; c += 32) tmem_loaded32(x + c);
+#pragma unroll
+                for (int c = kHeld; c < 128; c += 32) {
+                    tmem_load32(from_s + c, y);
+                    tmem_loaded32(y);
+                    cut(y, c);
+                    take_most(y);
                 }
-            };
-            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            auto take_most = [&](const uint32_t* v) {
+                if (valid < (int)kTile) {
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) top[(c >> 1) & 3] = max3(top[(c >> 1) & 3], __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
-            };
-            uint32_t x[kHeld], y[32];
+                    for (int c = 0; c < kHeld; c += 32) cut(x + c, c);
+                }
 #pragma unroll
-            for (int c = 0; c < kHeld; c += 32) tmem_load32(from_s + c, x + c);
-#pragma unroll
-            for (int c = 0; c < kHeld; c += 32) tmem_loaded32(x + c);
-#pragma unroll
-            for (int c = kHeld; c < 128; c += 32) {
-                tmem_load32(from_s + c, y);
-                tmem_loaded32(y);
-                cut(y, c);
-                take_most(y);
-            }
-            if (valid < (int)kTile) {
-#pragma unroll
-                for (int c = 0; c < kHeld; c += 32) cut(x + c, c);
-            }
-#pragma unroll
-            for (int c = 0; c < kHeld; c += 32) take_most(x + c);
-            const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sl2;
-            if (i == 0) {
-                m = most;
-            } else if (__any_sync(0xffffffffu, most > m + kSlack)) {
-                // The sums so far: all matrix instructions issued before these scores are done, P V of the last tile too.
-                const float to = most > m + kSlack ? most : m, by = to == m ? 1.f : exp2_fast(m - to);
-                m = to;
-                l *= by;
+                for (int c = 0; c < kHeld; c += 32) take_most(x + c);
+                const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sl2;
+                if (i == 0) {
+                    m = most;
+                } else if (__any_sync(0xffffffffu, most > m + kSlack)) {
+                    // The sums so far: all matrix instructions issued before these scores are done, P V of the last tile too.
+                    const float to = most > m + kSlack ? most : m, by = to == m ? 1.f : exp2_fast(m - to);
+                    m = to;
+                    l *= by;
 #pragma unroll 1
-                for (int c = 0; c < DV; c += 16) {     // (few registers: the scores are live)
-                    uint32_t o[16];
-                    tmem_load16(o_col(t) + lanes + c, o);
-                    tmem_loaded16(o);
+                    for (int c = 0; c < DV; c += 16) {     // (few registers: the scores are live)
+                        uint32_t o[16];
+                        tmem_load16(o_col(t) + lanes + c, o);
+                        tmem_loaded16(o);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * by);
-                    tmem_store16(o_col(t) + lanes + c, o);
-                }
-            }
-            const float from = kBias<BF16> - (m == -INFINITY ? 0.f : m);
-            const uint64_t scale2 = pair(sl2, sl2), from2 = pair(from, from);
-            uint64_t sum[2] = {0, 0};
-            auto turn = [&](const uint32_t* v, int c) {        // 32 scores into probabilities, over scores that have been read
-                uint32_t pk[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    float2 w = unpair(fma_pair(pair(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), scale2, from2));
-                    w.x = exp2_fast(w.x), w.y = exp2_fast(w.y);
-                    sum[j & 1] = add_pair(sum[j & 1], pair(w.x, w.y));
-                    pk[j] = pack2<BF16>(w.x, w.y);
-                }
-                tmem_store16(from_s + c / 2, pk);
-                if (c == 32 || c == 96) {
-                    tmem_stored();
-                    tcgen05_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(p_full(t, c / 64));
-                }
-            };
-#pragma unroll
-            for (int c = 0; c < kHeld; c += 32) turn(x + c, c);
-#pragma unroll
-            for (int c = kHeld; c < 128; c += 32) {
-                tmem_load32(from_s + c, y);
-                tmem_loaded32(y);
-                cut(y, c);
-                turn(y, c);
-            }
-            const float2 sums = unpair(add_pair(sum[0], sum[1]));
-            l += sums.x + sums.y;
-        }
-        const uint32_t token = q0 + t * kTile + row;
-        if (n && sound) sound = mbar_wait(o_full(t), 0, lost);
-        tcgen05_fence_after();
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        const uint64_t part_at = ((uint64_t)split * (p.tiles - p.whole) + (tile - p.whole)) * p.tile_rows + t * kTile + row;    // (if cut up)
-        if (sound && token < p.seq_q) {
-            const float l2 = l == 0.f ? -INFINITY : m - kBias<BF16> + log2f(l);
-            if (cut_up)
-                p.part_lse[part_at] = l2;
-            else if (p.lse)
-                p.lse[((uint64_t)b * p.q_heads + head) * p.seq_q + token] = l2 * kLn2;
-        }
-        if (sound) {
-            const int64_t to = (int64_t)b * p.os.batch + (int64_t)token * p.os.token + (int64_t)head * p.os.head;
-#pragma unroll
-            for (uint32_t c = 0; c < DV; c += 32) {
-                uint32_t o[32];
-                if (n) {
-                    tmem_load32(o_col(t) + lanes + c, o);
-                    tmem_loaded32(o);
-                }
-                if (token < p.seq_q && c < p.d_v) {
-                    float v[32];
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = l == 0.f ? 0.f : __uint_as_float(o[j]) * inv;
-                    if (cut_up) {
-                        if (l != 0.f) {
-                            float4* const q = reinterpret_cast<float4*>(p.part_o + part_at * p.d_v + c);
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                if (c + 4 * j < p.d_v) q[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-                        }
-                    } else {
-                        write_row<BF16>(p.o, to, v, c, p.d_v);
-                        if (p.rest) write_row<BF16, true>(p.rest, rest_at(p, b, token, head), v, c, p.d_v);
+                        for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * by);
+                        tmem_store16(o_col(t) + lanes + c, o);
                     }
                 }
-                __syncwarp();
+                const float from = kBias<BF16> - (m == -INFINITY ? 0.f : m);
+                const uint64_t scale2 = pair(sl2, sl2), from2 = pair(from, from);
+                uint64_t sum[2] = {0, 0};
+                auto turn = [&](const uint32_t* v, int c) {        // 32 scores into probabilities, over scores that have been read
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        float2 w = unpair(fma_pair(pair(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), scale2, from2));
+                        w.x = exp2_fast(w.x), w.y = exp2_fast(w.y);
+                        sum[j & 1] = add_pair(sum[j & 1], pair(w.x, w.y));
+                        pk[j] = pack2<BF16>(w.x, w.y);
+                    }
+                    tmem_store16(from_s + c / 2, pk);
+                    if (c == 32 || c == 96) {
+                        tmem_stored();
+                        tcgen05_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(p_full(t, c / 64));
+                    }
+                };
+#pragma unroll
+                for (int c = 0; c < kHeld; c += 32) turn(x + c, c);
+#pragma unroll
+                for (int c = kHeld; c < 128; c += 32) {
+                    tmem_load32(from_s + c, y);
+                    tmem_loaded32(y);
+                    cut(y, c);
+                    turn(y, c);
+                }
+                const float2 sums = unpair(add_pair(sum[0], sum[1]));
+                l += sums.x + sums.y;
+            }
+            const uint32_t token = q0 + t * kTile + row;
+            if (n && sound) sound = mbar_wait(o_full(t), 0, lost);
+            tcgen05_fence_after();
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const uint64_t part_at = ((uint64_t)split * (p.tiles - p.whole) + (tile - p.whole)) * p.tile_rows + t * kTile + row;    // (if cut up)
+            if (sound && token < p.seq_q) {
+                const float l2 = l == 0.f ? -INFINITY : m - kBias<BF16> + log2f(l);
+                if (cut_up)
+                    p.part_lse[part_at] = l2;
+                else if (p.lse)
+                    p.lse[((uint64_t)b * p.q_heads + head) * p.seq_q + token] = l2 * kLn2;
+            }
+            if (sound) {
+                const int64_t to = (int64_t)b * p.os.batch + (int64_t)token * p.os.token + (int64_t)head * p.os.head;
+#pragma unroll
+                for (uint32_t c = 0; c < DV; c += 32) {
+                    uint32_t o[32];
+                    if (n) {
+                        tmem_load32(o_col(t) + lanes + c, o);
+                        tmem_loaded32(o);
+                    }
+                    if (token < p.seq_q && c < p.d_v) {
+                        float v[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = l == 0.f ? 0.f : __uint_as_float(o[j]) * inv;
+                        if (cut_up) {
+                            if (l != 0.f) {
+                                float4* const q = reinterpret_cast<float4*>(p.part_o + part_at * p.d_v + c);
+#pragma unroll
+                                for (int j = 0; j < 8; ++j)
+                                    if (c + 4 * j < p.d_v) q[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                            }
+                        } else {
+                            write_row<BF16>(p.o, to, v, c, p.d_v);
+                            if (p.rest) write_row<BF16, true>(p.rest, rest_at(p, b, token, head), v, c, p.d_v);
+                        }
+                    }
+                    __syncwarp();
+                }
             }
         }
-    }
     }
     tcgen05_fence_before();
     __syncthreads();

@@ -61,6 +61,8 @@ int sm_count(uint32_t* out) {
 extern "C" int mmee_chain_status(void) {
     int (*const words[])(uint32_t*) = {mmee::attention_gave_up, mmee::attention_grad_gave_up, mmee::ffn_gave_up, mmee::ffn_narrow_gave_up};
     uint32_t any = 0;
+    const int done = mmee::cuda_status(cudaDeviceSynchronize());     // (streams that do not wait for the default one, too)
+    if (done) return done;
     for (const auto word : words) {
         uint32_t w = 0;
         const int rc = word(&w);
