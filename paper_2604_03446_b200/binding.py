@@ -459,7 +459,7 @@ def _space(ask, like, where, *args):
     code = ask(*args, C.addressof(need))
     if code:
         _check(code, where)
-    return (_torch.empty(need.value, dtype=_torch.uint8, device=like.device) if need.value else None), need.value
+    return (like.new_empty(need.value, dtype=_torch.uint8) if need.value else None), need.value
 
 
 def _attention_sizes(where, q, k, v, kv_len):
@@ -492,10 +492,10 @@ def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
     o = q.new_empty((batch, seq_q, q_heads, d_v))
     rows = batch * seq_q * q_heads
     ahead = (rows + 3) // 4 * 4                        # (what follows the rows' sums starts on sixteen bytes)
-    saved = _torch.empty(ahead + rows * d_v // 2, dtype=_torch.float32, device=q.device)
+    saved = q.new_empty(ahead + rows * d_v // 2, dtype=_torch.float32)
     at = saved.data_ptr()
     a = _ATTENTION(code, (d_qk or 1) ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
-                   *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], at, at + 4 * ahead,
+                   *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], seq_q * q_heads * d_v, q_heads * d_v, d_v, at, at + 4 * ahead,
                    0 if kv_len is None else kv_len.data_ptr(), space.data_ptr() if need else 0, need)
     code = calls.attention(w, a, _current_stream())
     if code:
@@ -561,7 +561,7 @@ def mmee_gated_ffn(x, w_gate, w_up, w_down, activation: int = ACT_SILU, save: bo
     calls = _chain()
     w = _WORKLOAD(1, 1, 1, tokens, d_ff, d_in, d_out, 2)
     hidden, y = x.new_empty((tokens, d_ff)), x.new_empty((tokens, d_out))
-    kept = _torch.empty((2, tokens, d_ff), dtype=_torch.float32, device=x.device) if save else None
+    kept = x.new_empty((2, tokens, d_ff), dtype=_torch.float32) if save else None
     space, need = _space(calls.gated_ffn_workspace, x, where, w, 0)
     f = _FFN(code, activation, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), x.stride(0), w_gate.stride(0),
              w_up.stride(0), w_down.stride(0), hidden.data_ptr(), kept.data_ptr() if save else 0, y.data_ptr(), space.data_ptr() if need else 0, need)

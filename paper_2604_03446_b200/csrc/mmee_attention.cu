@@ -51,9 +51,6 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     const uint32_t past = blockIdx.x - p.whole, split = cut_up ? past % p.splits : 0, tile = cut_up ? p.whole + past / p.splits : blockIdx.x;
     const uint32_t head = tile / p.tiles_q % p.q_heads, b = tile / p.tiles_q / p.q_heads, q0 = tile % p.tiles_q * (TILES * kTile);
     const uint32_t tiles = (p.seq_q - q0 <= kTile) ? 1 : TILES;
-    const uint32_t keys = valid_keys(p.kv_len, b, p.seq_kv);
-    const uint32_t t0 = split * p.tiles_per_split, t_all = (keys + kTile - 1) / kTile;
-    const uint32_t n = !cut_up ? t_all : t0 < t_all ? min(p.tiles_per_split, t_all - t0) : 0;     // key tiles of this CTA
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
 
     const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
@@ -95,7 +92,11 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     tcgen05_fence_after();
     const uint32_t tmem = tmem_base;
     volatile uint32_t* const lost = &gave_up;
-    asm volatile("griddepcontrol.launch_dependents;");        // (the joining kernel's launch, where there is one)
+    wait_for_stream();
+    release_stream();
+    const uint32_t keys = valid_keys(p.kv_len, b, p.seq_kv);
+    const uint32_t t0 = split * p.tiles_per_split, t_all = (keys + kTile - 1) / kTile;
+    const uint32_t n = !cut_up ? t_all : t0 < t_all ? min(p.tiles_per_split, t_all - t0) : 0;     // key tiles of this CTA
     auto s_col = [&](uint32_t t) { return tmem + t * 128; };
     auto o_col = [&](uint32_t t) { return tmem + TILES * 128 + t * DV; };
 
@@ -340,7 +341,8 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
 // in the same order.
 template <bool BF16>
 __global__ void __launch_bounds__(128) attention_join_kernel(const AttentionParams p) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    wait_for_stream();
+    release_stream();
     const uint64_t rows = (uint64_t)(p.tiles - p.whole) * p.tile_rows, at = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     const uint32_t lane = threadIdx.x & 31u;
     if (at >= rows) return;
@@ -384,7 +386,7 @@ int launch_forward(const Problem& x, cudaStream_t stream) {
     if (!rc) rc = view_map(&mk, BF16, x.p.batch, x.k);
     if (!rc) rc = view_map(&mv, BF16, x.p.batch, x.v);
     if (rc) return rc;
-    const LaunchAt at{dim3(x.p.whole + (x.p.tiles - x.p.whole) * x.p.splits), forward_threads(TILES), ForwardShape<DK, DV>::smem(TILES), 1, false, stream};
+    const LaunchAt at{dim3(x.p.whole + (x.p.tiles - x.p.whole) * x.p.splits), forward_threads(TILES), ForwardShape<DK, DV>::smem(TILES), 1, true, stream};
     return launch<attention_kernel<DK, DV, TILES, BF16>>(at, mq, mk, mv, x.p);
 }
 

@@ -51,7 +51,8 @@ __device__ __forceinline__ int ds_shift(const GradParams& p) {
 constexpr uint32_t kRowsOfBlock = 64;
 template <bool BF16>
 __global__ void __launch_bounds__(256) grad_rows_kernel(const GradParams p) {
-    asm volatile("griddepcontrol.launch_dependents;");
+    wait_for_stream();
+    release_stream();
     const AttentionParams& a = p.a;
     const uint32_t lane = threadIdx.x & 15u, head = blockIdx.y, b = blockIdx.z, t0 = blockIdx.x * kRowsOfBlock + (threadIdx.x >> 4);
     const uint16_t* const d_o = static_cast<const uint16_t*>(p.d_o) + (int64_t)b * p.dos.batch + (int64_t)head * p.dos.head + 8 * lane;
@@ -186,8 +187,8 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     const uint32_t tmem = beside.tmem_base, s_col = tmem, dp_col = tmem + 128, dv_col = tmem + 256, dk_col = dv_col + DV;
     volatile uint32_t* const lost = &gave_up;
     // The rows' kernel is done from here on.  The kernel of dQ, which needs it too, may start where this one leaves room.
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;");
+    wait_for_stream();
+    release_stream();
 
     if (warp == 8) {
         const int32_t bb = (int32_t)b, hk = (int32_t)head;
@@ -448,6 +449,9 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     const uint32_t tmem = tmem_base, dp_col = tmem + 256, dq_col = tmem + 384;
     auto s_col = [&](uint32_t t) { return tmem + 128 * t; };
     volatile uint32_t* const lost = &gave_up;
+    // Without a wait: the kernel of dK and dV, beside which this one starts, has released the stream after the rows' kernel was done, and
+    // writes nothing that is read here.
+    release_stream();
 
     if (warp == 8) {
         if (elect_one() && n) {
@@ -596,7 +600,7 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
         }
     }
     // (it was launched beside the kernel of dK and dV, and ends after it: what follows in the stream needs both)
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    wait_for_stream();
     tcgen05_fence_before();
     __syncthreads();
     if (warp == 9) {
@@ -627,7 +631,7 @@ int launch_grads(const Problem& x, const View& d_o, const GradParams& p, cudaStr
     if (!BF16 && (rc = cuda_status(cudaMemsetAsync(p.most, 0, 8, stream)))) return rc;
     const uint32_t longest = BF16 ? a.seq_q : max(a.seq_q, a.seq_kv);
     using Shape = GradShape<DK, DV>;
-    const LaunchAt rows{dim3((uint32_t)ceil_div(longest, kRowsOfBlock), a.q_heads, a.batch), 256, 0, 1, false, stream};
+    const LaunchAt rows{dim3((uint32_t)ceil_div(longest, kRowsOfBlock), a.q_heads, a.batch), 256, 0, 1, BF16, stream};       // (fp16: after the memset)
     const LaunchAt keys{dim3((uint32_t)ceil_div(a.seq_kv, kTile), p.kv_heads, a.batch), 320, Shape::smem_keys, 1, true, stream};
     const LaunchAt queries{dim3((uint32_t)ceil_div(a.seq_q, kTile), a.q_heads, a.batch), 320, Shape::smem, 1, true, stream};
     rc = launch<grad_rows_kernel<BF16>>(rows, p);

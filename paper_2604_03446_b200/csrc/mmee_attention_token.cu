@@ -56,7 +56,8 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 3 : 2) attention_token_
     constexpr uint32_t kRows = 8 * NT, kPitch = DV + 4;
     __shared__ __align__(16) float sums[kWarps][kRows][kPitch];
     __shared__ float tops[kWarps][kRows], totals[kWarps][kRows];
-    asm volatile("griddepcontrol.launch_dependents;");        // (the joining kernel's launch, where there is one)
+    wait_for_stream();
+    release_stream();
     const AttentionParams& a = p.a;
     const uint32_t head = blockIdx.y, b = blockIdx.z, parts = gridDim.x, part = blockIdx.x;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, g = lane >> 2, c = lane & 3u;
@@ -240,7 +241,7 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 3 : 2) attention_token_
 
 template <int DK, int DV, int NT>
 int launch_tokens(const TokenParams& p, bool bf16, cudaStream_t stream) {
-    const LaunchAt at{dim3(p.cluster * p.a.splits, p.a.q_heads / p.a.group, p.a.batch), kWarps * 32, 0, p.cluster, false, stream};
+    const LaunchAt at{dim3(p.cluster * p.a.splits, p.a.q_heads / p.a.group, p.a.batch), kWarps * 32, 0, p.cluster, true, stream};
     return bf16 ? launch<attention_token_kernel<DK, DV, NT, true>>(at, p) : launch<attention_token_kernel<DK, DV, NT, false>>(at, p);
 }
 

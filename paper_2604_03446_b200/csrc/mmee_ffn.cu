@@ -117,7 +117,8 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
     tcgen05_fence_after();
     const uint32_t tmem = tmem_base;
     volatile uint32_t* const lost = &gave_up;
-    asm volatile("griddepcontrol.launch_dependents;");
+    wait_for_stream();
+    release_stream();
     const uint32_t n_tiles = ps.of[ps.count - 1].end;
     // The product that tile i is part of, and the tile's number there.
     auto product_of = [&](uint32_t i, uint32_t* at) {
@@ -136,7 +137,6 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
 
     if (warp == 4) {                                   // operands
         if (elect_one()) {
-            asm volatile("griddepcontrol.wait;" ::: "memory");         // (operands may come from the kernel before)
             uint32_t it = 0;
             bool sound = true;
             for (uint32_t i = worker; i < n_tiles && sound; i += workers) {
@@ -417,8 +417,8 @@ void add_product(Products* ps, Operand* (&ops)[kMostProducts][4], Product p, Ope
 // Adds the parts of a product up, in order: eight values of a row to a thread.
 template <bool BF16>
 __global__ void __launch_bounds__(256) join_parts_kernel(const float* parts, uint32_t splits, uint32_t m, uint32_t n, void* out, int64_t out_stride) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;");
+    wait_for_stream();
+    release_stream();
     const uint64_t size = (uint64_t)m * n, at = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 8;
     if (at >= size) return;
     float4 sum[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
@@ -456,7 +456,7 @@ uint64_t cut_up(Products* ps, uint32_t sms) {
 }
 
 template <int EPI, bool PAIR, int TN, bool BF16>
-int launch_products(Products& ps, Operand* (&ops)[kMostProducts][4], uint32_t sms, bool early, float* parts, cudaStream_t stream) {
+int launch_products(Products& ps, Operand* (&ops)[kMostProducts][4], uint32_t sms, float* parts, cudaStream_t stream) {
     using Shape = TileShape<EPI, PAIR, TN>;
     constexpr uint32_t kRowsX = EPI == kGate && !PAIR ? TN / 2 : Shape::kRowsB;
     uint32_t end = 0;
@@ -485,7 +485,7 @@ int launch_products(Products& ps, Operand* (&ops)[kMostProducts][4], uint32_t sm
         if (!rc && p.gate) rc = tile_map(&ps.up, Values::f32, p.up, 2, result, packed, 32);
     }
     if (rc) return rc;
-    const LaunchAt at{dim3(PAIR ? 2 * min(sms / 2, end) : min(sms, end)), 192, Shape::smem, PAIR ? 2u : 1u, early, stream};
+    const LaunchAt at{dim3(PAIR ? 2 * min(sms / 2, end) : min(sms, end)), 192, Shape::smem, PAIR ? 2u : 1u, true, stream};
     rc = launch<product_kernel<EPI, PAIR, TN, BF16>>(at, ps);
     for (uint32_t i = 0; i < ps.count && !rc; ++i) {
         const Product& p = ps.of[i];
@@ -498,10 +498,9 @@ int launch_products(Products& ps, Operand* (&ops)[kMostProducts][4], uint32_t sm
 
 // Tiles of 256 x 256 by pairs of CTAs.  The kernels with work at the end of a tile take tiles of 128 x 128 by single CTAs where the large ones
 // would leave multiprocessors idle (us, large and small: gate of 512 x 4096 x 1024, 64 large tiles, 15 and 18; gradient, 32 tiles, 22 and 17;
-// gradient of 2048 x 4096 x 1024, 128 tiles, 39 and 43).  `early`: the kernel before it in the stream is one of this call.
-// parts: room for what cut_up says.
+// gradient of 2048 x 4096 x 1024, 128 tiles, 39 and 43).  parts: room for what cut_up says.
 template <int EPI>
-int products(bool bf16, Products& ps, Operand* (&ops)[kMostProducts][4], bool early, float* parts, cudaStream_t stream) {
+int products(bool bf16, Products& ps, Operand* (&ops)[kMostProducts][4], float* parts, cudaStream_t stream) {
     uint32_t sms;
     const int rc = sm_count(&sms);
     if (rc) return rc;
@@ -513,9 +512,9 @@ int products(bool bf16, Products& ps, Operand* (&ops)[kMostProducts][4], bool ea
         p.part_chunks = p.chunks0 + p.chunks1;
         const uint64_t large = ceil_div(p.m, 256) * ceil_div(p.n, EPI == kGate ? 128 : 256);
         if (large < (EPI == kGate ? sms / 4 : sms / 2))
-            return bf16 ? launch_products<EPI, false, 128, true>(ps, ops, sms, early, parts, stream) : launch_products<EPI, false, 128, false>(ps, ops, sms, early, parts, stream);
+            return bf16 ? launch_products<EPI, false, 128, true>(ps, ops, sms, parts, stream) : launch_products<EPI, false, 128, false>(ps, ops, sms, parts, stream);
     }
-    return bf16 ? launch_products<EPI, true, 256, true>(ps, ops, sms, early, parts, stream) : launch_products<EPI, true, 256, false>(ps, ops, sms, early, parts, stream);
+    return bf16 ? launch_products<EPI, true, 256, true>(ps, ops, sms, parts, stream) : launch_products<EPI, true, 256, false>(ps, ops, sms, parts, stream);
 }
 
 Product plain(uint32_t m, uint32_t n, void* out) {
@@ -651,8 +650,8 @@ extern "C" int mmee_gated_ffn(const mmee_workload_t* workload, const mmee_gated_
     Plan gate, down;
     plan_forward(s, *f, &gate, &down);
     if ((rc = check_space(f->workspace, f->workspace_bytes, &down, 0))) return rc;
-    if ((rc = products<kGate>(bf16, gate.ps, gate.ops, false, nullptr, stream))) return rc;
-    return products<kPlain>(bf16, down.ps, down.ops, true, static_cast<float*>(f->workspace), stream);
+    if ((rc = products<kGate>(bf16, gate.ps, gate.ops, nullptr, stream))) return rc;
+    return products<kPlain>(bf16, down.ps, down.ops, static_cast<float*>(f->workspace), stream);
 }
 
 extern "C" int mmee_gated_ffn_backward(const mmee_workload_t* workload, const mmee_gated_ffn_t* f, const mmee_gated_ffn_grad_t* g,
@@ -671,8 +670,8 @@ extern "C" int mmee_gated_ffn_backward(const mmee_workload_t* workload, const mm
     if ((rc = check_space(f->workspace, f->workspace_bytes, &rest, inner))) return rc;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool bf16 = f->dtype == MMEE_BF16;
-    if ((rc = products<kGrad>(bf16, grad.ps, grad.ops, false, nullptr, stream))) return rc;
-    return products<kPlain>(bf16, rest.ps, rest.ops, true, reinterpret_cast<float*>(static_cast<char*>(f->workspace) + inner), stream);
+    if ((rc = products<kGrad>(bf16, grad.ps, grad.ops, nullptr, stream))) return rc;
+    return products<kPlain>(bf16, rest.ps, rest.ops, reinterpret_cast<float*>(static_cast<char*>(f->workspace) + inner), stream);
 }
 
 extern "C" int mmee_gated_ffn_workspace(const mmee_workload_t* w, uint32_t backward, uint64_t* bytes) {

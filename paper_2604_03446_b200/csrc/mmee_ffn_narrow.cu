@@ -66,7 +66,10 @@ __global__ void __launch_bounds__(192) ffn_narrow_kernel(const __grid_constant__
     tcgen05_fence_after();
     const uint32_t tmem = tmem_base;
     volatile uint32_t* const lost = &gave_up;
-    if (GATE) asm volatile("griddepcontrol.launch_dependents;");
+    if (GATE) {
+        wait_for_stream();
+        release_stream();
+    }
 
     if (warp == 4) {
         if (elect_one()) {
@@ -83,7 +86,10 @@ __global__ void __launch_bounds__(192) ffn_narrow_kernel(const __grid_constant__
             };
             const uint32_t ahead = min(n, z.stages);
             for (uint32_t i = 0; i < ahead; ++i) load_w(i);
-            if (!GATE) asm volatile("griddepcontrol.wait;" ::: "memory");
+            if (!GATE) {                               // (the weights do not come from the gate kernel)
+                wait_for_stream();
+                release_stream();
+            }
             for (uint32_t i = 0; i < ahead; ++i) load_x(i);
             uint32_t sent = ahead;
             bool sound = true;
@@ -215,7 +221,7 @@ int launch_narrow(const FfnTokens& p, cudaStream_t stream) {
     // Parts of the reduction: as many as fill the multiprocessors twice, of two steps at least.
     const uint32_t tiles = (uint32_t)ceil_div(rows, kRowsW), most = (uint32_t)ceil_div(depth, 128);
     const uint32_t parts = max(1u, min(min(8u, 2 * sms / tiles), most));
-    const LaunchAt at{dim3(tiles * parts), 192, kNarrowSmem, parts, !GATE, stream};
+    const LaunchAt at{dim3(tiles * parts), 192, kNarrowSmem, parts, true, stream};
     return launch<ffn_narrow_kernel<GATE, BF16>>(at, w0, GATE ? w1 : w0, x, p, z);
 }
 

@@ -94,12 +94,11 @@ __global__ void __launch_bounds__(kMostWarps * 32, 2) ffn_tokens_kernel(const Ff
     };
     const uint32_t step = warps * kTurn;
     uint32_t k = warp * kTurn;
+    if (GATE) wait_for_stream();                       // (the weights of the second kernel do not come from the first)
     weights(w[0], k);
     weights(w[1], k + step);
-    if (GATE)
-        asm volatile("griddepcontrol.launch_dependents;");
-    else
-        asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!GATE) wait_for_stream();
+    release_stream();
     for (; k < depth; k += 2 * step) {
         multiply(w[0], k);
         weights(w[0], k + 2 * step);
@@ -138,7 +137,7 @@ int launch_both(const FfnTokens& p, cudaStream_t stream) {
         while (n < kMostWarps && n * 2 * turn <= depth) n *= 2;
         return 32 * n;
     };
-    const LaunchAt gate{dim3((uint32_t)ceil_div(p.d_ff, 16)), threads(p.d_in, 64), 0, 1, false, stream};
+    const LaunchAt gate{dim3((uint32_t)ceil_div(p.d_ff, 16)), threads(p.d_in, 64), 0, 1, true, stream};
     const LaunchAt down{dim3((uint32_t)ceil_div(p.d_out, 16)), threads(p.d_ff, 128), 0, 1, true, stream};
     const int rc = launch<ffn_tokens_kernel<true, BF16>>(gate, p);
     return rc ? rc : launch<ffn_tokens_kernel<false, BF16>>(down, p);

@@ -70,6 +70,15 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     return true;
 }
 
+// --- the order of kernels in a stream -------------------------------------------------------------------------------
+
+// A kernel that was launched early (LaunchAt::early) may run beside the one before it until it waits here; then that one is done, and
+// so is all before it.  Nothing in memory is touched before, but what no kernel of the same call writes.
+__device__ __forceinline__ void wait_for_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// From here on (in every block) the next kernel may be launched early.  After the wait: a kernel never runs beside any but the one
+// before it.
+__device__ __forceinline__ void release_stream() { asm volatile("griddepcontrol.launch_dependents;"); }
+
 // --- TMA ------------------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ void tma_prefetch(const CUtensorMap* map) {

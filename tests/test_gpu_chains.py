@@ -72,6 +72,59 @@ def test_a_captured_layer_replays_with_other_inputs_beside_eager_calls():
             assert torch.equal(out[n], want[n]) and torch.equal(eager[n], want[n]), n
 
 
+def test_a_capture_in_which_copies_and_fills_come_between():
+    """Kernels that start early wait for whatever is before them: copies, fills, other kernels, searches."""
+    t, src = inputs(), inputs(seed=7)
+    cfg = mi.config1()
+    h = mm.mmee_create(cfg["workload"], cfg["arch"], cfg["searches"][0])
+    buf = mm.result_buffer(1)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for n in t:
+            t[n].zero_()
+        for n in t:
+            t[n].copy_(src[n])
+        first = layer(t)
+        mm.mmee_search(h, buf)
+        t["q"].copy_(first["o"])
+        second = layer(t)
+        t["q"].fill_(0)
+    want = layer(src)
+    src2 = dict(src, q=want["o"])
+    want2 = layer(src2)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    mm.mmee_destroy(h)
+    for n in want:
+        assert torch.equal(first[n], want[n]) and torch.equal(second[n], want2[n]), n
+    assert float(t["q"].abs().max()) == 0
+
+
+def test_calls_that_feed_each_other_and_reuse_their_memory():
+    """Every call's output is the next one's input, its weights even, in place: none may start to read or write before."""
+    t = inputs(heads=4, kv_heads=4, d=64, d_ff=256)    # width 256
+    def chain(clone):
+        x = t["q"].clone()
+        w = [t[n].clone() for n in ("w_gate", "w_up", "w_down")]
+        for _ in range(6):
+            o, saved = mm.mmee_attention(x, t["k"], t["v"], kv_len=t["kv_len"])
+            rows = o.view(-1, 256)
+            y, kept = mm.mmee_gated_ffn(rows, *w, save=True)
+            few, _ = mm.mmee_gated_ffn(rows[:5], *w)
+            grads = mm.mmee_gated_ffn_backward(y, rows, *w, kept)
+            x.copy_(y.view(x.shape))
+            x[0, :5] = few.view(5, 4, 64)
+            for p, g in zip(w, grads[1:]):
+                p.add_(g, alpha=-1e-3)
+            if clone:
+                torch.cuda.synchronize()
+        return x, w
+    a, b = chain(True), chain(False)
+    torch.cuda.synchronize()
+    assert torch.equal(a[0], b[0]) and all(torch.equal(p, q) for p, q in zip(a[1], b[1]))
+
+
 def test_two_layers_at_once_on_two_streams():
     a, b = inputs(seed=3), inputs(seed=4, tokens=33, states=1000)
     want = layer(a), layer(b)
