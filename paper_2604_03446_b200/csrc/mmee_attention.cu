@@ -6,7 +6,7 @@
 // row, so that no reduction crosses threads) turns it into P in place, which the next matrix instruction takes from there.
 // While one tile's scores are turned, the tensor cores work for the other.
 //
-// 32/8 heads, 4096 queries, 8192 keys, d 128, bf16: 505 us, 1090 TFLOP/s.  The tensor cores are at work 56 % of the time, the
+// 32/8 heads, 4096 queries, 8192 keys, d 128, bf16: 514 us, 1070 TFLOP/s.  The tensor cores are at work 56 % of active cycles, the
 // exponentials' units as much.  What bounds it is a tile's way through a turn (scores read, maximum, 128 exponentials a thread,
 // written, P V, the next scores), which is longer than the other tile's products.  Measured on the way (narrow inputs, 459 us as it is):
 // exponentials on the multiply-add pipes for a quarter of the values 479; two warpgroups a tile, half a row to a thread, 490; blocks

@@ -7,7 +7,7 @@
 // and are operands of the next matrix instruction there.
 //
 // 2 x 32/8 heads, 2048 queries, 4096 keys, d 128, bf16: dK and dV 480 us (1140 TFLOP/s of its four products), dQ 357 us (1150 of its
-// three).  The tensor cores are at work 60 to 67 % of the time; what bounds them is the chain of a turn (scores, P, its product,
+// three).  The tensor cores are at work 60 to 67 % of active cycles; what bounds them is the chain of a turn (scores, P, its product,
 // dP, dS, its product), of which half is the registers' and half the tensor cores', with one tile of each to a CTA: tensor memory is full.
 //
 // In fp16 P is kept 2^12 larger, and dS by a power of two for which the largest value that these tensors allow,
