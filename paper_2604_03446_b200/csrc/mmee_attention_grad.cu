@@ -10,8 +10,9 @@
 // three).  The tensor cores are at work 60 to 67 % of active cycles; what bounds them is the chain of a turn (scores, P, its product,
 // dP, dS, its product), of which half is the registers' and half the tensor cores', with one tile of each to a CTA: tensor memory is full.
 //
-// In fp16 P is kept 2^12 larger, and dS by a power of two for which the largest value that these tensors allow,
-// 2 d_v max|dO| max|V|, still fits: gradients much smaller than one keep their bits.  Both leave the results exactly.
+// In fp16 P is kept 2^12 larger, and dS by a power of two for which the largest value that a sequence and key head allow,
+// 2 d_v max|dO| max|V| over its rows and valid keys, still fits: gradients much smaller than one keep their bits, whatever other
+// sequences and heads hold.  Both leave the results exactly.
 #include "mmee_attention.cuh"
 
 namespace mmee {
@@ -28,7 +29,7 @@ struct GradParams {
     Strides vs;
     uint32_t kv_heads;
     float* delta;                      // [batch][q_heads][seq_q]
-    uint32_t* most;                    // fp16: bits of max|dO| and of max|V|
+    uint32_t* most;                    // fp16: [batch][kv_heads] bits of max|dO| and of max|V|
     void *dq, *dk, *dv;
     Strides dqs, dks, dvs;
 };
@@ -36,18 +37,26 @@ struct GradParams {
 template <bool BF16>
 __device__ constexpr float kPShift = BF16 ? 0.f : 12.f;
 
-// Power of two that dS is kept larger by.
+// Power of two that dS of a key head is kept larger by.
 template <bool BF16>
-__device__ __forceinline__ int ds_shift(const GradParams& p) {
+__device__ __forceinline__ int ds_shift(const GradParams& p, uint32_t b, uint32_t kv_head) {
     if (BF16) return 0;
-    const float bound = 2.f * (float)p.a.d_v * __uint_as_float(p.most[0]) * __uint_as_float(p.most[1]);
-    if (!(bound > 0.f) || !(bound < INFINITY)) return 0;
+    const uint32_t* const most = p.most + 2 * ((uint64_t)b * p.kv_heads + kv_head);
+    const float bound = 2.f * (float)p.a.d_v * __uint_as_float(most[0]) * __uint_as_float(most[1]);
+    if (!(bound > 0.f)) return 0;
     return max(-100, min(100, 14 - ilogbf(bound)));
 }
 
+// An entry's size for that bound.  Infinities and NaN make their own row or key no number under any power, and are not to
+// take the others' bits.
+__device__ __forceinline__ float finite_size(float x) {
+    const float a = fabsf(x);
+    return a < INFINITY ? a : 0.f;
+}
+
 // delta of every query row, half a warp to a row, from o and what its rounding took off (o alone would add four fifths of the error that
-// a rounding of dQ and dK is: 384 queries, 512 keys, fp16); in fp16 also the largest sizes in dO and in V's valid rows (their order
-// does not matter).  A block takes 64 tokens of a head.
+// a rounding of dQ and dK is: 384 queries, 512 keys, fp16); in fp16 also the largest sizes in dO and in V's valid rows, of each key head
+// (their order does not matter).  A block takes 64 tokens of a head.
 constexpr uint32_t kRowsOfBlock = 64;
 template <bool BF16>
 __global__ void __launch_bounds__(256) grad_rows_kernel(const GradParams p) {
@@ -83,14 +92,14 @@ __global__ void __launch_bounds__(256) grad_rows_kernel(const GradParams p) {
         for (int j = 0; j < 4; ++j) {
             const float2 f = unpack2<BF16>(xs[j]), g = unpack2<BF16>(ys[j]), r = unpack2<BF16>(rs[j]);
             sum += f.x * (g.x + r.x) + f.y * (g.y + r.y);
-            if (!BF16) most[0] = fmaxf(most[0], fmaxf(fabsf(f.x), fabsf(f.y)));
+            if (!BF16) most[0] = fmaxf(most[0], fmaxf(finite_size(f.x), finite_size(f.y)));
         }
         if (!BF16) {
             const uint32_t zs[4] = {z[i].x, z[i].y, z[i].z, z[i].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float2 f = unpack2<BF16>(zs[j]);
-                most[1] = fmaxf(most[1], fmaxf(fabsf(f.x), fabsf(f.y)));
+                most[1] = fmaxf(most[1], fmaxf(finite_size(f.x), finite_size(f.y)));
             }
         }
         for (int d = 8; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -107,7 +116,9 @@ __global__ void __launch_bounds__(256) grad_rows_kernel(const GradParams p) {
         if (threadIdx.x < 2) {
             float m = 0.f;
             for (int w = 0; w < 8; ++w) m = fmaxf(m, largest[threadIdx.x][w]);
-            atomicMax(p.most + threadIdx.x, __float_as_uint(m));
+            // dO counts for the key head that this query head shares; V comes with the blocks of the first heads, its own head's.
+            const uint32_t kv_head = threadIdx.x == 0 ? head / a.group : head;
+            if (kv_head < p.kv_heads) atomicMax(p.most + 2 * ((uint64_t)b * p.kv_heads + kv_head) + threadIdx.x, __float_as_uint(m));
         }
     }
 }
@@ -287,7 +298,7 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     } else {
         const uint32_t half = warp / 4, row = (warp % 4) * 32 + lane, lanes = ((warp % 4) * 32) << 16;
         const float sl2 = a.scale * kLog2e;
-        const int shift = n ? ds_shift<BF16>(p) : 0;
+        const int shift = n ? ds_shift<BF16>(p, b, head) : 0;
         const float ds_scale = exp2f((float)shift - kPShift<BF16>);
         const bool valid = k0 + row < keys, whole = k0 + kTile <= keys;
         const uint64_t scale2 = pair(sl2, sl2), ds_scale2 = pair(ds_scale, ds_scale);
@@ -534,7 +545,7 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     } else {
         const uint32_t half = warp / 4, row = (warp % 4) * 32 + lane, lanes = ((warp % 4) * 32) << 16, token = q0 + row;
         const float sl2 = a.scale * kLog2e;
-        const int shift = n ? ds_shift<BF16>(p) : 0;
+        const int shift = n ? ds_shift<BF16>(p, b, head / a.group) : 0;
         const uint64_t at = ((uint64_t)b * a.q_heads + head) * a.seq_q + token;
         const bool in = token < a.seq_q;
         // dS = 2^shift exp2(S sl2 - log) (dP - delta): the power goes into the exponent.  Rows that count nothing: exp2(-infinity).
@@ -628,7 +639,7 @@ int launch_grads(const Problem& x, const View& d_o, const GradParams& p, cudaStr
     if (!rc) rc = view_map(&mv, BF16, a.batch, x.v);
     if (!rc) rc = view_map(&mo, BF16, a.batch, d_o);
     if (rc) return rc;
-    if (!BF16 && (rc = cuda_status(cudaMemsetAsync(p.most, 0, 8, stream)))) return rc;
+    if (!BF16 && (rc = cuda_status(cudaMemsetAsync(p.most, 0, 8ull * a.batch * p.kv_heads, stream)))) return rc;
     const uint32_t longest = BF16 ? a.seq_q : max(a.seq_q, a.seq_kv);
     using Shape = GradShape<DK, DV>;
     const LaunchAt rows{dim3((uint32_t)ceil_div(longest, kRowsOfBlock), a.q_heads, a.batch), 256, 0, 1, BF16, stream};       // (fp16: after the memset)
@@ -644,7 +655,9 @@ int grads_typed(const Problem& x, const View& d_o, const GradParams& p, cudaStre
     return x.bf16 ? launch_grads<DK, DV, true>(x, d_o, p, stream) : launch_grads<DK, DV, false>(x, d_o, p, stream);
 }
 
+// The workspace: delta, then the largest sizes of each sequence and key head.
 uint64_t rows_bytes(const mmee_workload_t& w) { return round_up((uint64_t)w.batch * w.q_heads * w.seq_q * 4, 16); }
+uint64_t space_bytes(const mmee_workload_t& w) { return rows_bytes(w) + round_up((uint64_t)w.batch * w.kv_heads * 8, 16); }
 
 }  // namespace
 
@@ -661,7 +674,7 @@ using namespace mmee;
 
 extern "C" int mmee_attention_backward_workspace(const mmee_workload_t* w, uint64_t* bytes) {
     if (!w || !bytes) return MMEE_ERR_ARG;
-    *bytes = rows_bytes(*w) + 16;
+    *bytes = space_bytes(*w);
     return MMEE_OK;
 }
 
@@ -677,7 +690,7 @@ extern "C" int mmee_attention_backward(const mmee_workload_t* workload, const mm
     const View dv{g->d_v, w.seq_kv, w.kv_heads, w.d_v, strides(g->d_v_stride)};
     for (const View* v : {&d_o, &dq, &dk, &dv})
         if (check_view(*v, w.batch)) return MMEE_ERR_ARG;
-    if (!g->workspace || !aligned16(g->workspace) || g->workspace_bytes < rows_bytes(w) + 16) return MMEE_ERR_ARG;
+    if (!g->workspace || !aligned16(g->workspace) || g->workspace_bytes < space_bytes(w)) return MMEE_ERR_ARG;
     GradParams p{};
     p.a = x.p;
     p.d_o = g->d_o;
