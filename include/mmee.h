@@ -502,7 +502,8 @@ int mmee_gated_ffn(const mmee_workload_t* workload, const mmee_gated_ffn_t* f, v
 /*
  * mmee_gated_ffn_backward -- the gradients of x and the three weights for a gradient d_y of y, from the
  * `hidden` and `kept` that the forward call wrote for the same x and weights.  The gradients of gate and up
- * are rounded once to the tensors' type, each result once.
+ * are rounded once to the tensors' type (in fp16 a power of two larger, so that small ones keep their bits and large
+ * ones fit), each result once.
  */
 typedef struct {
     const void *d_y;                         /* tokens x J                                        */

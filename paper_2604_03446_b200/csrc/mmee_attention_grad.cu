@@ -42,16 +42,7 @@ template <bool BF16>
 __device__ __forceinline__ int ds_shift(const GradParams& p, uint32_t b, uint32_t kv_head) {
     if (BF16) return 0;
     const uint32_t* const most = p.most + 2 * ((uint64_t)b * p.kv_heads + kv_head);
-    const float bound = 2.f * (float)p.a.d_v * __uint_as_float(most[0]) * __uint_as_float(most[1]);
-    if (!(bound > 0.f)) return 0;
-    return max(-100, min(100, 14 - ilogbf(bound)));
-}
-
-// An entry's size for that bound.  Infinities and NaN make their own row or key no number under any power, and are not to
-// take the others' bits.
-__device__ __forceinline__ float finite_size(float x) {
-    const float a = fabsf(x);
-    return a < INFINITY ? a : 0.f;
+    return fp16_shift(2.f * (float)p.a.d_v * __uint_as_float(most[0]) * __uint_as_float(most[1]), 100);
 }
 
 // delta of every query row, half a warp to a row, from o and what its rounding took off (o alone would add four fifths of the error that
@@ -299,7 +290,7 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         const uint32_t half = warp / 4, row = (warp % 4) * 32 + lane, lanes = ((warp % 4) * 32) << 16;
         const float sl2 = a.scale * kLog2e;
         const int shift = n ? ds_shift<BF16>(p, b, head) : 0;
-        const float ds_scale = exp2f((float)shift - kPShift<BF16>);
+        const float ds_scale = power_of_two(shift - (int)kPShift<BF16>);
         const bool valid = k0 + row < keys, whole = k0 + kTile <= keys;
         const uint64_t scale2 = pair(sl2, sl2), ds_scale2 = pair(ds_scale, ds_scale);
         const uint32_t s_at = s_col + lanes + 64 * half, dp_at = dp_col + lanes + 64 * half;
@@ -374,7 +365,7 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
         tcgen05_fence_after();
         if (sound) {
             const uint32_t token = k0 + row;
-            const float by_v = exp2f(-kPShift<BF16>), by_k = a.scale * exp2f((float)-shift);
+            const float by_v = power_of_two(-(int)kPShift<BF16>), by_k = a.scale * power_of_two(-shift);
             auto write = [&](uint32_t col, uint32_t d, uint32_t width, void* to, const Strides& st, float by) {
                 for (uint32_t c = half * d / 2; c < (half + 1) * d / 2; c += 32) {
                     uint32_t x[32];
@@ -593,7 +584,7 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
         if (n && sound) sound = mbar_wait(sums_full, 0, lost);
         tcgen05_fence_after();
         if (sound) {
-            const float by = a.scale * exp2f((float)-shift);
+            const float by = a.scale * power_of_two(-shift);
             for (uint32_t c = half * DK / 2; c < (half + 1) * DK / 2; c += 32) {
                 uint32_t x[32];
                 if (n) {

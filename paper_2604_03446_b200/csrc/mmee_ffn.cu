@@ -8,7 +8,9 @@
 // thread, which applies activation and product.
 //
 // Roundings: sums, gate, up and the gradient of h in 32 bits; h, dg and du are rounded once each to the type of the
-// operands, which the tensor cores need; results once.
+// operands, which the tensor cores need; results once.  In fp16 dg and du are kept larger by a power of two for which a bound on
+// them fits (grad_bound_kernel), which leaves the results exactly: gradients far below one keep their bits, large ones do not
+// overflow on the way.
 #include "mmee_ffn.cuh"
 
 namespace mmee {
@@ -31,6 +33,7 @@ struct Product {
     int64_t out_stride;                // elements from row to row of out and out2
     float* parts;                      // splits > 1: [splits][m][n]
     float *gate, *up;                  // kGate: where to keep them, or null; kGrad: what was kept.  Rows of n
+    uint32_t scaled;                   // fp16: dg and du leave it (kGrad) or go into it a power of two larger
 };
 
 constexpr uint32_t kMostProducts = 4;
@@ -40,6 +43,9 @@ struct Products {
     CUtensorMap out2, gate, up;        // kGate, kGrad: of the only product
     Product of[kMostProducts];
     uint32_t count;
+    // fp16: bounds by grad_bound_kernel, of the tokens' parts, then of the weights'; multiples of four
+    const float* bounds;
+    uint32_t token_bounds, weight_bounds;
 };
 
 // A tile: 128 rows to a CTA, PAIR: of two CTAs that share the columns' operand.
@@ -67,6 +73,23 @@ __device__ __forceinline__ void tile_of(const Product& p, uint32_t i, uint32_t* 
     const uint32_t rows = min(kGroup, p.tiles_m - first), r = i - g * per;
     *tm = first + r % rows;
     *tn = r / rows;
+}
+
+// Power of two that dg and du are kept larger by in fp16, by a whole warp.  (Not above 2^60: dh, which meets it first, stays finite
+// in 32 bits.)
+__device__ __forceinline__ int grad_shift(const Products& ps) {
+    const uint32_t lane = threadIdx.x & 31u;
+    auto largest = [&](const float* from, uint32_t n) {
+        float most = 0.f;
+#pragma unroll 8
+        for (uint32_t i = 4 * lane; i < n; i += 128) {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(from + i));
+            most = fmaxf(fmaxf(most, fmaxf(v.x, v.y)), fmaxf(v.z, v.w));
+        }
+        for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        return most;
+    };
+    return fp16_shift(largest(ps.bounds, ps.token_bounds) * largest(ps.bounds + ps.token_bounds, ps.weight_bounds), 60);
 }
 
 template <int EPI, bool PAIR, int TN, bool BF16>
@@ -117,8 +140,13 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
     tcgen05_fence_after();
     const uint32_t tmem = tmem_base;
     volatile uint32_t* const lost = &gave_up;
-    wait_for_stream();
-    release_stream();
+    // fp16 gradients: the kernel before this one finds their bounds, which the results alone need; operands come from before that
+    // kernel, which has waited for them.
+    constexpr bool kBounds = EPI == kGrad && !BF16;
+    if constexpr (!kBounds) {
+        wait_for_stream();
+        release_stream();
+    }
     const uint32_t n_tiles = ps.of[ps.count - 1].end;
     // The product that tile i is part of, and the tile's number there.
     auto product_of = [&](uint32_t i, uint32_t* at) {
@@ -224,6 +252,13 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
     } else {                                           // results
         uint32_t n = 0, stores = 0, kept = 0;          // tiles, groups of stores, pieces of gate and up asked for
         const uint32_t mine = tiles + kStages * kStage + warp * Shape::kParts * kPart;
+        if constexpr (kBounds) {
+            wait_for_stream();
+            release_stream();
+        }
+        float larger = 1.f;                            // fp16: the power of two in dh; out of it again in the products of dg and du
+        if constexpr (!BF16 && EPI != kGate)
+            if (ps.of[0].scaled) larger = power_of_two(EPI == kGrad ? grad_shift(ps) : -grad_shift(ps));
         auto part = [&](uint32_t i) { return mine + i * kPart; };
         // Lays a row of 64 results down, two to a word.
         auto lay = [&](uint32_t to, const uint32_t* v) {
@@ -272,6 +307,12 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
                     if (EPI == kGate) tmem_load32(acc + TN / 2 + d, y);
                     tmem_loaded32(x);
                     if (EPI == kGate) tmem_loaded32(y);
+                    if constexpr (!BF16 && EPI != kGate) {
+                        if (p.scaled) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * larger);
+                        }
+                    }
                     if (EPI == kPlain && p.splits > 1) {
                         if (d < cols) {                // a part, in 32 bits
                             const uint32_t to = part(stores & 1);
@@ -414,6 +455,83 @@ void add_product(Products* ps, Operand* (&ops)[kMostProducts][4], Product p, Ope
     ps->of[ps->count++] = p;
 }
 
+// What dg and du are at most, as the product of two maxima over its blocks: of |w_down|, and over the tokens of sqrt(J) |d_y| times
+// the largest of what dh meets -- |dh| is at most the 2-norm of the token's d_y times that of a column of w_down.  Typical values lie
+// some 2^12 below the bound, 16 bits above fp16's smallest normal value then.
+// Bound by memory, as gate, up and w_down are read once more; a token to a block at a time, so that few tokens have many loads under
+// way.  The gradient's kernel, which needs the bounds for its results alone, starts beside it.  us of forward and gradients without and
+// with it: 777 tokens, 1000-2728-712, 113 and 114; 512 tokens, 1024-4096-1024, 86 and 87; 64 tokens, 2048-5464-2048, 96 and 103; eight
+// tokens, 4096-16384-4096, 303 and 329 (25 of them w_down's 134 MB).
+constexpr uint32_t kTokenBounds = 1024, kWeightBounds = 592;
+struct BoundParams {
+    const uint16_t *d_y, *w_down;
+    int64_t d_y_stride, w_down_stride;
+    const float *gate, *up;
+    uint32_t tokens, d_ff, d_out, act;
+    float* bounds;
+    uint32_t token_bounds;
+};
+
+__global__ void __launch_bounds__(256) grad_bound_kernel(const BoundParams p) {
+    __shared__ float found[2][8];
+    wait_for_stream();
+    release_stream();
+    const uint32_t warp = threadIdx.x >> 5;
+    auto over_block = [&](float v, uint32_t at, bool sum) {
+        for (int d = 16; d; d >>= 1) {
+            const float x = __shfl_xor_sync(0xffffffffu, v, d);
+            v = sum ? v + x : fmaxf(v, x);
+        }
+        if ((threadIdx.x & 31u) == 0) found[at][warp] = v;
+        __syncthreads();
+        v = found[at][0];
+        for (int w = 1; w < 8; ++w) v = sum ? v + found[at][w] : fmaxf(v, found[at][w]);
+        return v;
+    };
+    float most = 0.f;
+    if (blockIdx.x >= p.token_bounds) {
+        for (uint32_t row = blockIdx.x - p.token_bounds; row < p.d_out; row += gridDim.x - p.token_bounds) {
+            const uint16_t* const from = p.w_down + (int64_t)row * p.w_down_stride;
+#pragma unroll 4
+            for (uint32_t i = threadIdx.x * 8; i < p.d_ff; i += 256 * 8) {
+                const uint4 v = *reinterpret_cast<const uint4*>(from + i);
+                for (const uint32_t w : {v.x, v.y, v.z, v.w}) {
+                    const float2 f = unpack2<false>(w);
+                    most = fmaxf(most, fmaxf(finite_size(f.x), finite_size(f.y)));
+                }
+            }
+        }
+        most = over_block(most, 0, false);
+    } else {
+        for (uint32_t token = blockIdx.x; token < p.tokens; token += p.token_bounds) {
+            // dh meets up times the activation's slope (1.13 at most, gelu's) and the activation: one at most for sigmoid, |gate| for the others.
+            float meets = 0.f, squares = 0.f;
+            const uint64_t at = (uint64_t)token * p.d_ff;
+            const bool by_gate = p.act != MMEE_ACT_SIGMOID;
+#pragma unroll 4
+            for (uint32_t i = threadIdx.x * 4; i < p.d_ff; i += 256 * 4) {
+                const float4 g = by_gate ? __ldcs(reinterpret_cast<const float4*>(p.gate + at + i)) : make_float4(1.f, 1.f, 1.f, 1.f);
+                const float4 u = __ldcs(reinterpret_cast<const float4*>(p.up + at + i));
+                for (const float v : {g.x, g.y, g.z, g.w, 1.13f * u.x, 1.13f * u.y, 1.13f * u.z, 1.13f * u.w}) meets = fmaxf(meets, finite_size(v));
+            }
+            const uint16_t* const d_y = p.d_y + (int64_t)token * p.d_y_stride;
+            for (uint32_t i = threadIdx.x * 8; i < p.d_out; i += 256 * 8) {
+                const uint4 v = *reinterpret_cast<const uint4*>(d_y + i);
+                for (const uint32_t w : {v.x, v.y, v.z, v.w}) {
+                    const float2 f = unpack2<false>(w);
+                    const float a = finite_size(f.x), b = finite_size(f.y);
+                    squares += a * a + b * b;
+                }
+            }
+            meets = over_block(meets, 0, false);
+            squares = over_block(squares, 1, true);
+            most = fmaxf(most, sqrtf(squares * (float)p.d_out) * meets);
+            __syncthreads();                           // (before the next token's are written)
+        }
+    }
+    if (threadIdx.x == 0) p.bounds[blockIdx.x] = most;
+}
+
 // Adds the parts of a product up, in order: eight values of a row to a thread.
 template <bool BF16>
 __global__ void __launch_bounds__(256) join_parts_kernel(const float* parts, uint32_t splits, uint32_t m, uint32_t n, void* out, int64_t out_stride) {
@@ -517,12 +635,13 @@ int products(bool bf16, Products& ps, Operand* (&ops)[kMostProducts][4], float* 
     return bf16 ? launch_products<EPI, true, 256, true>(ps, ops, sms, parts, stream) : launch_products<EPI, true, 256, false>(ps, ops, sms, parts, stream);
 }
 
-Product plain(uint32_t m, uint32_t n, void* out) {
+Product plain(uint32_t m, uint32_t n, void* out, bool scaled = false) {
     Product p{};
     p.m = m;
     p.n = n;
     p.out = out;
     p.out_stride = n;
+    p.scaled = scaled;
     return p;
 }
 
@@ -575,8 +694,20 @@ void plan_forward(const Sizes& s, const mmee_gated_ffn_t& f, Plan* gate, Plan* d
     add_product(&down->ps, down->ops, plain(s.tokens, s.d_out, f.y), &d[0], &d[1], nullptr, nullptr);
 }
 
+// The backward workspace: dg and du, the bounds, parts.
+uint64_t pair_bytes(const Sizes& s) { return 4 * (uint64_t)s.tokens * s.d_ff; }
+uint32_t token_bounds(const Sizes& s) { return (uint32_t)round_up(min(s.tokens, kTokenBounds), 4); }
+uint32_t weight_bounds(const Sizes& s) { return (uint32_t)round_up(min(s.d_out, kWeightBounds), 4); }
+uint64_t fixed_bytes(const Sizes& s) { return pair_bytes(s) + 4 * (token_bounds(s) + weight_bounds(s)); }
+
 void plan_backward(const Sizes& s, const mmee_gated_ffn_t& f, const mmee_gated_ffn_grad_t& g, Plan* grad, Plan* rest) {
     const uint64_t inner = (uint64_t)s.tokens * s.d_ff;            // (a multiple of eight)
+    const bool scaled = f.dtype == MMEE_F16;
+    for (Plan* const plan : {grad, rest}) {
+        plan->ps.bounds = reinterpret_cast<const float*>(static_cast<char*>(f.workspace) + pair_bytes(s));
+        plan->ps.token_bounds = token_bounds(s);
+        plan->ps.weight_bounds = weight_bounds(s);
+    }
     uint16_t* const dg = static_cast<uint16_t*>(f.workspace);
     uint16_t* const du = dg ? dg + inner : nullptr;
     Operand* const o = grad->held;
@@ -587,6 +718,7 @@ void plan_backward(const Sizes& s, const mmee_gated_ffn_t& f, const mmee_gated_f
     p.act = f.activation;
     p.gate = f.kept;
     p.up = f.kept ? f.kept + inner : nullptr;
+    p.scaled = scaled;
     grad->ps.count = 0;
     add_product(&grad->ps, grad->ops, p, &o[0], &o[1], nullptr, nullptr);
     // The other four products depend on nothing but these, and are one launch: the one with the longest reduction first.
@@ -601,10 +733,17 @@ void plan_backward(const Sizes& s, const mmee_gated_ffn_t& f, const mmee_gated_f
     r[7] = {f.hidden, s.tokens, s.d_ff, s.d_ff, true};
     r[8] = {g.d_y, s.tokens, s.d_out, g.d_y_stride, true};
     rest->ps.count = 0;
-    add_product(&rest->ps, rest->ops, plain(s.tokens, s.d_in, g.d_x), &r[0], &r[2], &r[1], &r[3]);
-    add_product(&rest->ps, rest->ops, plain(s.d_ff, s.d_in, g.d_w_gate), &r[4], &r[6], nullptr, nullptr);
-    add_product(&rest->ps, rest->ops, plain(s.d_ff, s.d_in, g.d_w_up), &r[5], &r[6], nullptr, nullptr);
+    add_product(&rest->ps, rest->ops, plain(s.tokens, s.d_in, g.d_x, scaled), &r[0], &r[2], &r[1], &r[3]);
+    add_product(&rest->ps, rest->ops, plain(s.d_ff, s.d_in, g.d_w_gate, scaled), &r[4], &r[6], nullptr, nullptr);
+    add_product(&rest->ps, rest->ops, plain(s.d_ff, s.d_in, g.d_w_up, scaled), &r[5], &r[6], nullptr, nullptr);
     add_product(&rest->ps, rest->ops, plain(s.d_out, s.d_ff, g.d_w_down), &r[8], &r[7], nullptr, nullptr);
+}
+
+int grad_bound(const Sizes& s, const mmee_gated_ffn_t& f, const mmee_gated_ffn_grad_t& g, cudaStream_t stream) {
+    const BoundParams p{static_cast<const uint16_t*>(g.d_y), static_cast<const uint16_t*>(f.w_down), g.d_y_stride, f.w_down_stride, f.kept,
+                        f.kept + (uint64_t)s.tokens * s.d_ff, s.tokens, s.d_ff, s.d_out, f.activation,
+                        reinterpret_cast<float*>(static_cast<char*>(f.workspace) + pair_bytes(s)), token_bounds(s)};
+    return launch<grad_bound_kernel>(LaunchAt{dim3(token_bounds(s) + weight_bounds(s)), 256, 0, 1, true, stream}, p);
 }
 
 // Workspace of a call: `fixed` bytes and the parts of the plan's products.
@@ -666,12 +805,12 @@ extern "C" int mmee_gated_ffn_backward(const mmee_workload_t* workload, const mm
         if (!o || !aligned16(o)) return MMEE_ERR_ARG;
     Plan grad, rest;
     plan_backward(s, *f, *g, &grad, &rest);
-    const uint64_t inner = 4 * (uint64_t)s.tokens * s.d_ff;        // bytes of dg and du
-    if ((rc = check_space(f->workspace, f->workspace_bytes, &rest, inner))) return rc;
+    if ((rc = check_space(f->workspace, f->workspace_bytes, &rest, fixed_bytes(s)))) return rc;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool bf16 = f->dtype == MMEE_BF16;
+    if (!bf16 && (rc = grad_bound(s, *f, *g, stream))) return rc;
     if ((rc = products<kGrad>(bf16, grad.ps, grad.ops, nullptr, stream))) return rc;
-    return products<kPlain>(bf16, rest.ps, rest.ops, reinterpret_cast<float*>(static_cast<char*>(f->workspace) + inner), stream);
+    return products<kPlain>(bf16, rest.ps, rest.ops, reinterpret_cast<float*>(static_cast<char*>(f->workspace) + fixed_bytes(s)), stream);
 }
 
 extern "C" int mmee_gated_ffn_workspace(const mmee_workload_t* w, uint32_t backward, uint64_t* bytes) {
@@ -685,5 +824,5 @@ extern "C" int mmee_gated_ffn_workspace(const mmee_workload_t* w, uint32_t backw
         plan_backward(s, mmee_gated_ffn_t{}, mmee_gated_ffn_grad_t{}, &first, &rest);
     else
         plan_forward(s, mmee_gated_ffn_t{}, &first, &rest);
-    return space_of(&rest, backward ? 4 * (uint64_t)s.tokens * s.d_ff : 0, bytes);
+    return space_of(&rest, backward ? fixed_bytes(s) : 0, bytes);
 }

@@ -6,6 +6,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 namespace mmee {
@@ -310,6 +311,21 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
+
+// An entry's size for a bound that a power of two is chosen by.  Infinities and NaN make their own row or column no number under
+// any power, and are not to take the others' bits.
+__device__ __forceinline__ float finite_size(float x) {
+    const float a = fabsf(x);
+    return a < INFINITY ? a : 0.f;
+}
+
+// The power of two (-100 to `most`) that values up to `bound` are kept larger by in fp16: they then end at 2^15.
+__device__ __forceinline__ int fp16_shift(float bound, int most) {
+    return bound > 0.f ? max(-100, min(most, 14 - ilogbf(bound))) : 0;
+}
+
+// 2^n for n from -126 to 127, exactly.
+__device__ __forceinline__ float power_of_two(int n) { return __uint_as_float((uint32_t)(127 + n) << 23); }
 
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
