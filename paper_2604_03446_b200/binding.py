@@ -27,7 +27,7 @@ EXPORTS = ("mmee_create", "mmee_search", "mmee_search_host", "mmee_destroy", "mm
            "mmee_query_vector", "mmee_recompute_flag", "mmee_row_pruning_keep", "mmee_last_search_stats", "mmee_kernel_timing",
            "mmee_alu_peak", "mmee_gated_ffn", "mmee_gated_ffn_backward", "mmee_gated_ffn_workspace",
            "mmee_attention", "mmee_attention_workspace", "mmee_attention_backward", "mmee_attention_backward_workspace",
-           "mmee_chain_status")
+           "mmee_chain_status", "mmee_chain_wait_limit")
 
 
 class Workload(C.Structure):
@@ -171,6 +171,7 @@ def library():
     L.mmee_attention_backward.argtypes = [C.POINTER(Workload), C.POINTER(Attention), C.POINTER(AttentionGrad), C.c_void_p]
     L.mmee_attention_backward_workspace.argtypes = [C.POINTER(Workload), C.POINTER(C.c_uint64)]
     L.mmee_chain_status.argtypes = []
+    L.mmee_chain_wait_limit.argtypes = [C.c_uint64]
     _lib = L
     return L
 
@@ -605,6 +606,11 @@ def mmee_gated_ffn_backward(d_y, x, w_gate, w_up, w_down, saved, activation: int
 def mmee_chain_status() -> None:
     """Raises once after a wait inside a chain's kernel ran out (its outputs are not a result).  Waits for the device."""
     _check(library().mmee_chain_status(), "mmee_chain_status")
+
+
+def mmee_chain_wait_limit(seconds: float = 4.0) -> None:
+    """How long a wait for a barrier in the chains' kernels on the current device may last.  Waits for the device."""
+    _check(library().mmee_chain_wait_limit(int(seconds * 1e9)), "mmee_chain_wait_limit")
 
 
 def read_results(buf, n: int):

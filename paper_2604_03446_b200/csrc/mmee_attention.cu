@@ -18,8 +18,6 @@ namespace mmee {
 
 namespace {
 
-__device__ uint32_t g_gave_up;
-
 // --- forward --------------------------------------------------------------------------------------------------------
 
 template <int DK, int DV>
@@ -99,39 +97,32 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     const uint32_t n = !cut_up ? t_all : t0 < t_all ? min(p.tiles_per_split, t_all - t0) : 0;     // key tiles of this CTA
     auto s_col = [&](uint32_t t) { return tmem + t * 128; };
     auto o_col = [&](uint32_t t) { return tmem + TILES * 128 + t * DV; };
+    uint32_t q_sent = 0, k_sent = 0, v_sent = 0;       // loads on their way or landed (of the thread that issues them)
 
     if (warp >= kLoad) {
         if constexpr (TILES == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         if (warp == kLoad) {
             if (elect_one() && n) {
                 const int32_t h = (int32_t)head, hk = (int32_t)(head / p.group), bb = (int32_t)b;
-                uint32_t k_sent = 0, v_sent = 0;
-                bool sound = true;
                 auto load_q = [&](uint32_t t) {
                     mbar_expect(q_full(t), Shape::kQ);
                     for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(q_tile(t) + j * kTile * kRowBytes, &mq, q_full(t), 64 * j, (int32_t)(q0 + t * kTile), h, bb);
+                    ++q_sent;
                 };
                 load_q(0);
                 for (uint32_t i = 0; i < n; ++i) {
                     const uint32_t s = i % kRing, turn = ((i / kRing) & 1) ^ 1;
                     const int32_t row = (int32_t)((t0 + i) * kTile);
-                    if (!(sound = mbar_wait(k_empty(s), turn, lost))) break;
+                    if (!mbar_wait(k_empty(s), turn, lost)) break;
                     mbar_expect(k_full(s), Shape::kQ);
                     for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(k_tile(s) + j * kTile * kRowBytes, &mk, k_full(s), 64 * j, row, hk, bb);
                     ++k_sent;
                     if (i == 0)
                         for (uint32_t t = 1; t < tiles; ++t) load_q(t);
-                    if (!(sound = mbar_wait(v_empty(s), turn, lost))) break;
+                    if (!mbar_wait(v_empty(s), turn, lost)) break;
                     mbar_expect(v_full(s), Shape::kV);
                     for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(v_tile(s) + j * kTile * kRowBytes, &mv, v_full(s), 64 * j, row, hk, bb);
                     ++v_sent;
-                }
-                if (!sound) {                              // what is in flight lands before the CTA ends
-                    for (uint32_t t = 0; t < (k_sent ? tiles : 1); ++t) mbar_wait(q_full(t), 0, nullptr);
-                    for (uint32_t s = 0; s < kRing; ++s) {
-                        if (k_sent > s) mbar_wait(k_full(s), ((k_sent - 1 - s) / kRing) & 1, nullptr);
-                        if (v_sent > s) mbar_wait(v_full(s), ((v_sent - 1 - s) / kRing) & 1, nullptr);
-                    }
                 }
             }
             __syncwarp();
@@ -323,6 +314,16 @@ attention_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     }
     tcgen05_fence_before();
     __syncthreads();
+    if (gave_up && warp == kLoad) {                    // what is in flight lands before the CTA ends
+        if (elect_one()) {
+            for (uint32_t t = 0; t < q_sent; ++t) mbar_wait(q_full(t), 0, nullptr);
+            for (uint32_t s = 0; s < kRing; ++s) {
+                if (k_sent > s) mbar_wait(k_full(s), ((k_sent - 1 - s) / kRing) & 1, nullptr);
+                if (v_sent > s) mbar_wait(v_full(s), ((v_sent - 1 - s) / kRing) & 1, nullptr);
+            }
+        }
+        __syncwarp();
+    }
     if (warp == kMma) {
         if (gave_up) {                                 // matrix instructions in flight end before their memory is freed
             if (elect_one()) {
@@ -444,12 +445,7 @@ uint64_t parts_bytes(const AttentionParams& p) { return round_up(part_rows(p) * 
 
 }  // namespace
 
-int attention_gave_up(uint32_t* word) {
-    const uint32_t zero = 0;
-    int rc = cuda_status(cudaMemcpyFromSymbol(word, g_gave_up, sizeof *word));
-    if (!rc && *word) rc = cuda_status(cudaMemcpyToSymbol(g_gave_up, &zero, sizeof zero));
-    return rc;
-}
+int attention_waits(uint32_t* gave_up, const uint64_t* limit_ns) { return waits_of_file(gave_up, limit_ns); }
 
 }  // namespace mmee
 

@@ -19,8 +19,6 @@ namespace mmee {
 
 namespace {
 
-__device__ uint32_t g_gave_up;
-
 struct GradParams {
     AttentionParams a;                 // (lse: in)
     const void* d_o;
@@ -191,6 +189,7 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     // The rows' kernel is done from here on.  The kernel of dQ, which needs it too, may start where this one leaves room.
     wait_for_stream();
     release_stream();
+    uint32_t q_sent = 0, o_sent = 0;                   // loads on their way or landed
 
     if (warp == 8) {
         const int32_t bb = (int32_t)b, hk = (int32_t)head;
@@ -199,8 +198,6 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
             for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(k_tile + j * kTile * kRowBytes, &mk, kv_full, 64 * j, (int32_t)k0, hk, bb);
             for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(v_tile + j * kTile * kRowBytes, &mv, kv_full, 64 * j, (int32_t)k0, hk, bb);
         }
-        uint32_t q_sent = 0, o_sent = 0;
-        bool sound = true;
         for (uint32_t i = 0; i < n; ++i) {
             const uint32_t s = i % kRingV, h = head * a.group + i / tiles_q, row = i % tiles_q * kTile;
             const uint64_t at = ((uint64_t)b * a.q_heads + h) * a.seq_q + row + 4 * lane;
@@ -211,13 +208,13 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                 logs[j] = kPShift<BF16> - row_log(p, at + j, in);
                 deltas[j] = in ? -p.delta[at + j] : 0.f;
             }
-            if (!(sound = mbar_wait(q_empty(i), q_turn(i) ^ 1, lost))) break;
+            if (!mbar_wait(q_empty(i), q_turn(i) ^ 1, lost)) break;
             if (lane == 0) {
                 mbar_expect(q_full(i), Shape::kQ);
                 for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(q_tile(i) + j * kTile * kRowBytes, &mq, q_full(i), 64 * j, (int32_t)row, (int32_t)h, bb);
             }
             ++q_sent;
-            if (!(sound = mbar_wait(o_empty(i), o_turn(i) ^ 1, lost))) break;
+            if (!mbar_wait(o_empty(i), o_turn(i) ^ 1, lost)) break;
             *reinterpret_cast<float4*>(&row_stats[s][0][4 * lane]) = make_float4(logs[0], logs[1], logs[2], logs[3]);
             *reinterpret_cast<float4*>(&row_stats[s][1][4 * lane]) = make_float4(deltas[0], deltas[1], deltas[2], deltas[3]);
             __syncwarp();
@@ -226,13 +223,6 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
                 for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(o_tile(i) + j * kTile * kRowBytes, &mo, o_full(i), 64 * j, (int32_t)row, (int32_t)h, bb);
             }
             ++o_sent;
-        }
-        if (!sound) {                                  // what is in flight lands before the CTA ends
-            mbar_wait(kv_full, 0, nullptr);
-            for (uint32_t s = 1; s <= kRingQ; ++s)
-                if (q_sent >= s) mbar_wait(q_full(q_sent - s), q_turn(q_sent - s), nullptr);
-            for (uint32_t s = 1; s <= kRingV; ++s)
-                if (o_sent >= s) mbar_wait(o_full(o_sent - s), o_turn(o_sent - s), nullptr);
         }
         __syncwarp();
     } else if (warp == 9) {
@@ -388,6 +378,13 @@ grad_keys_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__
     }
     tcgen05_fence_before();
     __syncthreads();
+    if (gave_up && warp == 8 && n) {                   // what is in flight lands before the CTA ends
+        mbar_wait(kv_full, 0, nullptr);
+        for (uint32_t s = 1; s <= kRingQ; ++s)
+            if (q_sent >= s) mbar_wait(q_full(q_sent - s), q_turn(q_sent - s), nullptr);
+        for (uint32_t s = 1; s <= kRingV; ++s)
+            if (o_sent >= s) mbar_wait(o_full(o_sent - s), o_turn(o_sent - s), nullptr);
+    }
     if (warp == 9) {
         if (gave_up) {                                 // matrix instructions in flight end before their memory is freed
             if (elect_one()) {
@@ -454,6 +451,7 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     // Without a wait: the kernel of dK and dV, beside which this one starts, has released the stream after the rows' kernel was done, and
     // writes nothing that is read here.
     release_stream();
+    uint32_t k_sent = 0, v_sent = 0;                   // loads on their way or landed (of the thread that issues them)
 
     if (warp == 8) {
         if (elect_one() && n) {
@@ -461,24 +459,15 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             mbar_expect(q_full, Shape::kQ + Shape::kV);
             for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(q_tile + j * kTile * kRowBytes, &mq, q_full, 64 * j, (int32_t)q0, h, bb);
             for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(o_tile + j * kTile * kRowBytes, &mo, q_full, 64 * j, (int32_t)q0, h, bb);
-            uint32_t k_sent = 0, v_sent = 0;
-            bool sound = true;
             for (uint32_t i = 0; i < n; ++i) {
-                if (!(sound = mbar_wait(k_empty(i), k_turn(i) ^ 1, lost))) break;
+                if (!mbar_wait(k_empty(i), k_turn(i) ^ 1, lost)) break;
                 mbar_expect(k_full(i), Shape::kQ);
                 for (int32_t j = 0; j < DK / 64; ++j) tma_load_4d(k_tile(i) + j * kTile * kRowBytes, &mk, k_full(i), 64 * j, (int32_t)(i * kTile), hk, bb);
                 ++k_sent;
-                if (!(sound = mbar_wait(v_empty(i), v_turn(i) ^ 1, lost))) break;
+                if (!mbar_wait(v_empty(i), v_turn(i) ^ 1, lost)) break;
                 mbar_expect(v_full(i), Shape::kV);
                 for (int32_t j = 0; j < DV / 64; ++j) tma_load_4d(v_tile(i) + j * kTile * kRowBytes, &mv, v_full(i), 64 * j, (int32_t)(i * kTile), hk, bb);
                 ++v_sent;
-            }
-            if (!sound) {                              // what is in flight lands before the CTA ends
-                mbar_wait(q_full, 0, nullptr);
-                for (uint32_t s = 1; s <= kRingK; ++s)
-                    if (k_sent >= s) mbar_wait(k_full(k_sent - s), k_turn(k_sent - s), nullptr);
-                for (uint32_t s = 1; s <= kRingV; ++s)
-                    if (v_sent >= s) mbar_wait(v_full(v_sent - s), v_turn(v_sent - s), nullptr);
             }
         }
         __syncwarp();
@@ -605,6 +594,16 @@ grad_queries_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     wait_for_stream();
     tcgen05_fence_before();
     __syncthreads();
+    if (gave_up && warp == 8 && n) {                   // what is in flight lands before the CTA ends
+        if (elect_one()) {
+            mbar_wait(q_full, 0, nullptr);
+            for (uint32_t s = 1; s <= kRingK; ++s)
+                if (k_sent >= s) mbar_wait(k_full(k_sent - s), k_turn(k_sent - s), nullptr);
+            for (uint32_t s = 1; s <= kRingV; ++s)
+                if (v_sent >= s) mbar_wait(v_full(v_sent - s), v_turn(v_sent - s), nullptr);
+        }
+        __syncwarp();
+    }
     if (warp == 9) {
         if (gave_up) {                                 // matrix instructions in flight end before their memory is freed
             if (elect_one()) {
@@ -652,12 +651,7 @@ uint64_t space_bytes(const mmee_workload_t& w) { return rows_bytes(w) + round_up
 
 }  // namespace
 
-int attention_grad_gave_up(uint32_t* word) {
-    const uint32_t zero = 0;
-    int rc = cuda_status(cudaMemcpyFromSymbol(word, g_gave_up, sizeof *word));
-    if (!rc && *word) rc = cuda_status(cudaMemcpyToSymbol(g_gave_up, &zero, sizeof zero));
-    return rc;
-}
+int attention_grad_waits(uint32_t* gave_up, const uint64_t* limit_ns) { return waits_of_file(gave_up, limit_ns); }
 
 }  // namespace mmee
 

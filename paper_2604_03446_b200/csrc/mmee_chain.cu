@@ -1,6 +1,8 @@
 // Host side shared by the calls that run a chain: tensor maps, device limits, the status of past launches.
 #include "mmee_chain.h"
 
+#include <initializer_list>
+
 namespace mmee {
 
 namespace {
@@ -58,16 +60,22 @@ int sm_count(uint32_t* out) {
 
 }  // namespace mmee
 
-extern "C" int mmee_chain_status(void) {
-    int (*const words[])(uint32_t*) = {mmee::attention_gave_up, mmee::attention_grad_gave_up, mmee::ffn_gave_up, mmee::ffn_narrow_gave_up};
-    uint32_t any = 0;
+static int all_waits(uint32_t* any, const uint64_t* limit_ns) {
     const int done = mmee::cuda_status(cudaDeviceSynchronize());     // (streams that do not wait for the default one, too)
     if (done) return done;
-    for (const auto word : words) {
+    for (const auto waits : {mmee::attention_waits, mmee::attention_grad_waits, mmee::ffn_waits, mmee::ffn_narrow_waits}) {
         uint32_t w = 0;
-        const int rc = word(&w);
+        const int rc = waits(any ? &w : nullptr, limit_ns);
         if (rc) return rc;
-        any |= w;
+        if (any) *any |= w;
     }
-    return any ? MMEE_ERR_TIMEOUT : MMEE_OK;
+    return MMEE_OK;
 }
+
+extern "C" int mmee_chain_status(void) {
+    uint32_t any = 0;
+    const int rc = all_waits(&any, nullptr);
+    return rc ? rc : any ? MMEE_ERR_TIMEOUT : MMEE_OK;
+}
+
+extern "C" int mmee_chain_wait_limit(uint64_t nanoseconds) { return all_waits(nullptr, &nanoseconds); }

@@ -75,10 +75,11 @@ inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 constexpr uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 constexpr uint64_t round_up(uint64_t a, uint64_t b) { return ceil_div(a, b) * b; }
 
-// The words that kernels set when a wait ran out, read and cleared (one for each file with such kernels).
-int attention_gave_up(uint32_t* word);
-int attention_grad_gave_up(uint32_t* word);
-int ffn_gave_up(uint32_t* word);
-int ffn_narrow_gave_up(uint32_t* word);
+// For each file with kernels that wait: reads and clears the word that they set when a wait ran out, sets the limit of their waits
+// (either may be null).
+int attention_waits(uint32_t* gave_up, const uint64_t* limit_ns);
+int attention_grad_waits(uint32_t* gave_up, const uint64_t* limit_ns);
+int ffn_waits(uint32_t* gave_up, const uint64_t* limit_ns);
+int ffn_narrow_waits(uint32_t* gave_up, const uint64_t* limit_ns);
 
 }  // namespace mmee

@@ -17,8 +17,6 @@ namespace mmee {
 
 namespace {
 
-__device__ uint32_t g_gave_up;
-
 enum Epilogue { kPlain, kGate, kGrad };
 
 // One product of a launch.
@@ -100,7 +98,7 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
     constexpr uint32_t kRowsX = EPI == kGate && !PAIR ? TN / 2 : Shape::kRowsB;    // rows of B from one matrix in a CTA
     extern __shared__ uint8_t raw[];
     __shared__ __align__(8) uint64_t bars[2 * kStages + 5 + 8];
-    __shared__ uint32_t tmem_base, gave_up;
+    __shared__ uint32_t tmem_base, gave_up, others_sent;       // others_sent: loads of the pair's other CTA, told to the leader
     const uint32_t tiles = (smem_addr(raw) + 1023u) & ~1023u;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     const uint32_t rank = PAIR ? cluster_rank() : 0, workers = PAIR ? gridDim.x / 2 : gridDim.x, worker = PAIR ? blockIdx.x / 2 : blockIdx.x;
@@ -163,9 +161,10 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
             mma_commit(bar);
     };
 
+    uint32_t sent = 0;                                 // steps whose loads are on their way or landed (of the thread that issues them)
     if (warp == 4) {                                   // operands
         if (elect_one()) {
-            uint32_t it = 0;
+            uint32_t& it = sent;
             bool sound = true;
             for (uint32_t i = worker; i < n_tiles && sound; i += workers) {
                 uint32_t at, tm, tn, split;
@@ -209,9 +208,7 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
                     }
                 }
             }
-            if (!sound && rank == 0)                   // what is in flight lands before the CTA ends
-                for (uint32_t s = 0; s < kStages; ++s)
-                    if (it > s) mbar_wait(full(s), ((it - 1 - s) / kStages) & 1, nullptr);
+            if (PAIR && rank) store_cluster(pair_leader(smem_addr(&others_sent)), sent);
         }
         __syncwarp();
     } else if (warp == 5) {                            // matrix instructions, of a pair the leader's
@@ -250,7 +247,8 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
             }
         }
     } else {                                           // results
-        uint32_t n = 0, stores = 0, kept = 0;          // tiles, groups of stores, pieces of gate and up asked for
+        uint32_t n = 0, stores = 0, kept = 0, asked = 0;       // tiles, groups of stores, pieces of gate and up: used, asked for
+        bool sound = true;
         const uint32_t mine = tiles + kStages * kStage + warp * Shape::kParts * kPart;
         if constexpr (kBounds) {
             wait_for_stream();
@@ -269,7 +267,7 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
             fence_async_shared();
             __syncwarp();
         };
-        for (uint32_t i = worker; i < n_tiles; i += workers, ++n) {
+        for (uint32_t i = worker; i < n_tiles && sound; i += workers, ++n) {
             const uint32_t b = n & 1;
             uint32_t at, tm, tn, split;
             const uint32_t k = product_of(i, &at);
@@ -277,27 +275,25 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
             tile_of<Shape::kM>(p, at, &tm, &tn, &split);
             const uint32_t row0 = tm * Shape::kM + rank * 128 + warp * 32, col0 = tn * kCols;
             const uint32_t cols = row0 < p.m ? min(kCols, p.n - col0) : 0;     // of this warp's rows, inside
-            auto ask_kept = [&](uint32_t c, uint32_t piece) {          // gate and up of 32 columns
-                if (lane == 0 && c < cols) {
-                    const uint32_t q = piece & 1, bar = kept_full(warp, q);
+            auto ask_kept = [&](uint32_t c) {          // gate and up of 32 columns
+                if (c >= cols) return;
+                if (lane == 0) {
+                    const uint32_t q = asked & 1, bar = kept_full(warp, q);
                     mbar_expect(bar, 2 * kPart);
                     tma_load_2d(part(2 + 2 * q), &ps.gate, bar, (int32_t)(col0 + c), (int32_t)row0);
                     tma_load_2d(part(3 + 2 * q), &ps.up, bar, (int32_t)(col0 + c), (int32_t)row0);
                 }
+                ++asked;
             };
             if (EPI == kGrad) {
-                ask_kept(0, kept);
-                ask_kept(32, kept + 1);
+                ask_kept(0);
+                ask_kept(32);
             }
-            if (!mbar_wait(acc_full(b), (n >> 1) & 1, lost)) {
-                if (EPI == kGrad && lane == 0)         // what is in flight lands before the CTA ends
-                    for (uint32_t c = 0; c < min(64u, cols); c += 32) mbar_wait(kept_full(warp, (kept + c / 32) & 1), ((kept + c / 32) >> 1) & 1, nullptr);
-                break;
-            }
+            if (!mbar_wait(acc_full(b), (n >> 1) & 1, lost)) break;
             tcgen05_fence_after();
             const uint32_t acc = tmem + b * TN + ((warp * 32) << 16);
 #pragma unroll 1
-            for (uint32_t c = 0; c < kCols; c += 64) {
+            for (uint32_t c = 0; c < kCols && sound; c += 64) {
                 uint32_t o[32], o2[32];
 #pragma unroll
                 for (uint32_t half = 0; half < 2; ++half) {
@@ -353,9 +349,9 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
                                 o[16 * half + j] = pack2<BF16>(act_value<kAct>(__uint_as_float(x[2 * j])) * __uint_as_float(y[2 * j]),
                                                                act_value<kAct>(__uint_as_float(x[2 * j + 1])) * __uint_as_float(y[2 * j + 1]));
                         });
-                    } else if (d < cols) {
+                    } else if (d < cols && sound) {
                         const uint32_t q = kept & 1;
-                        mbar_wait(kept_full(warp, q), (kept >> 1) & 1, lost);
+                        if (!(sound = mbar_wait(kept_full(warp, q), (kept >> 1) & 1, lost))) continue;
                         with_act(p.act, [&](auto kind) {
 #pragma unroll
                             for (uint32_t j = 0; j < 8; ++j) {
@@ -377,11 +373,11 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
                             }
                         });
                         __syncwarp();                  // all have read these places: the next but one goes there
-                        ask_kept(d + 64, kept);
+                        ask_kept(d + 64);
                         ++kept;
                     }
                 }
-                if (c >= cols || (EPI == kPlain && p.splits > 1)) continue;        // (the same for the whole warp)
+                if (c >= cols || !sound || (EPI == kPlain && p.splits > 1)) continue;      // (the same for the whole warp)
                 const uint32_t to = EPI == kGrad ? part(0) : part(stores & 1);
                 if (lane == 0) {
                     if (EPI == kGrad || (EPI == kGate && p.gate))
@@ -402,33 +398,53 @@ __global__ void __launch_bounds__(192, 1) product_kernel(const __grid_constant__
             }
             tcgen05_fence_before();
             __syncwarp();
-            if (lane == 0) {
+            if (lane == 0 && sound) {
                 if constexpr (PAIR)
                     mbar_arrive_cluster(pair_leader(acc_empty(b)));
                 else
                     mbar_arrive(acc_empty(b));
             }
         }
-        if (lane == 0) tma_store_read<0>();            // shared memory stays until it has been read
+        // Shared memory stays until it has been read; after a wait that ran out, until what was asked for is there.
+        if (lane == 0) tma_store_read<0>();
+        for (; EPI == kGrad && kept < asked; ++kept) mbar_wait(kept_full(warp, kept & 1), (kept >> 1) & 1, nullptr);
     }
     __syncwarp();
     tcgen05_fence_before();
     // (of a pair: neither's shared or tensor memory goes away while the other uses it)
-    if constexpr (PAIR)
+    if constexpr (PAIR) {
+        if (gave_up && lane == 0) store_cluster(cluster_addr(smem_addr(&gave_up), rank ^ 1), 1);       // both know before either ends
+        __syncwarp();
         cluster_barrier();
-    else
+    } else {
         __syncthreads();
-    if (warp == 5) {
-        if (gave_up) {                                 // matrix instructions in flight end before their memory is freed
+    }
+    if (gave_up) {                                     // what is in flight lands, matrix instructions end
+        if (warp == 4 && rank == 0) {
+            if (elect_one()) {
+                // Steps that only one CTA of a pair has issued: the barrier is told of the bytes that come, or that do not.
+                const uint32_t others = PAIR ? others_sent : sent, all = max(sent, others);
+                for (uint32_t i = min(sent, others); i < all; ++i) {
+                    if (sent > others)
+                        mbar_count_landed(full(i % kStages), kStage);
+                    else
+                        mbar_expect(full(i % kStages), kStage);
+                }
+                for (uint32_t s = 0; s < kStages; ++s)
+                    if (all > s) mbar_wait(full(s), ((all - 1 - s) / kStages) & 1, nullptr);
+            }
+            __syncwarp();
+        } else if (warp == 5) {
             if (elect_one()) {
                 g_gave_up = 1;
-                if (rank == 0) {
-                    commit(drained);
-                    mbar_wait(drained, 0, nullptr);
-                }
+                if (rank == 0) commit(drained);
+                mbar_wait(drained, 0, nullptr);
             }
             __syncwarp();
         }
+        if constexpr (PAIR) cluster_barrier();
+    }
+    if (warp == 5) {
         tcgen05_fence_after();
         if constexpr (PAIR)
             tmem_free_pair(tmem, 2 * TN);
@@ -762,12 +778,7 @@ int check_space(const void* space, uint64_t bytes, Plan* plan, uint64_t fixed) {
 
 }  // namespace
 
-int ffn_gave_up(uint32_t* word) {
-    const uint32_t zero = 0;
-    int rc = cuda_status(cudaMemcpyFromSymbol(word, g_gave_up, sizeof *word));
-    if (!rc && *word) rc = cuda_status(cudaMemcpyToSymbol(g_gave_up, &zero, sizeof zero));
-    return rc;
-}
+int ffn_waits(uint32_t* gave_up, const uint64_t* limit_ns) { return waits_of_file(gave_up, limit_ns); }
 
 }  // namespace mmee
 

@@ -15,8 +15,6 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-__device__ uint32_t g_gave_up;
-
 constexpr uint32_t kRowsW = 128, kTileW = kRowsW * kRowBytes;
 constexpr uint32_t kNarrowSmem = 112 * 1024;           // a CTA's share of a multiprocessor
 constexpr uint32_t kSlice = 32;                        // columns that are joined at a time
@@ -71,6 +69,7 @@ __global__ void __launch_bounds__(192) ffn_narrow_kernel(const __grid_constant__
         release_stream();
     }
 
+    uint32_t sent = 0;                                 // steps whose loads are on their way or landed (of the thread that issues them)
     if (warp == 4) {
         if (elect_one()) {
             auto load_w = [&](uint32_t i) {
@@ -91,17 +90,13 @@ __global__ void __launch_bounds__(192) ffn_narrow_kernel(const __grid_constant__
                 release_stream();
             }
             for (uint32_t i = 0; i < ahead; ++i) load_x(i);
-            uint32_t sent = ahead;
-            bool sound = true;
+            sent = ahead;
             for (uint32_t i = ahead; i < n; ++i) {
-                if (!(sound = mbar_wait(empty(i % z.stages), ((i / z.stages) & 1) ^ 1, lost))) break;
+                if (!mbar_wait(empty(i % z.stages), ((i / z.stages) & 1) ^ 1, lost)) break;
                 load_w(i);
                 load_x(i);
                 ++sent;
             }
-            if (!sound)                                // what is in flight lands before the CTA ends
-                for (uint32_t s = 0; s < z.stages; ++s)
-                    if (sent > s) mbar_wait(full(s), ((sent - 1 - s) / z.stages) & 1, nullptr);
         }
         __syncwarp();
     } else if (warp == 5) {
@@ -183,6 +178,12 @@ __global__ void __launch_bounds__(192) ffn_narrow_kernel(const __grid_constant__
     }
     tcgen05_fence_before();
     __syncthreads();
+    if (gave_up && warp == 4) {                        // what is in flight lands before the CTA ends
+        if (elect_one())
+            for (uint32_t s = 0; s < z.stages; ++s)
+                if (sent > s) mbar_wait(full(s), ((sent - 1 - s) / z.stages) & 1, nullptr);
+        __syncwarp();
+    }
     if (warp == 5) {
         if (gave_up) {                                 // matrix instructions in flight end before their memory is freed
             if (elect_one()) {
@@ -232,11 +233,6 @@ int ffn_narrow(const FfnTokens& p, bool bf16, cudaStream_t stream) {
     return rc ? rc : bf16 ? launch_narrow<false, true>(p, stream) : launch_narrow<false, false>(p, stream);
 }
 
-int ffn_narrow_gave_up(uint32_t* word) {
-    const uint32_t zero = 0;
-    int rc = cuda_status(cudaMemcpyFromSymbol(word, g_gave_up, sizeof *word));
-    if (!rc && *word) rc = cuda_status(cudaMemcpyToSymbol(g_gave_up, &zero, sizeof zero));
-    return rc;
-}
+int ffn_narrow_waits(uint32_t* gave_up, const uint64_t* limit_ns) { return waits_of_file(gave_up, limit_ns); }
 
 }  // namespace mmee

@@ -11,6 +11,8 @@
 
 namespace mmee {
 
+int cuda_status(cudaError_t e);        // mmee_api.cu
+
 constexpr uint32_t kRowBytes = 128;            // one row of a swizzled tile: 64 values of 16 bits
 constexpr uint32_t kGroupBytes = 8 * kRowBytes;    // eight rows: the unit of the swizzle pattern
 
@@ -54,16 +56,32 @@ __device__ __forceinline__ uint64_t global_ns() {
 }
 
 constexpr uint64_t kWaitNs = 4000000000ull;    // no wait of a sound launch comes near this
+// One of each for every file with waits: what holds as the limit, and a word that a kernel sets when a wait ran out.
+static __device__ uint64_t g_wait_ns = kWaitNs;
+static __device__ uint32_t g_gave_up;
+
+// Host side of the two: reads and clears the word, sets the limit (either may be null).
+inline int waits_of_file(uint32_t* gave_up, const uint64_t* limit_ns) {
+    const uint32_t zero = 0;
+    cudaError_t e = cudaSuccess;
+    if (gave_up) e = cudaMemcpyFromSymbol(gave_up, g_gave_up, sizeof *gave_up);
+    if (e == cudaSuccess && gave_up && *gave_up) e = cudaMemcpyToSymbol(g_gave_up, &zero, sizeof zero);
+    if (e == cudaSuccess && limit_ns) e = cudaMemcpyToSymbol(g_wait_ns, limit_ns, sizeof *limit_ns);
+    return cuda_status(e);
+}
 
 // Waits until the barrier's phase of this parity is over.  False: the wait ran out, here or in another role of the CTA
-// (`gave_up`, one word of shared memory); the role then leaves its loop.  With gave_up = nullptr: a wait of its own.
+// (`gave_up`, one word of shared memory); the role then leaves its loop.  With gave_up = nullptr: for what is in flight when a
+// kernel gives up, with a limit of its own.
+// (Lanes of a warp wait in step: each try, and each look at the clock and the word, is one instruction for them all, so that they
+// leave together.  A vote after every wait would cost attention 3 to 4 %.)
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up) {
     uint64_t end = 0;
     for (uint32_t tries = 1; !mbar_try(bar, parity); ++tries) {
         if (tries % 256) continue;                     // (a look at the clock would delay what waits)
         const uint64_t now = global_ns();
-        if (!end) end = now + kWaitNs;
-        if ((gave_up && *gave_up) || now > end) {
+        if (!end) end = now + (gave_up ? g_wait_ns : kWaitNs);
+        if ((gave_up && *gave_up) || now >= end) {
             if (gave_up) *gave_up = 1;
             return false;
         }
@@ -132,11 +150,21 @@ __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// The same place in the shared memory of the cluster's first CTA.
-__device__ __forceinline__ uint32_t pair_leader(uint32_t addr) {
+// The same place in the shared memory of the cluster's CTA `rank`.
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
     uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
+}
+__device__ __forceinline__ uint32_t pair_leader(uint32_t addr) { return cluster_addr(addr, 0); }
+
+__device__ __forceinline__ void store_cluster(uint32_t at, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
+}
+
+// Counts bytes at a barrier as landed that will not come.
+__device__ __forceinline__ void mbar_count_landed(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.complete_tx.relaxed.cluster.shared::cluster.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
