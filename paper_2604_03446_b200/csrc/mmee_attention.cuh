@@ -37,9 +37,11 @@ struct AttentionParams {
     float *part_o, *part_lse;          // [split][tiles - whole][tile_rows] rows of d_v; log2 of the sums
 };
 
+// (Not through the read-only path, see read_once.)
 __device__ __forceinline__ uint32_t valid_keys(const int32_t* kv_len, uint32_t b, uint32_t seq_kv) {
     if (!kv_len) return seq_kv;
-    const int32_t n = __ldg(kv_len + b);
+    int32_t n;
+    asm volatile("ld.global.b32 %0, [%1];" : "=r"(n) : "l"(kv_len + b) : "memory");
     return n < 0 ? 0u : min((uint32_t)n, seq_kv);
 }
 

@@ -25,12 +25,6 @@ struct TokenParams {
     uint32_t cluster;                  // CTAs that join their parts themselves; a.splits counts clusters
 };
 
-__device__ __forceinline__ uint4 read16(const uint16_t* p) {
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
-}
-
 template <bool BF16>
 __device__ __forceinline__ void mma16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     if (BF16)
@@ -74,7 +68,7 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 3 : 2) attention_token_
         const uint32_t r = 8 * t + g, h = r / a.seq_q, token = r % a.seq_q;
         const uint16_t* const row = p.q + (int64_t)b * p.qs.batch + (int64_t)token * p.qs.token + (int64_t)(head * a.group + h) * p.qs.head;
 #pragma unroll
-        for (int j = 0; j < DK / 32; ++j) q[t][j] = r < rows && 32 * j + 8 * c < a.d_qk ? read16(row + 32 * j + 8 * c) : none;
+        for (int j = 0; j < DK / 32; ++j) q[t][j] = r < rows && 32 * j + 8 * c < a.d_qk ? read_once(row + 32 * j + 8 * c) : none;
     }
     float acc[NT][DV / 64][4][4];
     float m[NT][2], l[NT][2];
@@ -95,7 +89,7 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 3 : 2) attention_token_
             const uint32_t at = key + g + 8 * i;
             const uint16_t* const row = kp + (int64_t)at * p.ks.token + 8 * c;
 #pragma unroll
-            for (int j = 0; j < DK / 32; ++j) kf[i][j] = at < end && 32 * j + 8 * c < a.d_qk ? read16(row + 32 * j) : none;
+            for (int j = 0; j < DK / 32; ++j) kf[i][j] = at < end && 32 * j + 8 * c < a.d_qk ? read_once(row + 32 * j) : none;
         }
     };
     auto load_values = [&](uint32_t key) {
@@ -104,7 +98,7 @@ __global__ void __launch_bounds__(kWarps * 32, NT == 1 ? 3 : 2) attention_token_
             const uint32_t at = key + 2 * c + (i & 1) + 8 * (i >> 1);
             const uint16_t* const row = vp + (int64_t)at * p.vs.token + 8 * g;
 #pragma unroll
-            for (int j = 0; j < DV / 64; ++j) vf[j][i] = at < end && 64 * j + 8 * g < a.d_v ? read16(row + 64 * j) : none;
+            for (int j = 0; j < DV / 64; ++j) vf[j][i] = at < end && 64 * j + 8 * g < a.d_v ? read_once(row + 64 * j) : none;
         }
     };
     load_keys(begin + warp * kStep);

@@ -14,14 +14,7 @@ namespace {
 
 constexpr uint32_t kMostWarps = 8;
 
-__device__ __forceinline__ uint4 read_once(const uint16_t* p) {
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
-}
-
-// Tokens' values: they come back to L1 for the next rows.  (Not through the read-only path: an earlier kernel of the stream may
-// still be writing them when this one starts.)
+// Tokens' values: they come back to L1 for the next rows.
 __device__ __forceinline__ uint4 read_token(const uint16_t* p) {
     uint4 v;
     asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");

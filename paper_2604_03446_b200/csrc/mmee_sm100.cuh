@@ -98,6 +98,14 @@ __device__ __forceinline__ void wait_for_stream() { asm volatile("griddepcontrol
 // before it.
 __device__ __forceinline__ void release_stream() { asm volatile("griddepcontrol.launch_dependents;"); }
 
+// Sixteen bytes that are read once.  Not through the read-only path, which is for what nothing writes as long as a kernel runs: an
+// earlier kernel of the stream may still be writing them when one that was launched early starts.
+__device__ __forceinline__ uint4 read_once(const uint16_t* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
 // --- TMA ------------------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ void tma_prefetch(const CUtensorMap* map) {
