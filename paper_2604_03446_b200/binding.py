@@ -381,26 +381,39 @@ def _refuse(where: str, why: str):
     raise MmeeError(ERR_ARG, "%s: %s" % (where, why))
 
 
-_torch = None
+_torch = _forward_mode = None
 _type_codes = {}
+
+
+def _no_graph(where, tensors):
+    """Refuses tensors that autograd, or a forward-mode level, would carry on from: the call's results would silently drop out."""
+    recorded = _torch.is_grad_enabled() and any(t.requires_grad for t in tensors)
+    if recorded or (_forward_mode._current_level >= 0 and any(_forward_mode.unpack_dual(t).tangent is not None for t in tensors)):
+        _refuse(where, "tensors that want a gradient: automatic differentiation does not see this call (under torch.no_grad(), or on "
+                       "detached tensors, call it and its _backward yourself)")
 
 
 def _chain_code(where: str, rank: int, *tensors):
     """The type code that the tensors of one call share: CUDA tensors of one 16-bit type on one device, of `rank` dimensions with
-    the last one contiguous."""
-    global _torch
+    the last one contiguous, none of which takes part in an automatic differentiation."""
+    global _torch, _forward_mode
     if _torch is None:
         import torch
+        import torch.autograd.forward_ad
+        _forward_mode = torch.autograd.forward_ad
         _torch = torch
         _type_codes.update({torch.bfloat16: BF16, torch.float16: F16})
     try:
         dtype, at = tensors[0].dtype, tensors[0].get_device()
-        code = _type_codes[dtype]
+        code, graph = _type_codes[dtype], False
         for t in tensors:
             steps = t.stride()
+            graph = graph or t.requires_grad
             if t.dtype is not dtype or t.get_device() != at or len(steps) != rank or (steps[-1] != 1 and t.shape[-1] > 1):
                 break
         else:
+            if graph or _forward_mode._current_level >= 0:
+                _no_graph(where, tensors)
             if at >= 0:
                 return code
     except (AttributeError, KeyError, TypeError):
@@ -480,7 +493,7 @@ def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
     """softmax(scale q k^T) v over each sequence's first kv_len keys: (o, saved).  q: (batch, tokens, q_heads, d_qk), k: (batch, keys,
     kv_heads, d_qk), v: (batch, keys, kv_heads, d_v), bfloat16 or float16; kv_len: int32 tensor with an entry per sequence, None: all keys;
     scale: d_qk ** -0.5 unless given.  saved: what mmee_attention_backward needs; attention_lse(saved, o) is the part of it that is
-    of use elsewhere.  Asynchronous."""
+    of use elsewhere.  Not recorded by autograd: tensors that require a gradient are refused unless under torch.no_grad().  Asynchronous."""
     where = "mmee_attention"
     code = _chain_code(where, 4, q, k, v)
     if stream is not None or _current_device() != q.get_device():
@@ -552,7 +565,8 @@ def _ffn_sizes(where, x, w_gate, w_up, w_down):
 
 def mmee_gated_ffn(x, w_gate, w_up, w_down, activation: int = ACT_SILU, save: bool = False, stream=None):
     """y = (act(x w_gate^T) * (x w_up^T)) w_down^T: (y, saved).  x: (tokens, in), w_gate and w_up: (inner, in), w_down: (out, inner),
-    bfloat16 or float16.  saved: what mmee_gated_ffn_backward needs where `save`, otherwise None.  Asynchronous."""
+    bfloat16 or float16.  saved: what mmee_gated_ffn_backward needs where `save`, otherwise None.  Not recorded by autograd, as
+    mmee_attention.  Asynchronous."""
     where = "mmee_gated_ffn"
     code = _chain_code(where, 2, x, w_gate, w_up, w_down)
     if stream is not None or _current_device() != x.get_device():

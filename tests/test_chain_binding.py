@@ -1,0 +1,75 @@
+"""What the Python entry points of the chains do before anything is launched (no GPU: tensors and the library are stand-ins)."""
+import threading
+import types
+
+import pytest
+import torch
+
+import paper_2604_03446_b200.binding as b
+
+
+class Fake:
+    """A tensor as the entry points look at it: a CUDA one by what it says."""
+
+    def __init__(self, *shape, dtype=torch.bfloat16, device=0, requires_grad=False):
+        self.shape, self.dtype, self.device, self.requires_grad = torch.Size(shape), dtype, torch.device("cuda", device), requires_grad
+
+    def get_device(self):
+        return self.device.index
+
+    def stride(self, i=None):
+        s = torch.empty(self.shape, device="meta").stride()
+        return s if i is None else s[i]
+
+
+def attention(**kw):
+    return Fake(2, 3, 4, 64, **kw), Fake(2, 5, 2, 64, **kw), Fake(2, 5, 2, 64, **kw)
+
+
+def block(**kw):
+    return Fake(4, 32, **kw), Fake(64, 32, **kw), Fake(64, 32, **kw), Fake(16, 64, **kw)
+
+
+def refused(call, *args, **kw):
+    with pytest.raises(b.MmeeError) as e:
+        call(*args, **kw)
+    assert e.value.code == b.ERR_ARG
+    return str(e.value)
+
+
+def calls(which):
+    """Each entry point with sound arguments, its tensors made by `which`."""
+    q, k, v = attention(**which)
+    o, w = Fake(2, 3, 4, 64, **which), block(**which)
+    return [(b.mmee_attention, (q, k, v)), (b.mmee_attention_backward, (o, q, k, v, o, None)), (b.mmee_gated_ffn, w),
+            (b.mmee_gated_ffn_backward, (Fake(4, 16, **which), *w, (Fake(4, 64, **which), None)))]
+
+
+# --- gradients ------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("i", range(4))
+def test_tensors_that_want_a_gradient_are_refused_where_it_would_be_lost(i):
+    call, args = calls(dict(requires_grad=True))[i]
+    assert "gradient" in refused(call, *args)
+
+
+@pytest.mark.parametrize("i", range(4))
+def test_tensors_that_want_a_gradient_pass_where_none_is_recorded(i, monkeypatch):
+    """Under no_grad (and in a Function's own forward and backward) the call goes on: to its next question, here."""
+    class GoesOn(Exception):
+        pass
+
+    def device():
+        raise GoesOn
+    monkeypatch.setattr(b, "_current_device", device)
+    call, args = calls(dict(requires_grad=True))[i]
+    with torch.no_grad(), pytest.raises(GoesOn):
+        call(*args)
+
+
+def test_dual_numbers_are_refused(monkeypatch):
+    import torch.autograd.forward_ad as fwd
+    monkeypatch.setattr(fwd, "unpack_dual", lambda t: types.SimpleNamespace(tangent=t))
+    for call, args in calls({}):
+        with fwd.dual_level():
+            assert "gradient" in refused(call, *args)
