@@ -401,8 +401,8 @@ def _chain_code(where: str, rank: int, *tensors):
         import torch
         import torch.autograd.forward_ad
         _forward_mode = torch.autograd.forward_ad
-        _torch = torch
         _type_codes.update({torch.bfloat16: BF16, torch.float16: F16})
+        _torch = torch                                 # (last: another thread's first call goes by it)
     try:
         dtype, at = tensors[0].dtype, tensors[0].get_device()
         code, graph = _type_codes[dtype], False

@@ -73,3 +73,25 @@ def test_dual_numbers_are_refused(monkeypatch):
     for call, args in calls({}):
         with fwd.dual_level():
             assert "gradient" in refused(call, *args)
+
+
+# --- two threads ----------------------------------------------------------------------------------------------------
+
+def test_a_first_call_of_two_threads_at_once(monkeypatch):
+    """Whoever finds the module's view of torch made finds its table of types filled."""
+    seen = []
+
+    class Table(dict):
+        def update(self, *args):
+            seen.append(b._torch)                      # what a thread that comes in now would go by
+            super().update(*args)
+
+    monkeypatch.setattr(b, "_torch", None)
+    monkeypatch.setattr(b, "_type_codes", Table())
+    codes = []
+    threads = [threading.Thread(target=lambda: codes.append(b._chain_code("x", 4, *attention()))) for _ in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert codes == [b.BF16] * 4 and seen and seen[0] is None and all(v is None or b._type_codes for v in seen)
