@@ -430,10 +430,13 @@ def _current_device():
     return n
 
 
-def _there(t, stream):
+def _there(where, t, stream):
     """Makes the tensor's device and the stream current: launches and the memory that a call takes are theirs."""
-    import torch
-    return torch.cuda.stream(stream) if stream is not None else torch.cuda.device(t.device)
+    if stream is None:
+        return _torch.cuda.device(t.device)
+    if stream.device != t.device:
+        _refuse(where, "a stream of the tensors' device is wanted")
+    return _torch.cuda.stream(stream)
 
 
 # The call structs as bytes, in the layouts of Workload, Attention, AttentionGrad, GatedFfn and GatedFfnGrad: filling a
@@ -497,7 +500,7 @@ def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
     where = "mmee_attention"
     code = _chain_code(where, 4, q, k, v)
     if stream is not None or _current_device() != q.get_device():
-        with _there(q, stream):
+        with _there(where, q, stream):
             return mmee_attention(q, k, v, kv_len, scale)
     batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v = _attention_sizes(where, q, k, v, kv_len)
     calls = _chain()
@@ -529,7 +532,7 @@ def mmee_attention_backward(d_o, q, k, v, o, saved, kv_len=None, scale=None, str
     where = "mmee_attention_backward"
     code = _chain_code(where, 4, q, k, v, o, d_o)
     if stream is not None or _current_device() != q.get_device():
-        with _there(q, stream):
+        with _there(where, q, stream):
             return mmee_attention_backward(d_o, q, k, v, o, saved, kv_len, scale)
     batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v = _attention_sizes(where, q, k, v, kv_len)
     if o.shape != (batch, seq_q, q_heads, d_v) or d_o.shape != o.shape:
@@ -570,7 +573,7 @@ def mmee_gated_ffn(x, w_gate, w_up, w_down, activation: int = ACT_SILU, save: bo
     where = "mmee_gated_ffn"
     code = _chain_code(where, 2, x, w_gate, w_up, w_down)
     if stream is not None or _current_device() != x.get_device():
-        with _there(x, stream):
+        with _there(where, x, stream):
             return mmee_gated_ffn(x, w_gate, w_up, w_down, activation, save)
     tokens, d_ff, d_in, d_out = _ffn_sizes(where, x, w_gate, w_up, w_down)
     calls = _chain()
@@ -594,7 +597,7 @@ def mmee_gated_ffn_backward(d_y, x, w_gate, w_up, w_down, saved, activation: int
         _refuse(where, "saved is what the forward call with save=True returned")
     code = _chain_code(where, 2, x, w_gate, w_up, w_down, d_y, saved[0])
     if stream is not None or _current_device() != x.get_device():
-        with _there(x, stream):
+        with _there(where, x, stream):
             return mmee_gated_ffn_backward(d_y, x, w_gate, w_up, w_down, saved, activation)
     tokens, d_ff, d_in, d_out = _ffn_sizes(where, x, w_gate, w_up, w_down)
     hidden, kept = saved

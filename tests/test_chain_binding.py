@@ -95,3 +95,27 @@ def test_a_first_call_of_two_threads_at_once(monkeypatch):
     for t in threads:
         t.join()
     assert codes == [b.BF16] * 4 and seen and seen[0] is None and all(v is None or b._type_codes for v in seen)
+
+
+# --- streams --------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("i", range(4))
+def test_a_stream_of_another_device_than_the_tensors_is_refused(i, monkeypatch):
+    """(It was dropped: the call ran on the current stream of the tensors' device.)"""
+    entered = []
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: entered.append(s) or pytest.fail("made current"))
+    call, args = calls({})[i]
+    stream = types.SimpleNamespace(device=torch.device("cuda", 1), device_index=1, cuda_stream=4096)
+    assert "stream" in refused(call, *args, stream=stream) and not entered
+
+
+def test_a_stream_of_the_tensors_device_is_made_current(monkeypatch):
+    class Entered(Exception):
+        pass
+
+    def enter(s):
+        raise Entered
+    monkeypatch.setattr(torch.cuda, "stream", enter)
+    for call, args in calls({}):
+        with pytest.raises(Entered):
+            call(*args, stream=types.SimpleNamespace(device=torch.device("cuda", 0), device_index=0, cuda_stream=4096))
