@@ -503,18 +503,21 @@ def mmee_attention(q, k, v, kv_len=None, scale=None, stream=None):
         with _there(where, q, stream):
             return mmee_attention(q, k, v, kv_len, scale)
     batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v = _attention_sizes(where, q, k, v, kv_len)
-    calls = _chain()
-    w = _WORKLOAD(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v, 2)
-    space, need = _space(calls.attention_workspace, q, where, w)
-    o = q.new_empty((batch, seq_q, q_heads, d_v))
-    rows = batch * seq_q * q_heads
-    ahead = (rows + 3) // 4 * 4                        # (what follows the rows' sums starts on sixteen bytes)
-    saved = q.new_empty(ahead + rows * d_v // 2, dtype=_torch.float32)
-    at = saved.data_ptr()
-    a = _ATTENTION(code, (d_qk or 1) ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
-                   *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], seq_q * q_heads * d_v, q_heads * d_v, d_v, at, at + 4 * ahead,
-                   0 if kv_len is None else kv_len.data_ptr(), space.data_ptr() if need else 0, need)
-    code = calls.attention(w, a, _current_stream())
+    try:
+        calls = _chain()
+        w = _WORKLOAD(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v, 2)
+        space, need = _space(calls.attention_workspace, q, where, w)
+        o = q.new_empty((batch, seq_q, q_heads, d_v))
+        rows = batch * seq_q * q_heads
+        ahead = (rows + 3) // 4 * 4                        # (what follows the rows' sums starts on sixteen bytes)
+        saved = q.new_empty(ahead + rows * d_v // 2, dtype=_torch.float32)
+        at = saved.data_ptr()
+        a = _ATTENTION(code, (d_qk or 1) ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+                       *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], seq_q * q_heads * d_v, q_heads * d_v, d_v, at, at + 4 * ahead,
+                       0 if kv_len is None else kv_len.data_ptr(), space.data_ptr() if need else 0, need)
+        code = calls.attention(w, a, _current_stream())
+    except (struct.error, OverflowError) as e:
+        _refuse(where, "an argument is no number that the call holds (%s)" % e)
     if code:
         _check(code, where)
     return o, saved
@@ -543,16 +546,19 @@ def mmee_attention_backward(d_o, q, k, v, o, saved, kv_len=None, scale=None, str
             saved.get_device() == q.get_device() and saved.is_contiguous()):
         _refuse(where, "saved is what the forward call for these tensors returned")
     at = saved.data_ptr()
-    calls = _chain()
-    w = _WORKLOAD(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v, 2)
-    space, need = _space(calls.attention_backward_workspace, q, where, w)
-    d_q, d_k, d_v_ = q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(v.shape)
-    a = _ATTENTION(code, (d_qk or 1) ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
-                   *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], at, at + 4 * ahead,
-                   0 if kv_len is None else kv_len.data_ptr(), 0, 0)
-    g = _ATTENTION_GRAD(d_o.data_ptr(), d_q.data_ptr(), d_k.data_ptr(), d_v_.data_ptr(), *d_o.stride()[:3], *d_q.stride()[:3],
-                        *d_k.stride()[:3], *d_v_.stride()[:3], space.data_ptr(), need)
-    code = calls.attention_backward(w, a, g, _current_stream())
+    try:
+        calls = _chain()
+        w = _WORKLOAD(batch, q_heads, kv_heads, seq_q, seq_kv, d_qk, d_v, 2)
+        space, need = _space(calls.attention_backward_workspace, q, where, w)
+        d_q, d_k, d_v_ = q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(v.shape)
+        a = _ATTENTION(code, (d_qk or 1) ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+                       *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], at, at + 4 * ahead,
+                       0 if kv_len is None else kv_len.data_ptr(), 0, 0)
+        g = _ATTENTION_GRAD(d_o.data_ptr(), d_q.data_ptr(), d_k.data_ptr(), d_v_.data_ptr(), *d_o.stride()[:3], *d_q.stride()[:3],
+                            *d_k.stride()[:3], *d_v_.stride()[:3], space.data_ptr(), need)
+        code = calls.attention_backward(w, a, g, _current_stream())
+    except (struct.error, OverflowError) as e:
+        _refuse(where, "an argument is no number that the call holds (%s)" % e)
     if code:
         _check(code, where)
     return d_q, d_k, d_v_
@@ -576,14 +582,17 @@ def mmee_gated_ffn(x, w_gate, w_up, w_down, activation: int = ACT_SILU, save: bo
         with _there(where, x, stream):
             return mmee_gated_ffn(x, w_gate, w_up, w_down, activation, save)
     tokens, d_ff, d_in, d_out = _ffn_sizes(where, x, w_gate, w_up, w_down)
-    calls = _chain()
-    w = _WORKLOAD(1, 1, 1, tokens, d_ff, d_in, d_out, 2)
-    hidden, y = x.new_empty((tokens, d_ff)), x.new_empty((tokens, d_out))
-    kept = x.new_empty((2, tokens, d_ff), dtype=_torch.float32) if save else None
-    space, need = _space(calls.gated_ffn_workspace, x, where, w, 0)
-    f = _FFN(code, activation, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), x.stride(0), w_gate.stride(0),
-             w_up.stride(0), w_down.stride(0), hidden.data_ptr(), kept.data_ptr() if save else 0, y.data_ptr(), space.data_ptr() if need else 0, need)
-    code = calls.gated_ffn(w, f, _current_stream())
+    try:
+        calls = _chain()
+        w = _WORKLOAD(1, 1, 1, tokens, d_ff, d_in, d_out, 2)
+        hidden, y = x.new_empty((tokens, d_ff)), x.new_empty((tokens, d_out))
+        kept = x.new_empty((2, tokens, d_ff), dtype=_torch.float32) if save else None
+        space, need = _space(calls.gated_ffn_workspace, x, where, w, 0)
+        f = _FFN(code, activation, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), x.stride(0), w_gate.stride(0),
+                 w_up.stride(0), w_down.stride(0), hidden.data_ptr(), kept.data_ptr() if save else 0, y.data_ptr(), space.data_ptr() if need else 0, need)
+        code = calls.gated_ffn(w, f, _current_stream())
+    except (struct.error, OverflowError) as e:
+        _refuse(where, "an argument is no number that the call holds (%s)" % e)
     if code:
         _check(code, where)
     return y, ((hidden, kept) if save else None)
@@ -603,18 +612,21 @@ def mmee_gated_ffn_backward(d_y, x, w_gate, w_up, w_down, saved, activation: int
     hidden, kept = saved
     if d_y.shape != (tokens, d_out):
         _refuse(where, "d_y is (tokens, out)")
-    if (hidden.shape != (tokens, d_ff) or not hidden.is_contiguous() or kept.shape != (2, tokens, d_ff) or
+    if (hidden.shape != (tokens, d_ff) or not hidden.is_contiguous() or getattr(kept, "shape", None) != (2, tokens, d_ff) or
             kept.dtype is not _torch.float32 or not kept.is_contiguous() or kept.get_device() != x.get_device()):
         _refuse(where, "saved is not what the forward call for these tensors returned")
-    calls = _chain()
-    w = _WORKLOAD(1, 1, 1, tokens, d_ff, d_in, d_out, 2)
-    space, need = _space(calls.gated_ffn_workspace, x, where, w, 1)
-    grads = tuple([x.new_empty(t.shape) for t in (x, w_gate, w_up, w_down)])
-    f = _FFN(code, activation, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), x.stride(0), w_gate.stride(0),
-             w_up.stride(0), w_down.stride(0), hidden.data_ptr(), kept.data_ptr(), 0,
-             space.data_ptr() if need else 0, need)
-    g = _FFN_GRAD(d_y.data_ptr(), d_y.stride(0), *[t.data_ptr() for t in grads])
-    code = calls.gated_ffn_backward(w, f, g, _current_stream())
+    try:
+        calls = _chain()
+        w = _WORKLOAD(1, 1, 1, tokens, d_ff, d_in, d_out, 2)
+        space, need = _space(calls.gated_ffn_workspace, x, where, w, 1)
+        grads = tuple([x.new_empty(t.shape) for t in (x, w_gate, w_up, w_down)])
+        f = _FFN(code, activation, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), x.stride(0), w_gate.stride(0),
+                 w_up.stride(0), w_down.stride(0), hidden.data_ptr(), kept.data_ptr(), 0,
+                 space.data_ptr() if need else 0, need)
+        g = _FFN_GRAD(d_y.data_ptr(), d_y.stride(0), *[t.data_ptr() for t in grads])
+        code = calls.gated_ffn_backward(w, f, g, _current_stream())
+    except (struct.error, OverflowError) as e:
+        _refuse(where, "an argument is no number that the call holds (%s)" % e)
     if code:
         _check(code, where)
     return grads

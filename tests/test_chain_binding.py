@@ -21,6 +21,15 @@ class Fake:
         s = torch.empty(self.shape, device="meta").stride()
         return s if i is None else s[i]
 
+    def new_empty(self, shape, dtype=None):
+        return Fake(*([shape] if isinstance(shape, int) else shape), dtype=dtype or self.dtype)
+
+    def data_ptr(self):
+        return 4096
+
+    def is_contiguous(self):
+        return True
+
 
 def attention(**kw):
     return Fake(2, 3, 4, 64, **kw), Fake(2, 5, 2, 64, **kw), Fake(2, 5, 2, 64, **kw)
@@ -119,3 +128,54 @@ def test_a_stream_of_the_tensors_device_is_made_current(monkeypatch):
     for call, args in calls({}):
         with pytest.raises(Entered):
             call(*args, stream=types.SimpleNamespace(device=torch.device("cuda", 0), device_index=0, cuda_stream=4096))
+
+
+# --- arguments that no call struct holds -----------------------------------------------------------------------------
+
+@pytest.fixture
+def no_library(monkeypatch):
+    """Everything up to the library's call, which a sound call gets to."""
+    made = []
+
+    class Calls:
+        def __getattr__(self, name):
+            return lambda *args: (None if name.endswith("workspace") else made.append(name)) or b.OK
+    monkeypatch.setattr(b, "_chain", Calls)
+    monkeypatch.setattr(b, "_current_device", lambda: 0)
+    monkeypatch.setattr(b, "_current_stream", lambda: 0)
+    return made
+
+
+def test_sound_calls_get_to_the_library(no_library):
+    b.mmee_attention(*attention())
+    b.mmee_gated_ffn(*block(), save=True)
+    b.mmee_gated_ffn_backward(Fake(4, 16), *block(), (Fake(4, 64), KEPT))
+    assert no_library == ["attention", "gated_ffn", "gated_ffn_backward"]
+
+
+KEPT = Fake(2, 4, 64, dtype=torch.float32)
+
+
+@pytest.mark.parametrize("scale", ["a", 1e39, 1j, [1.0]])
+def test_a_scale_that_is_no_32_bit_number_is_refused(scale, no_library):
+    refused(b.mmee_attention, *attention(), scale=scale)
+    assert not no_library
+
+
+@pytest.mark.parametrize("activation", [-1, 1 << 32, "silu", 1.5, None])
+def test_an_activation_that_is_no_number_of_one_is_refused(activation, no_library):
+    refused(b.mmee_gated_ffn, *block(), activation=activation)
+    refused(b.mmee_gated_ffn_backward, Fake(4, 16), *block(), (Fake(4, 64), KEPT), activation=activation)
+    assert not no_library
+
+
+def test_sizes_of_more_than_32_bits_are_refused(no_library):
+    refused(b.mmee_gated_ffn, Fake((1 << 32) + 4, 32), *block()[1:])
+    refused(b.mmee_attention, Fake(2, 1 << 32, 4, 64), *attention()[1:])
+    assert not no_library
+
+
+@pytest.mark.parametrize("saved", [None, (), (Fake(4, 64), None), (None, KEPT), (Fake(4, 64), KEPT, KEPT), [Fake(4, 64), KEPT]])
+def test_what_the_forward_call_did_not_return_is_refused(saved, no_library):
+    refused(b.mmee_gated_ffn_backward, Fake(4, 16), *block(), saved)
+    assert not no_library
