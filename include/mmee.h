@@ -422,7 +422,8 @@ int mmee_alu_peak(double out[4]);
 /* ------------------------------------------------------------------------------------------------
  * The chains themselves, run on this GPU.  Their sizes come as the workload that a mapping is searched
  * for; tensors are DEVICE memory of 16-bit values (word_bytes = 2), 16-byte aligned, the last dimension
- * contiguous, every other stride positive and a multiple of eight elements (a dimension of one entry may have any).
+ * contiguous, every other stride positive and a multiple of eight elements (a dimension of one entry may have any);
+ * 32-bit words (lse, kv_len) are aligned to their size.
  * Calls are asynchronous on cuda_stream, allocate nothing, keep nothing from call to call and may be
  * captured into a graph; sums are kept in 32 bits and no result depends on the order in which blocks
  * finish.  A call that returns another status than MMEE_OK has launched nothing or (MMEE_ERR_CUDA) left
