@@ -448,7 +448,7 @@ int mmee_alu_peak(double out[4]);
 #define MMEE_ATTENTION_MAX_D  128u
 typedef struct {
     uint32_t dtype;                          /* MMEE_F16 or MMEE_BF16                             */
-    float    scale;                          /* positive and finite                               */
+    float    scale;                          /* from 2^-126 to 2^127                              */
     const void *q, *k, *v;                   /* [batch][token][head][d], any order of strides     */
     void    *o;                              /* out (backward: in)                                */
     int64_t  q_stride[3], k_stride[3], v_stride[3], o_stride[3];   /* elements: batch, token, head */

@@ -159,7 +159,8 @@ inline int check(const mmee_workload_t* w, const mmee_attention_t* a, Problem* o
     if (w->d_qk > MMEE_ATTENTION_MAX_D || w->d_v > MMEE_ATTENTION_MAX_D) return MMEE_ERR_RANGE;
     if (w->batch > 4095 || w->q_heads > 65535 || (w->seq_q | w->seq_kv) >> 30) return MMEE_ERR_RANGE;
     if (a->dtype != MMEE_F16 && a->dtype != MMEE_BF16) return MMEE_ERR_ARG;
-    if (!(a->scale > 0.f) || !(a->scale < INFINITY)) return MMEE_ERR_ARG;
+    // (times log2 e it has to stay a normal number: masked scores, -infinity, are multiplied by it)
+    if (!(a->scale >= 0x1p-126f) || !(a->scale <= 0x1p127f)) return MMEE_ERR_ARG;
     if (((uintptr_t)a->lse | (uintptr_t)a->kv_len) % 4) return MMEE_ERR_ARG;
     out->q = {a->q, w->seq_q, w->q_heads, w->d_qk, strides(a->q_stride)};
     out->k = {a->k, w->seq_kv, w->kv_heads, w->d_qk, strides(a->k_stride)};
