@@ -55,11 +55,13 @@ __device__ __forceinline__ float act_value(uint32_t act, float g) {
 }
 
 // The block for few tokens, which the weights' way from memory bounds.  Up to kNarrow tokens: mmee_ffn_narrow.cu; up to kFew
-// tokens and weights of less than kFewBytes: mmee_ffn_tokens.cu, which starts faster and reads slower.
-// One token, us (narrow, few): 12.6 MB of weights 9.1 and 14.4; 67 MB 20.6 and 22.4; 403 MB 73.7 and 68.6.  Thirteen tokens, 67 MB:
-// 28.8 and 24.1.  128 tokens (narrow, tiles of 128 x 256): 25 MB 41 and 40, 67 MB 55 and 78, 403 MB 119 and 151.
+// tokens and weights of less than kFewBytes: mmee_ffn_tokens.cu, which starts faster and, with many rows, reads a little slower.
+// us of a captured call, weights from memory, one token / eight, few and narrow: 13 MB of weights 5.9 and 9.8 / 6.2 and 10.4; 67 MB 17.6 and
+// 19.3 / 20.1 and 20.1; 126 MB 25.3 and 26.6 / 27.0 and 27.8; 201 MB 36.3 and 38.3 / 38.4 and 40.1; 252 MB 46.2 and 45.2 / 50.2 and 46.7; 302 MB
+// 51.0 and 59.8 / 54.0 and 62.2; 403 MB 67.5 and 67.2 / 71.1 and 69.7 (two and four tokens in between): from 240 MB on it goes by how the rows
+// divide.  128 tokens (narrow, tiles of 128 x 256): 25 MB 41 and 40, 67 MB 55 and 78, 403 MB 119 and 151.
 constexpr uint32_t kFew = 8, kNarrow = 128;
-constexpr uint64_t kFewBytes = 96ull << 20;
+constexpr uint64_t kFewBytes = 224ull << 20;
 struct FfnTokens {
     uint32_t tokens, d_in, d_ff, d_out, act;
     const void *x, *w_gate, *w_up, *w_down;
