@@ -9,7 +9,8 @@ the cloud accelerator, latency-driven then energy-delay-product-driven, 3.39e9 m
     python bench.py [--gpus N] [--steps K] [--warmup W] [--impl ours|reference] [--workload NAME] [--run]
 
 --run also runs the workload's chains on this GPU (mmee_attention, or mmee_gated_ffn for the two-GEMM chains) and adds their
-times, next to the cycles of the best mapping that the search found, under "chains".
+times, next to the cycles of the best mapping that the search found, under "chains".  The gated block has a second projection that
+the searched two-GEMM chain has not: "products" gives both counts, and only where they agree are the two the same work.
 
 Prints one JSON line.  With N > 1 (under torchrun) every rank runs an independent replica on its
 own GPU: the search is launched per workload and does not shard in this build.
@@ -217,12 +218,12 @@ def run_chains(name, jobs, bests, steps=10):
             b.record()
             torch.cuda.synchronize()
             ms.append(a.elapsed_time(b))
-        # multiply-adds of the chain as it is searched; the gated block has a second projection
+        # multiply-adds of the chain that is run: the gated block has a second projection, the searched chain has not
         per_row = w["seq_kv"] * ((2 if gated else 1) * w["d_qk"] + w["d_v"])
         flops = 2 * w["batch"] * w["q_heads"] * w["seq_q"] * per_row
         mean = statistics.mean(ms[3:])
         out.append(dict(problem=cfg["name"], call=call.__name__, ms=mean, tflops=flops / mean / 1e9,
-                        searched=OBJ_NAMES[search["objective"]], mapping_idx=best.idx, mapping_latency_cycles=best.latency_cycles))
+                        products=dict(searched=2, run=3 if gated else 2), searched=OBJ_NAMES[search["objective"]], mapping_idx=best.idx, mapping_latency_cycles=best.latency_cycles))
         del inputs
     return out
 
@@ -264,6 +265,8 @@ def main():
     ap.add_argument("--workload", default="gqa", choices=sorted(WORKLOADS) + ["sweep", "ffn", "beyond", "reconfig"])
     ap.add_argument("--run", action="store_true", help="run the workload's chains on this GPU as well")
     args = ap.parse_args()
+    if args.run and (args.workload == "reconfig" or args.impl == "reference"):
+        ap.error("--run goes with this implementation's searches of a workload, not with reconfig or the reference")
     args.warmup = max(args.warmup, 3) if args.impl == "ours" else args.warmup
 
     rank = int(os.environ.get("RANK", "0"))
