@@ -92,10 +92,14 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
 // --- the order of kernels in a stream -------------------------------------------------------------------------------
 
 // A kernel that was launched early (LaunchAt::early) may run beside the one before it until it waits here; then that one is done, and
-// so is all before it.  Nothing in memory is touched before, but what no kernel of the same call writes.
+// so is all before it: every kernel here waits before it ends.  Before the wait it touches no memory but what nothing that may still
+// run writes.  What that is goes by the call: its first kernel may stand behind anything (a search, which releases at its start, with
+// others still running before it) and touches nothing before; a later one may read what no kernel of the call writes, if the
+// one before it releases after its own wait.
 __device__ __forceinline__ void wait_for_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-// From here on (in every block) the next kernel may be launched early.  After the wait: a kernel never runs beside any but the one
-// before it.
+// From here on (in every block) the next kernel may be launched early.  After the wait, so that the next one knows all but the
+// kernel before it to be done.  One exception: the kernel of dQ, which releases at once, beside that of dK and dV; what comes next is
+// a call's first kernel.
 __device__ __forceinline__ void release_stream() { asm volatile("griddepcontrol.launch_dependents;"); }
 
 // Sixteen bytes that are read once.  Not through the read-only path, which is for what nothing writes as long as a kernel runs: an
