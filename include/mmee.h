@@ -519,7 +519,7 @@ int mmee_gated_ffn_workspace(const mmee_workload_t* workload, uint32_t backward,
 /*
  * mmee_chain_status -- MMEE_OK, or MMEE_ERR_TIMEOUT once after a wait inside one of the chains' kernels on the current device
  * ran out (outputs of such a call are not a result).  Waits for the device's work.
- * mmee_chain_wait_limit -- how long a wait for a barrier in these kernels may last on the current device, in ns; 4e9 unless set.
+ * mmee_chain_wait_limit -- how long a wait for a barrier in these kernels may last on the current device, in ns, below 2^62; 4e9 unless set.
  * Kernels look at the clock after some 0.35 ms of a wait: a shorter limit ends it then.  Waits for the device's work.
  */
 int mmee_chain_status(void);

@@ -639,6 +639,8 @@ def mmee_chain_status() -> None:
 
 def mmee_chain_wait_limit(seconds: float = 4.0) -> None:
     """How long a wait for a barrier in the chains' kernels on the current device may last.  Waits for the device."""
+    if not 0 <= seconds < 2 ** 32:
+        _refuse("mmee_chain_wait_limit", "seconds from nothing to 2^32 are wanted")
     _check(library().mmee_chain_wait_limit(int(seconds * 1e9)), "mmee_chain_wait_limit")
 
 

@@ -78,4 +78,7 @@ extern "C" int mmee_chain_status(void) {
     return rc ? rc : any ? MMEE_ERR_TIMEOUT : MMEE_OK;
 }
 
-extern "C" int mmee_chain_wait_limit(uint64_t nanoseconds) { return all_waits(nullptr, &nanoseconds); }
+extern "C" int mmee_chain_wait_limit(uint64_t nanoseconds) {
+    if (nanoseconds >> 62) return MMEE_ERR_ARG;        // (it is added to the clock)
+    return all_waits(nullptr, &nanoseconds);
+}

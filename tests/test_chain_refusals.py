@@ -43,3 +43,15 @@ def test_the_ends_of_the_scales_are_taken(scale, seq_q):
         q = q * 0
     n = torch.tensor([300, 77, 0], dtype=torch.int32, device="cuda")
     attention.check_forward(q, k, v, n, scale)
+
+
+@pytest.mark.parametrize("ns", [1 << 62, (1 << 64) - 1])
+def test_limits_that_pass_the_clock_are_refused(ns):
+    assert mm.library().mmee_chain_wait_limit(ns) == mm.ERR_ARG
+
+
+@pytest.mark.parametrize("seconds", [-1.0, float("nan"), float("inf"), 2.0 ** 32])
+def test_limits_that_are_no_time_are_refused(seconds):
+    with pytest.raises(mm.MmeeError) as e:
+        mm.mmee_chain_wait_limit(seconds)
+    assert e.value.code == mm.ERR_ARG
