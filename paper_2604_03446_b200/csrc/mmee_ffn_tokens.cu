@@ -21,18 +21,6 @@ __device__ __forceinline__ uint4 read_token(const uint16_t* p) {
     return v;
 }
 
-template <bool BF16>
-__device__ __forceinline__ void mma16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    if (BF16)
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-    else
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
 // GATE: hidden from x, w_gate and w_up; otherwise y from hidden and w_down.
 // A warp has two turns of eight sixteen-byte reads a lane under way.  Measured at 4096-16384-4096, one token: two CTAs of eight
 // warps a multiprocessor with the second turn 73.7 us; four CTAs without it 79; one turn of sixteen reads 85; three CTAs, whose

@@ -65,3 +65,57 @@ def test_the_block_takes_weights_that_a_call_has_just_written(tokens):
         torch.cuda.synchronize()
         for g, w in zip(got, want):
             assert all(torch.equal(a, b) for a, b in zip(g, w))
+
+
+def training(x, ws, q, k, v, n):
+    """The block on tokens, attention of its rows, both backwards, weights changed in place, twice over."""
+    ws = [w.clone() for w in ws]
+    out = []
+    for _ in range(2):
+        y, kept = mm.mmee_gated_ffn(x, *ws, save=True)
+        o, saved = mm.mmee_attention(y.view(q.shape), k, v, kv_len=n)
+        dq, dk, dv = mm.mmee_attention_backward(q, y.view(q.shape), k, v, o, saved, kv_len=n)
+        grads = mm.mmee_gated_ffn_backward(dq.view(y.shape), x, *ws, kept)
+        for w, g in zip(ws, grads[1:]):
+            w.add_(g, alpha=-2.0 ** -6)
+        out += [y, o, dq, dk, dv, *grads]
+    return out + ws
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16], ids=["fp16", "bf16"])
+@pytest.mark.parametrize("tokens", [3, 64, 450])
+def test_training_steps_without_a_pause_on_streams_and_replayed(tokens, dtype):
+    """The same bits as with a pause after every step: eager, on two streams at once, and captured."""
+    gen = torch.Generator(device="cuda").manual_seed(tokens)
+    mk = lambda *s, std=1.0: (torch.randn(*s, generator=gen, device="cuda") * std).to(dtype)
+
+    def case():
+        return (mk(2 * tokens, 192), [mk(520, 192, std=0.07), mk(520, 192, std=0.07), mk(256, 520, std=0.04)],
+                mk(2, tokens, 4, 64, std=2.0 ** -8), mk(2, 200, 2, 64), mk(2, 200, 2, 64), torch.tensor([200, 31], dtype=torch.int32, device="cuda"))
+    cases = [case() for _ in range(3)]
+    want = []
+    for c in cases:
+        want.append(training(*c))
+        torch.cuda.synchronize()
+    for _ in range(3):
+        got = [training(*c) for c in cases]
+        streams = [torch.cuda.Stream() for _ in cases]
+        for s in streams:
+            s.wait_stream(torch.cuda.current_stream())
+        for s, c in zip(streams, cases):
+            with torch.cuda.stream(s):
+                got.append(training(*c))
+        torch.cuda.synchronize()
+        for i, g in enumerate(got):
+            assert all(torch.equal(a, b) for a, b in zip(g, want[i % 3]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = training(*cases[0])
+    for _ in range(2):
+        for t in out:
+            t.zero_()
+        graph.replay()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want[0]))
+    mm.mmee_chain_status()
