@@ -476,8 +476,8 @@ void add_product(Products* ps, Operand* (&ops)[kMostProducts][4], Product p, Ope
 // some 2^12 below the bound, 16 bits above fp16's smallest normal value then.
 // Bound by memory, as gate, up and w_down are read once more; a token to a block at a time, so that few tokens have many loads under
 // way.  The gradient's kernel, which needs the bounds for its results alone, starts beside it.  us of forward and gradients without and
-// with it: 777 tokens, 1000-2728-712, 113 and 114; 512 tokens, 1024-4096-1024, 86 and 87; 64 tokens, 2048-5464-2048, 96 and 103; eight
-// tokens, 4096-16384-4096, 303 and 329 (25 of them w_down's 134 MB).
+// with all this: 777 tokens, 1000-2728-712, 112 and 116; 512 tokens, 1024-4096-1024, 85 and 87; 64 tokens, 2048-5464-2048, 96 and 103; eight
+// tokens, 4096-16384-4096, 304 and 333 (25 of them w_down's 134 MB); 4096 tokens of that 4577 and 4750.
 constexpr uint32_t kTokenBounds = 1024, kWeightBounds = 592;
 struct BoundParams {
     const uint16_t *d_y, *w_down;

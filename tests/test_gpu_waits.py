@@ -59,11 +59,12 @@ def test_a_wait_that_runs_out_in_the_block(sizes, no_patience):
     assert (y == 0).all()
 
 
-def test_a_wait_that_runs_out_in_the_gradients(no_patience):
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "fp16"])
+def test_a_wait_that_runs_out_in_the_gradients(dtype, no_patience):
     """The gradient of hidden, whose kernel has asked for gate and up when its sums do not come."""
     mm.mmee_chain_status()
     tokens, d_in, d_ff, d_out = 130, 8, 8, 1 << 22
-    mk = lambda r, c: torch.zeros(r, c, dtype=torch.bfloat16, device="cuda")
+    mk = lambda r, c: torch.zeros(r, c, dtype=dtype, device="cuda")
     t = mk(tokens, d_in), mk(d_ff, d_in), mk(d_ff, d_in), mk(d_out, d_ff)
     _, saved = mm.mmee_gated_ffn(*t, save=True)
     mm.mmee_chain_status()
